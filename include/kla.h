@@ -329,6 +329,133 @@ int kla_decode_step_diag_opts(const void *q, const void *k, const void *v,
 int kla_beta(const void *k, const float *eta, float eps, float *beta,
              long n_token_heads, int dk, kla_dtype dt, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The operators around the recurrence in a layer: the short convolution ahead of it, another recurrence for hybrid
+ * layers, and the norms before and after a block.  The conventions above hold, except:
+ *   - Inputs whose row stride ld_* (elements from one token to the next) is an argument may be column ranges of a wider
+ *     tensor, e.g. of the output of one projection for several of them; a row itself is contiguous.  Everything else is
+ *     contiguous, and so are all outputs.
+ *   - Data pointers have to be aligned to their element only (A, states and checkpoints: 16 bytes).  Rows that start on
+ *     16-byte boundaries are taken 16 bytes at a time, others element by element, with the same results.
+ *   - Parameters (weights, biases, scales) and their gradients are fp32.
+ * All sums, states and norms are fp32; an output is rounded to dt once.  Results are deterministic (no atomics).
+ * ------------------------------------------------------------------------------------------------------------------ */
+enum { KLA_LAYER_SILU = 1,        /* kla_conv_*: y = p sigmoid(p) instead of y = p                                         */
+       KLA_LAYER_SOFTPLUS = 2,    /* kla_ssm_*: delta = log(1 + exp(raw + bias)) instead of raw + bias                     */
+       KLA_LAYER_SIGMOID = 4,     /* kla_gated_norm_*: the gate's activation is sigmoid(g) instead of g sigmoid(g)         */
+       KLA_LAYER_GATE_FIRST = 8   /* kla_gated_norm_*: the gate multiplies what is normalised instead of the result        */ };
+
+/*
+ * Short causal convolution of every channel:  p_t[d] = bias[d] + sum_j weight[d][j] x_{t-W+1+j}[d],  y = p sigmoid(p) or p.
+ * Before a sequence's first token stands its state, the last W - 1 inputs of the tokens before, oldest first (or zeros).
+ *   x           [N, T, D] dt, rows ld_x apart       in
+ *   weight      [D, W], bias [D] or NULL            in
+ *   state       [n_states, W-1, D] dt or NULL       in   n_states, packed batches: as in kla_chunk_fwd
+ *   y           [N, T, D] dt                        out
+ *   state_out   [n_states, W-1, D] dt or NULL       out  the last W - 1 inputs; must not alias state
+ * W in 2..4, any D >= 1.
+ */
+int kla_conv_fwd(const void *x, long ld_x, const float *weight, const float *bias, const void *state,
+                 void *y, void *state_out,
+                 const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                 int N, int T, int D, int W, kla_dtype dt, void *hip_stream, unsigned opts);
+
+/* Gradients of sum <d_y, y> + sum <d_state_out, state_out> (d_state_out NULL: zeros) from the inputs of the forward.
+ * d_y, dx [N, T, D] contiguous; dbias, d_state NULL if unwanted; workspace 256-byte aligned. */
+size_t kla_conv_bwd_workspace_bytes(int N, int T, int D, int W);
+int kla_conv_bwd(const void *x, long ld_x, const float *weight, const float *bias, const void *state,
+                 const void *d_y, const void *d_state_out,
+                 void *dx, float *dweight, float *dbias, void *d_state,
+                 const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                 int N, int T, int D, int W, kla_dtype dt,
+                 void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
+
+/* One token for B sequences: x [B, D], y [B, D], state [B, W-1, D] updated in place. */
+int kla_conv_step(const void *x, long ld_x, const float *weight, const float *bias, void *state, void *y,
+                  int B, int D, int W, kla_dtype dt, void *hip_stream, unsigned opts);
+
+/*
+ * Selective state space scan, one decay per channel and state:
+ *     delta_t = softplus(raw_t + delta_bias) (or without softplus)
+ *     h_t[d][n] = exp(delta_t[d] A[d][n]) h_{t-1}[d][n] + delta_t[d] u_t[d] B_t[n]
+ *     y_t[d] = (sum_n C_t[n] h_t[d][n] + skip[d] u_t[d]) z_t[d] sigmoid(z_t[d])
+ *   u, delta (raw), z   [N, T, D] dt, rows ld_u, ld_delta, ld_z apart   in   z NULL: no gate
+ *   A           [D, S]                                                  in   (negative expected)
+ *   B, C        [N, T, G, S] dt, tokens ld_B, ld_C apart                in   group g serves channels g D/G .. (g+1) D/G - 1
+ *   skip, delta_bias [D]                                                in   or NULL
+ *   h0          [n_states, D, S] fp32                                   in   or NULL for zeros
+ *   y           [N, T, D] dt                                            out
+ *   hT          [n_states, D, S] fp32                                   out  or NULL; may alias h0
+ *   saved       kla_ssm_saved_bytes(...): the states at every 256/S-th token, for the backward; or NULL
+ * S in {8, 16, 32, 64}; D a multiple of G; at most 65535 sequences.  The queries need only know whether the batch is packed and
+ * of how many sequences.
+ */
+size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, int n_seq);
+size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, int n_seq);
+int kla_ssm_fwd(const void *u, long ld_u, const void *delta, long ld_delta, const float *A,
+                const void *B, long ld_B, const void *C, long ld_C,
+                const float *skip, const void *z, long ld_z, const float *delta_bias, const float *h0,
+                void *y, float *hT, float *saved, size_t saved_bytes,
+                const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                int N, int T, int D, int G, int S, kla_dtype dt,
+                void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
+
+/* Gradients of sum <d_y, y> + sum <d_hT, hT> (d_hT NULL: zeros) from the inputs of the forward; saved: what a forward with these
+ * arguments left, or NULL (it is formed again, in the workspace).  du, ddelta, dz [N, T, D], dB, dC [N, T, G, S] contiguous; dz
+ * needed iff z; dskip, ddelta_bias, dh0 NULL if unwanted. */
+size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, int n_seq, int has_saved);
+int kla_ssm_bwd(const void *u, long ld_u, const void *delta, long ld_delta, const float *A,
+                const void *B, long ld_B, const void *C, long ld_C,
+                const float *skip, const void *z, long ld_z, const float *delta_bias, const float *h0,
+                const void *d_y, const float *d_hT, const float *saved, size_t saved_bytes,
+                void *du, void *ddelta, float *dA, void *dB, void *dC, float *dskip, void *dz, float *ddelta_bias, float *dh0,
+                const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                int N, int T, int D, int G, int S, kla_dtype dt,
+                void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
+
+/* One token for N sequences: u, delta, z, y [N, D], B, C [N, G, S]; h [N, D, S] fp32 updated in place. */
+int kla_ssm_step(const void *u, long ld_u, const void *delta, long ld_delta, const float *A,
+                 const void *B, long ld_B, const void *C, long ld_C,
+                 const float *skip, const void *z, long ld_z, const float *delta_bias, float *h, void *y,
+                 int N, int D, int G, int S, kla_dtype dt, void *hip_stream, unsigned opts);
+
+/*
+ * Before a block: the residual stream plus the scaled output of the block before, and its RMS norm.
+ *     r' = residual + scale x,   y = weight r' / sqrt(mean(r'^2) + eps)        (0 for a row of zeros with eps = 0)
+ *   x           [M, D] dt, rows ld_x apart          in
+ *   residual    [M, D] res_dt                       in   or NULL: r' = scale x
+ *   scale       [D] or NULL for ones, weight [D]    in
+ *   y           [M, D] dt                           out  of the unrounded r'
+ *   residual_out [M, D] res_dt                      out  r', or NULL if unwanted; may alias residual
+ * res_dt: dt or fp32.  D at most 8192.
+ */
+int kla_add_norm_fwd(const void *x, long ld_x, const void *residual, const float *scale, const float *weight, float eps,
+                     void *y, void *residual_out, long M, int D, kla_dtype dt, kla_dtype res_dt, void *hip_stream);
+
+/* Gradients of sum <d_y, y> + sum <d_residual_out, r'> (d_residual_out NULL: zeros).  dscale, d_residual NULL if unwanted;
+ * d_residual may alias d_residual_out. */
+size_t kla_add_norm_bwd_workspace_bytes(long M, int D, kla_dtype dt);
+int kla_add_norm_bwd(const void *x, long ld_x, const void *residual, const float *scale, const float *weight, float eps,
+                     const void *d_y, const void *d_residual_out,
+                     void *dx, void *d_residual, float *dscale, float *dweight,
+                     long M, int D, kla_dtype dt, kla_dtype res_dt,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * After a block: RMS norm of every head, times the activated gate (or, KLA_LAYER_GATE_FIRST, of the head times the gate).
+ *     y = weight n act(gate), n = x / sqrt(mean(x^2) + eps);    or  y = weight n, n of x act(gate)
+ *   x, gate     [M, H, D] dt, tokens ld_x, ld_gate apart   in
+ *   weight      [D]                                        in   the same for all heads
+ *   y           [M, H, D] dt                               out
+ * D at most 8192.
+ */
+int kla_gated_norm_fwd(const void *x, long ld_x, const void *gate, long ld_gate, const float *weight, float eps, void *y,
+                       long M, int H, int D, kla_dtype dt, void *hip_stream, unsigned opts);
+size_t kla_gated_norm_bwd_workspace_bytes(long M, int H, int D, kla_dtype dt);
+int kla_gated_norm_bwd(const void *x, long ld_x, const void *gate, long ld_gate, const float *weight, float eps,
+                       const void *d_y, void *dx, void *d_gate, float *dweight, long M, int H, int D, kla_dtype dt,
+                       void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
+
 /*
  * Test hook: the per-chunk objects the first stage of kla_chunk_fwd leaves in its workspace,
  * unpacked to plain row-major fp32 so that they can be compared one by one with eqs. (6)-(7).

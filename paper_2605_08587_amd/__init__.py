@@ -124,7 +124,7 @@ def lib():
                 raise RuntimeError("libkla.so is not built: run `python -m paper_2605_08587_amd.build` "
                                    "(there is no CPU fallback)")
             l = ctypes.CDLL(LIB_PATH)
-            for name, (res, args) in _SIGNATURES.items():
+            for name, (res, args) in {**_SIGNATURES, **layer.SIGNATURES}.items():
                 fn = getattr(l, name)
                 fn.restype, fn.argtypes = res, args
             _native, _lib = _load_native(l), l
@@ -635,3 +635,9 @@ def kla_chunk(q, k, v, log_alpha, eta, eps, h0=None, cu_seqlens=None, cu_seqlens
             return r
     return _KlaChunk.apply(q, k, v, log_alpha, eta, h0, eps, cu_seqlens, cu_seqlens_host, normalize_q, gdn_beta,
                            bool(save) and torch.is_grad_enabled())
+
+
+from . import layer  # noqa: E402  (needs the names above)
+from .layer import (KLA_LAYER_GATE_FIRST, KLA_LAYER_SIGMOID, KLA_LAYER_SILU, KLA_LAYER_SOFTPLUS,  # noqa: E402, F401
+                    kla_add_norm, kla_add_norm_bwd, kla_add_norm_fwd, kla_conv, kla_conv_bwd, kla_conv_fwd, kla_conv_step, kla_gated_norm,
+                    kla_gated_norm_bwd, kla_gated_norm_fwd, kla_ssm, kla_ssm_bwd, kla_ssm_fwd, kla_ssm_step)

@@ -1,0 +1,370 @@
+// Short causal convolution of every channel with its activation, forward, backward and for single tokens:
+//   p_t = b + sum_j w_j x_{t-W+1+j},  y_t = p_t sigmoid(p_t)  (or p_t)
+// and backward, with p'_t = d_y_t dy_t/dp_t:
+//   d_x_s = sum_j w_j p'_{s+W-1-j},  d_w_j = sum_t p'_t x_{t-W+1+j},  d_b = sum_t p'_t.
+// Before a sequence's first token stands its state, the last W - 1 inputs of earlier tokens (or zeros); nothing of another
+// sequence is ever multiplied, not even by zero.  Two passes over the elements forward, three backward: bound by memory.
+#include "kla_layer.hpp"
+
+namespace kla {
+
+template <bool SILU> __device__ __forceinline__ float act(float p) { return SILU ? p * sigmoid(p) : p; }
+template <bool SILU> __device__ __forceinline__ float act_slope(float p)
+{
+    if constexpr (!SILU) return 1.f;
+    const float s = sigmoid(p);
+    return s * fmaf(p, 1.f - s, 1.f);
+}
+
+// Threads of a workgroup along a row, a power of two up to a wave: V channels each.
+static int row_threads(long n_vec)
+{
+    int tx = 1;
+    while (tx < 64 && tx < n_vec) tx *= 2;
+    return tx;
+}
+
+// Taps and bias of V channels, and the W - 1 inputs ahead of token t of sequence p.
+template <int W, int V> struct Taps {
+    float w[W][V], b[V];
+    __device__ __forceinline__ void load(const float* weight, const float* bias, int c)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j][i] = weight[(long)(c + i) * W + j];
+            b[i] = bias ? bias[c + i] : 0.f;
+        }
+    }
+};
+template <typename T, int W, int V> __device__ __forceinline__ void load_window(const ConvArgs<T>& a, const Place& p, long t, int c, Floats<V> (&win)[W])
+{
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        const long s = t - (W - 1) + j;
+        if (s >= p.first) win[j] = load_vec<T, V>(a.x + s * a.ld_x + c);
+        else if (a.state) win[j] = load_vec<T, V>(a.state + ((long)p.n * (W - 1) + (W - 1) + (s - p.first)) * a.D + c);
+        else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) win[j].v[i] = 0.f;
+        }
+    }
+}
+
+constexpr int kRowsAhead = 8;                            // rows in flight per thread
+
+// A thread takes V channels of L consecutive tokens with the window in registers; a workgroup's strips follow each other, so
+// that the W - 1 rows before a strip come from the caches.  Workgroups from n_main on write the states instead.
+template <typename T, int W, int V, bool SILU>
+__global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs<T> a, int tx, int L, int blocks_c, unsigned n_main)
+{
+    const int lane = threadIdx.x % tx, row = threadIdx.x / tx, ty = 256 / tx;
+    const unsigned blk = blockIdx.x < n_main ? blockIdx.x : blockIdx.x - n_main;
+    const int c = ((int)(blk % blocks_c) * tx + lane) * V;
+    const long strip = (long)(blk / blocks_c) * ty + row;
+    if (c >= a.D) return;
+    if (blockIdx.x >= n_main) {                          // strip: the sequence whose state is written
+        if (strip >= a.seqs.n_seq) return;
+        const Place p = sequence(a.seqs, (int)strip);
+        Floats<V> win[W];
+        load_window<T, W, V>(a, p, p.end, c, win);
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) store_vec<T, V>(a.state_out + ((long)p.n * (W - 1) + j) * a.D + c, win[j]);
+        return;
+    }
+    const long t0 = strip * L, t1 = min(t0 + L, a.M);
+    if (t0 >= t1) return;
+    Taps<W, V> k;
+    k.load(a.weight, a.bias, c);
+    Place p = sequence_of(a.seqs, t0);
+    Floats<V> win[W];
+    load_window<T, W, V>(a, p, t0, c, win);
+    for (long base = t0; base < t1; base += kRowsAhead) {
+        Floats<V> in[kRowsAhead];
+#pragma unroll
+        for (int r = 0; r < kRowsAhead; ++r) in[r] = load_vec<T, V>(a.x + min(base + r, t1 - 1) * a.ld_x + c);
+#pragma unroll
+        for (int r = 0; r < kRowsAhead; ++r) {
+            const long t = base + r;
+            if (t < t1) {
+                if (t == p.end) {
+                    p = sequence_of(a.seqs, t);
+                    load_window<T, W, V>(a, p, t, c, win);
+                }
+                win[W - 1] = in[r];
+                Floats<V> out;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float s = k.b[i];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) s = fmaf(k.w[j][i], win[j].v[i], s);
+                    out.v[i] = act<SILU>(s);
+                }
+                store_vec<T, V>(a.y + t * a.D + c, out);
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
+            }
+        }
+    }
+}
+
+// Backward: the same strips; p' is formed once per token of the strip and again for the W - 1 tokens behind it, whose
+// gradients reach into it.  acc[j] gathers d_x of token t - (W - 1) + j; the sums for the taps stay in registers, are joined over the
+// workgroup's strips and leave one row of partial[blocks_t][D W + D] per workgroup.  Workgroups from n_main on form the gradients of
+// the states instead.
+template <typename T, int W, int V, bool SILU>
+__global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs<T> a, int tx, int L, int blocks_c, unsigned n_main)
+{
+    const int lane = threadIdx.x % tx, row = threadIdx.x / tx, ty = 256 / tx;
+    const unsigned blk = blockIdx.x < n_main ? blockIdx.x : blockIdx.x - n_main;
+    const int c = ((int)(blk % blocks_c) * tx + lane) * V;
+    const long strip = (long)(blk / blocks_c) * ty + row;
+    const bool mine = c < a.D;
+    Taps<W, V> k;
+    if (mine) k.load(a.weight, a.bias, c);
+
+    if (blockIdx.x >= n_main) {
+        if (!mine || strip >= a.seqs.n_seq) return;
+        const Place p = sequence(a.seqs, (int)strip);
+        const long len = p.end - p.first;
+        Floats<V> win[W], ds[W - 1];
+        load_window<T, W, V>(a, p, p.first, c, win);
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) ds[i].v[e] = 0.f;
+            // entry i is an entry of the state behind the sequence too where the sequence has fewer than W - 1 tokens
+            if (a.d_state_out && i >= len) ds[i] = load_vec<T, V>(a.d_state_out + ((long)p.n * (W - 1) + (i - len)) * a.D + c);
+        }
+#pragma unroll
+        for (int r = 0; r < W - 1; ++r) {
+            if (r >= len) break;
+            win[W - 1] = load_vec<T, V>(a.x + (p.first + r) * a.ld_x + c);
+            const Floats<V> dy = load_vec<T, V>(a.d_y + (p.first + r) * (long)a.D + c);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float s = k.b[e];
+#pragma unroll
+                for (int j = 0; j < W; ++j) s = fmaf(k.w[j][e], win[j].v[e], s);
+                const float dp = dy.v[e] * act_slope<SILU>(s);
+#pragma unroll
+                for (int j = 0; j + r < W - 1; ++j) ds[j + r].v[e] = fmaf(k.w[j][e], dp, ds[j + r].v[e]);
+            }
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
+        }
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) store_vec<T, V>(a.d_state + ((long)p.n * (W - 1) + i) * a.D + c, ds[i]);
+        return;
+    }
+
+    float dw[W][V], db[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        db[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) dw[j][e] = 0.f;
+    }
+    const long t0 = strip * L, t1 = min(t0 + L, a.M);
+    if (mine && t0 < t1) {
+        const long t2 = min(t1 + W - 1, a.M);
+        Place p = sequence_of(a.seqs, t0);
+        Floats<V> win[W], acc[W];
+        load_window<T, W, V>(a, p, t0, c, win);
+        auto clear = [&]() {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[j].v[e] = 0.f;
+        };
+        // d_x of token s, where it is this strip's and of the present sequence
+        auto emit = [&](long s, Floats<V> g) {
+            if (s < t0 || s < p.first || s >= t1) return;
+            const long i = s - (p.end - (W - 1));
+            if (a.d_state_out && i >= 0) {
+                const Floats<V> d = load_vec<T, V>(a.d_state_out + ((long)p.n * (W - 1) + i) * a.D + c);
+#pragma unroll
+                for (int e = 0; e < V; ++e) g.v[e] += d.v[e];
+            }
+            store_vec<T, V>(a.dx + s * (long)a.D + c, g);
+        };
+        clear();
+        long t = t0;
+        bool on = true;
+        for (long base = t0; base < t2 && on; base += kRowsAhead) {
+            Floats<V> xin[kRowsAhead], gin[kRowsAhead];
+#pragma unroll
+            for (int r = 0; r < kRowsAhead; ++r) {
+                const long at = min(base + r, t2 - 1);
+                xin[r] = load_vec<T, V>(a.x + at * a.ld_x + c);
+                gin[r] = load_vec<T, V>(a.d_y + at * a.D + c);
+            }
+#pragma unroll
+            for (int r = 0; r < kRowsAhead; ++r) {
+                t = base + r;
+                if (t < t2 && on) {
+                    if (t == p.end) {
+#pragma unroll
+                        for (int j = 0; j < W - 1; ++j) emit(t - (W - 1) + j, acc[j]);
+                        clear();
+                        if (t >= t1) on = false;
+                        else {
+                            p = sequence_of(a.seqs, t);
+                            load_window<T, W, V>(a, p, t, c, win);
+                        }
+                    }
+                    if (on) {
+                        win[W - 1] = xin[r];
+                        const bool own = t < t1;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            float s = k.b[e];
+#pragma unroll
+                            for (int j = 0; j < W; ++j) s = fmaf(k.w[j][e], win[j].v[e], s);
+                            const float dp = gin[r].v[e] * act_slope<SILU>(s);
+#pragma unroll
+                            for (int j = 0; j < W; ++j) acc[j].v[e] = fmaf(k.w[j][e], dp, acc[j].v[e]);
+                            if (own) {
+                                db[e] += dp;
+#pragma unroll
+                                for (int j = 0; j < W; ++j) dw[j][e] = fmaf(dp, win[j].v[e], dw[j][e]);
+                            }
+                        }
+                        emit(t - (W - 1), acc[0]);
+#pragma unroll
+                        for (int j = 0; j < W - 1; ++j) { acc[j] = acc[j + 1]; win[j] = win[j + 1]; }
+#pragma unroll
+                        for (int e = 0; e < V; ++e) acc[W - 1].v[e] = 0.f;
+                    }
+                }
+            }
+        }
+        if (on) {                                        // the batch ends within W - 1 tokens: nothing follows these
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) emit(t2 - (W - 1) + j, acc[j]);
+        }
+    }
+    __shared__ float red[256][V * (W + 1) + 1];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) red[threadIdx.x][e * W + j] = dw[j][e];
+        red[threadIdx.x][V * W + e] = db[e];
+    }
+    __syncthreads();
+    const int nc = min(tx * V, a.D - (int)(blk % blocks_c) * tx * V);    // channels of this workgroup
+    float* out = a.partial + (long)(blk / blocks_c) * ((long)a.D * (W + 1));
+    const int c0 = (int)(blk % blocks_c) * tx * V;
+    for (int i = threadIdx.x; i < nc * (W + 1); i += 256) {
+        const bool tap = i < nc * W;
+        const int ch = tap ? i / W : i - nc * W, at = tap ? (ch % V) * W + i % W : V * W + ch % V;
+        float s = 0.f;
+        for (int r = 0; r < ty; ++r) s += red[r * tx + ch / V][at];
+        out[tap ? (long)c0 * W + i : (long)a.D * W + c0 + ch] = s;
+    }
+}
+
+// One token for B sequences: a thread per channel and sequence.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void conv_step_kernel(const T* __restrict__ x, long ld_x, const float* __restrict__ weight,
+                                                        const float* __restrict__ bias, T* __restrict__ state, T* __restrict__ y, int D,
+                                                        int blocks_c, bool silu)
+{
+    const int c = (blockIdx.x % blocks_c) * 256 + threadIdx.x;
+    const long b = blockIdx.x / blocks_c;
+    if (c >= D) return;
+    T* st = state + b * (W - 1) * D + c;
+    T line[W];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) line[j] = st[(long)j * D];
+    line[W - 1] = x[b * ld_x + c];
+    float s = bias ? bias[c] : 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) s = fmaf(weight[(long)c * W + j], to_float(line[j]), s);
+    y[b * D + c] = from_float<T>(silu ? s * sigmoid(s) : s);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) st[(long)j * D] = line[j + 1];
+}
+
+ConvBwdPlan conv_bwd_plan(long M, int D)
+{
+    // laid out for four channels per thread; with one channel each there are more workgroups along a row, not more partial rows
+    ConvBwdPlan p;
+    p.tx = row_threads((D + 3) / 4);
+    p.ty = 256 / p.tx;
+    p.L = 32;
+    const long strips = (M + p.L - 1) / p.L;
+    p.blocks_t = (strips + p.ty - 1) / p.ty;
+    return p;
+}
+
+template <typename T, int W, int V, bool SILU> static hipError_t conv_fwd(const ConvArgs<T>& a, hipStream_t st)
+{
+    const long n_vec = (a.D + V - 1) / V;
+    const int tx = row_threads(n_vec), ty = 256 / tx, blocks_c = (int)((n_vec + tx - 1) / tx);
+    int L = 16;
+    const long strips = (a.M + L - 1) / L, n_main = (strips + ty - 1) / ty * blocks_c;
+    const long n_state = a.state_out ? (a.seqs.n_seq + (long)ty - 1) / ty * blocks_c : 0;
+    if (n_main + n_state == 0) return hipSuccess;
+    if (n_main + n_state > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((conv_fwd_kernel<T, W, V, SILU>), dim3((unsigned)(n_main + n_state)), dim3(256), 0, st, a, tx, L, blocks_c, (unsigned)n_main);
+    return hipGetLastError();
+}
+template <typename T, int W, int V, bool SILU> static hipError_t conv_bwd(const ConvArgs<T>& a, float* dweight, float* dbias, hipStream_t st)
+{
+    const ConvBwdPlan p = conv_bwd_plan(a.M, a.D);
+    const int blocks_c = (a.D + p.tx * V - 1) / (p.tx * V);
+    const long n_main = p.blocks_t * blocks_c, n_state = a.d_state ? (a.seqs.n_seq + (long)p.ty - 1) / p.ty * blocks_c : 0;
+    if (n_main + n_state > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (n_main + n_state > 0) {
+        hipLaunchKernelGGL((conv_bwd_kernel<T, W, V, SILU>), dim3((unsigned)(n_main + n_state)), dim3(256), 0, st, a, p.tx, p.L, blocks_c, (unsigned)n_main);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return launch_column_sums(a.partial, p.blocks_t, {{(long)a.D * W, a.D, 0}, {dweight, dbias, nullptr}}, st);
+}
+
+template <typename T, int V, typename F> static hipError_t by_taps(int W, bool silu, F&& f)
+{
+    switch (W * 2 + (silu ? 1 : 0)) {
+        case 4: return f(IntC<2>(), IntC<V>(), IntC<0>());
+        case 5: return f(IntC<2>(), IntC<V>(), IntC<1>());
+        case 6: return f(IntC<3>(), IntC<V>(), IntC<0>());
+        case 7: return f(IntC<3>(), IntC<V>(), IntC<1>());
+        case 8: return f(IntC<4>(), IntC<V>(), IntC<0>());
+        default: return f(IntC<4>(), IntC<V>(), IntC<1>());
+    }
+}
+template <typename T> hipError_t launch_conv_fwd(const ConvArgs<T>& a, int W, bool silu, bool vec, hipStream_t st)
+{
+    auto f = [&](auto w, auto v, auto s) { return conv_fwd<T, w.value, v.value, (s.value != 0)>(a, st); };
+    return vec ? by_taps<T, kVec<T>>(W, silu, f) : by_taps<T, 1>(W, silu, f);
+}
+template <typename T> hipError_t launch_conv_bwd(const ConvArgs<T>& a, int W, bool silu, bool vec, float* dweight, float* dbias, hipStream_t st)
+{
+    auto f = [&](auto w, auto v, auto s) { return conv_bwd<T, w.value, v.value, (s.value != 0)>(a, dweight, dbias, st); };
+    return vec ? by_taps<T, 4>(W, silu, f) : by_taps<T, 1>(W, silu, f);
+}
+template <typename T> hipError_t launch_conv_step(const T* x, long ld_x, const float* weight, const float* bias, T* state, T* y, int B, int D, int W,
+                                                  bool silu, hipStream_t st)
+{
+    const int blocks_c = (D + 255) / 256;
+    const long blocks = (long)blocks_c * B;
+    if (blocks == 0) return hipSuccess;
+    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks), block(256);
+    switch (W) {
+        case 2:  hipLaunchKernelGGL((conv_step_kernel<T, 2>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+        case 3:  hipLaunchKernelGGL((conv_step_kernel<T, 3>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+        default: hipLaunchKernelGGL((conv_step_kernel<T, 4>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+    }
+    return hipGetLastError();
+}
+
+#define KLA_CONV(T)                                                                                                                       \
+    template hipError_t launch_conv_fwd<T>(const ConvArgs<T>&, int, bool, bool, hipStream_t);                                             \
+    template hipError_t launch_conv_bwd<T>(const ConvArgs<T>&, int, bool, bool, float*, float*, hipStream_t);                             \
+    template hipError_t launch_conv_step<T>(const T*, long, const float*, const float*, T*, T*, int, int, int, bool, hipStream_t);
+KLA_CONV(float)
+KLA_CONV(bf16_t)
+
+}  // namespace kla

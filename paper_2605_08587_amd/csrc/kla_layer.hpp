@@ -1,0 +1,170 @@
+// What the operators around the recurrence share (short convolution, selective scan, norms): where a token lies in its batch,
+// vector loads, activations, and the launchers' arguments.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kla_common.hpp"
+
+namespace kla {
+
+// option bits (the values of KLA_LAYER_* in include/kla.h)
+constexpr unsigned kLayerSilu = 1u, kLayerSoftplus = 2u, kLayerSigmoid = 4u, kLayerGateFirst = 8u;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// 2^x and 1/x in hardware (1 ulp each)
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float rcp_hw(float x) { return __builtin_amdgcn_rcpf(x); }
+__device__ __forceinline__ float sigmoid(float x) { return rcp_hw(1.f + exp2_hw(-kLog2e * x)); }
+// log(1 + e^x) = max(x, 0) + log1p(e^-|x|), the second term as 2 atanh(s) = 2 (s + s^3/3 + ...), s = e/(2 + e) <= 1/3: full
+// relative precision also where the result is as small as e^x itself (a logarithm of 1 + e loses it there).
+__device__ __forceinline__ float softplus(float x)
+{
+    const float e = exp2_hw(-kLog2e * fabsf(x));
+    const float s = e * rcp_hw(2.f + e), q = s * s;
+    float p = 1.f / 15.f;
+    p = fmaf(p, q, 1.f / 13.f);
+    p = fmaf(p, q, 1.f / 11.f);
+    p = fmaf(p, q, 1.f / 9.f);
+    p = fmaf(p, q, 1.f / 7.f);
+    p = fmaf(p, q, 1.f / 5.f);
+    p = fmaf(p, q, 1.f / 3.f);
+    p = fmaf(p, q, 1.f);
+    // (a NaN stays one: fmaxf alone would drop it, the sum with p does not)
+    return fmaf(2.f * s, p, fmaxf(x, 0.f));
+}
+
+// V consecutive elements <-> fp32 registers; V * sizeof(T) is 16 or 8 bytes, aligned so, or V = 1.
+template <int V> struct Floats { float v[V]; };
+template <typename T, int V> __device__ __forceinline__ Floats<V> load_vec(const T* p)
+{
+    Floats<V> r;
+    if constexpr (V == 1) {
+        r.v[0] = to_float(*p);
+    } else if constexpr (sizeof(T) == 4) {
+        static_assert(V % 4 == 0, "whole float4");
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const float4 f = reinterpret_cast<const float4*>(p)[i];
+            r.v[4 * i] = f.x; r.v[4 * i + 1] = f.y; r.v[4 * i + 2] = f.z; r.v[4 * i + 3] = f.w;
+        }
+    } else {
+        static_assert(V == 4 || V == 8, "8 or 16 bytes");
+        uint32_t w[V / 2];
+        if constexpr (V == 8) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            w[0] = u.x; w[1] = u.y;
+        }
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            r.v[2 * i] = __uint_as_float(w[i] << 16);
+            r.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, const Floats<V>& r)
+{
+    if constexpr (V == 1) {
+        *p = from_float<T>(r.v[0]);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i)
+            reinterpret_cast<float4*>(p)[i] = make_float4(r.v[4 * i], r.v[4 * i + 1], r.v[4 * i + 2], r.v[4 * i + 3]);
+    } else if constexpr (V == 8) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(r.v[0], r.v[1]), pack_bf16x2(r.v[2], r.v[3]),
+                                                  pack_bf16x2(r.v[4], r.v[5]), pack_bf16x2(r.v[6], r.v[7]));
+    } else {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(r.v[0], r.v[1]), pack_bf16x2(r.v[2], r.v[3]));
+    }
+}
+// Elements of T in 16 bytes
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
+
+// The sequences of a batch of flattened tokens: offsets cu[n_seq + 1] of a packed batch, or cu = NULL and n_seq sequences of T tokens.
+struct Seqs { const int* cu; int n_seq; int T; };
+struct Place { int n; long first, end; };                // a sequence: its number, first token, token after its last
+__device__ __forceinline__ Place sequence(const Seqs& s, int n)
+{
+    if (s.cu) return {n, s.cu[n], s.cu[n + 1]};
+    return {n, (long)n * s.T, ((long)n + 1) * s.T};
+}
+// the sequence of token t (sequences without a token hold none)
+__device__ __forceinline__ Place sequence_of(const Seqs& s, long t)
+{
+    if (!s.cu) return sequence(s, (int)(t / s.T));
+    int lo = 0, hi = s.n_seq - 1;                        // last n with cu[n] <= t
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (s.cu[mid] <= t) lo = mid; else hi = mid - 1; }
+    return sequence(s, lo);
+}
+
+// ---- launchers ------------------------------------------------------------------------------------------------------------------
+// Sums over the rows of partial[P][n0 + n1 + n2] in a fixed order, the columns to up to three outputs (each may be NULL).
+struct ColumnSums { long n[3]; float* out[3]; };
+hipError_t launch_column_sums(const float* partial, long P, const ColumnSums& s, hipStream_t st);
+
+template <typename T> struct ConvArgs {
+    const T* x; long ld_x; const float* weight; const float* bias; const T* state;      // bias, state: or NULL
+    T* y; T* state_out;                                                                   // state_out: or NULL
+    const T* d_y; const T* d_state_out; T* dx; T* d_state; float* partial;               // backward
+    Seqs seqs; long M; int D;
+};
+// Threads along a row of D channels and rows of threads (strips) of one workgroup of the backward, and its strips' tokens: what
+// lays out the partial sums.
+struct ConvBwdPlan { int tx, ty, L; long blocks_t; };
+ConvBwdPlan conv_bwd_plan(long M, int D);
+template <typename T> hipError_t launch_conv_fwd(const ConvArgs<T>& a, int W, bool silu, bool vec, hipStream_t st);
+template <typename T> hipError_t launch_conv_bwd(const ConvArgs<T>& a, int W, bool silu, bool vec, float* dweight, float* dbias, hipStream_t st);
+template <typename T> hipError_t launch_conv_step(const T* x, long ld_x, const float* weight, const float* bias, T* state, T* y, int B, int D, int W,
+                                                  bool silu, hipStream_t st);
+
+// T: type of x, y; R: type of the residual stream
+template <typename T, typename R> struct AddNormArgs {
+    const T* x; long ld_x; const R* residual; const float* scale; const float* weight; float eps;   // residual, scale: or NULL
+    T* y; R* residual_out;                                                                           // residual_out: or NULL
+    const T* d_y; const R* d_residual_out; T* dx; R* d_residual; float* partial;                    // backward; d_residual_out, d_residual: or NULL
+    long M; int D;
+};
+template <typename T> struct GatedNormArgs {
+    const T* x; long ld_x; const T* gate; long ld_gate; const float* weight; float eps;
+    T* y;
+    const T* d_y; T* dx; T* d_gate; float* partial;
+    long M; int H, D;                                    // M tokens of H rows of D
+    unsigned opts;                                       // kLayerSigmoid | kLayerGateFirst
+};
+// Workgroups of a norm's backward, each of which leaves a row of partial sums
+int norm_bwd_blocks(long rows, int D, bool vec, int vec_len);
+template <typename T, typename R> hipError_t launch_add_norm_fwd(const AddNormArgs<T, R>& a, bool vec, hipStream_t st);
+template <typename T, typename R> hipError_t launch_add_norm_bwd(const AddNormArgs<T, R>& a, bool vec, float* dweight, float* dscale, hipStream_t st);
+template <typename T> hipError_t launch_gated_norm_fwd(const GatedNormArgs<T>& a, bool vec, hipStream_t st);
+template <typename T> hipError_t launch_gated_norm_bwd(const GatedNormArgs<T>& a, bool vec, float* dweight, hipStream_t st);
+
+// Selective scan.  The tokens of a sequence are taken in segments of Lseg (a multiple of the checkpoint distance); segment k of
+// sequence n has the slot first/Lseg + n + k (packed) or n * ceil(T/Lseg) + k, which nothing has to count: a few slots stay empty.
+template <typename T> struct SsmArgs {
+    const T* u; long ld_u; const T* delta; long ld_delta; const float* A;
+    const T* B; long ld_B; const T* C; long ld_C;
+    const float* skip; const T* z; long ld_z; const float* delta_bias; const float* h0;  // each of these or NULL
+    T* y; float* hT;                                     // hT: or NULL
+    float* saved;                                        // states at every checkpoint, or NULL
+    float* seg_state; float* seg_delta;                  // per slot: [D][S] and [D]; NULL: one segment per sequence
+    Seqs seqs; long M; int D, G, Lseg; long slots;
+    bool softplus;
+    // backward
+    const T* d_y; const float* d_hT;
+    T* du; T* ddelta; T* dz; float* dh0;
+    float* part_bc;                                      // [channel block][token][2 S]: gradients of C, then of B
+    float* part_p;                                       // [slot][D S + 2 D]: gradients of A, skip, delta_bias
+};
+constexpr int kSsmTile = 64;                             // channels per workgroup
+inline int ssm_checkpoint(int S) { return 256 / S; }     // tokens between checkpoints
+template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st);
+template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st);
+template <typename T> hipError_t launch_ssm_step(const SsmArgs<T>& a, float* h, int B, int S, hipStream_t st);
+
+}  // namespace kla

@@ -1,0 +1,38 @@
+// Sums over the rows of partial results: what a backward's workgroups leave for the gradients of parameters.
+#include "kla_layer.hpp"
+
+namespace kla {
+
+// 64 columns per workgroup, its 16 waves take every sixteenth row, joined in a fixed order.
+__global__ __launch_bounds__(1024) void column_sums_kernel(const float* __restrict__ partial, long P, ColumnSums s)
+{
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long col = (long)blockIdx.x * 64 + lane, C = s.n[0] + s.n[1] + s.n[2];
+    float x = 0.f;
+    if (col < C) {
+#pragma unroll 8
+        for (long r = wave; r < P; r += 16) x += partial[r * C + col];
+    }
+    red[wave][lane] = x;
+    __syncthreads();
+    if (wave == 0 && col < C) {
+        x = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) x += red[w][lane];
+        long at = col;
+        int o = 0;
+        while (o < 2 && at >= s.n[o]) at -= s.n[o++];
+        if (s.out[o]) s.out[o][at] = x;
+    }
+}
+hipError_t launch_column_sums(const float* partial, long P, const ColumnSums& s, hipStream_t st)
+{
+    const long C = s.n[0] + s.n[1] + s.n[2];
+    if (C == 0) return hipSuccess;
+    if ((C + 63) / 64 > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((C + 63) / 64)), dim3(1024), 0, st, partial, P, s);
+    return hipGetLastError();
+}
+
+}  // namespace kla

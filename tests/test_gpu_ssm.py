@@ -1,0 +1,250 @@
+"""Selective state space scan against its definition in 64 bits: forward, backward, single tokens, at the lengths, widths, groups, strides
+and values where it can go wrong."""
+import pytest
+import torch
+
+from layer_cases import SCAN, bits, close, columns, offsets, randn, to_gpu
+from oracle import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def kla():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2605_08587_amd as m
+    m.lib()
+    return m
+
+
+def _inputs(dtype, lead, n, D, G, S, opt, wide, seed):
+    g = torch.Generator().manual_seed(seed)
+    cols = columns(g, lead, [D, D, D, G * S, G * S], dtype, wide)
+    dev_cols = to_gpu(cols)
+    if not isinstance(cols, list):
+        whole, at = cols
+        cols = [whole[..., a:a + w] for a, w in at]
+    d, dev = {}, {}
+    for i, k in enumerate(("u", "delta", "z")):
+        d[k], dev[k] = cols[i], dev_cols[i]
+    for i, k in enumerate(("B", "C")):
+        d[k], dev[k] = cols[3 + i].unflatten(-1, (G, S)), dev_cols[3 + i].unflatten(-1, (G, S))
+    more = dict(A=-torch.arange(1, S + 1) * torch.exp(0.2 * randn(g, D, S)), skip=randn(g, D), delta_bias=randn(g, D) - 1, h0=randn(g, n, D, S))
+    for k, v in more.items():
+        d[k], dev[k] = v, v.cuda()
+    for k in ("skip", "z", "delta_bias", "h0"):
+        if k not in opt:
+            d[k] = dev[k] = None
+    return g, d, dev
+
+
+ALL = ("skip", "z", "delta_bias", "h0")
+CASES = [
+    # dtype, N, T, D, G, S, lens, what is given, softplus, wide
+    (torch.bfloat16, 1, 1, 64, 1, 16, None, ALL, True, False),
+    (torch.bfloat16, 2, 2, 16, 1, 8, None, ALL, True, False),
+    (torch.bfloat16, 2, 75, 200, 1, 16, None, ALL, True, True),
+    (torch.bfloat16, 1, 130, 132, 2, 16, None, ("z",), True, "odd"),
+    (torch.bfloat16, 3, 33, 70, 1, 32, None, ("skip", "delta_bias"), True, False),
+    (torch.bfloat16, 1, 21, 48, 3, 64, None, ALL, True, True),
+    (torch.bfloat16, 1, 0, 130, 1, 16, [0, 1, 16, 17, 0, 100, 2], ALL, True, "odd"),
+    (torch.bfloat16, 1, 0, 64, 2, 8, [31, 33, 64, 1, 0], ("z", "h0"), True, False),
+    (torch.float32, 1, 3, 5, 1, 16, None, ALL, True, False),
+    (torch.float32, 2, 100, 66, 2, 16, None, ALL, True, "odd"),
+    (torch.float32, 2, 40, 64, 1, 8, None, (), True, False),
+    (torch.float32, 1, 0, 96, 1, 32, [8, 7, 9, 50, 0], ("h0", "skip"), True, True),
+    (torch.float32, 1, 18, 32, 1, 64, None, ("delta_bias", "z"), True, False),
+    (torch.float32, 1, 50, 64, 1, 16, None, ("delta_bias",), "positive", False),
+    (torch.bfloat16, 1, 600, 64, 1, 16, None, ALL, True, False),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_against_definition(kla, case):
+    dtype, N, T, D, G, S, lens, opt, softplus, wide = CASES[case]
+    print("ssm", CASES[case], flush=True)
+    lead, n = ((1, sum(lens)), len(lens)) if lens else ((N, T), N)
+    g, d, dev = _inputs(dtype, lead, n, D, G, S, opt, wide, 200 + case)
+    if softplus == "positive":          # steps given as they are
+        softplus = False
+        d["delta"] = d["delta"].abs() + 2
+        d["delta_bias"] = d["delta_bias"].abs()
+        dev["delta"], dev["delta_bias"] = d["delta"].cuda(), d["delta_bias"].cuda()
+    cu = offsets(lens) if lens else None
+    dy, dh = randn(g, *lead, D, dtype=dtype), randn(g, n, D, S)
+    seqs = lo.sequences(N, T, cu)
+    flat = {k: v if v is None or k in ("A", "skip", "delta_bias", "h0") else v.flatten(0, 1) for k, v in d.items()}
+    f = lambda **k: lo.ssm(**k, softplus=softplus, seqs=seqs)  # noqa: E731
+    (y_ref, h_ref), g_ref = lo.gradients(f, flat, (dy.flatten(0, 1), dh))
+    packed = {} if cu is None else dict(cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
+    y, hT = kla.kla_ssm_fwd(**dev, softplus=softplus, **packed)
+    torch.cuda.synchronize()
+    close("y", y.flatten(0, 1), y_ref, SCAN)
+    close("hT", hT, h_ref, SCAN)
+    gr = kla.kla_ssm_bwd(**dev, d_y=dy.cuda(), d_hT=dh.cuda(), softplus=softplus, **packed)
+    torch.cuda.synchronize()
+    for k in g_ref:
+        close("d" + k, gr["d" + k].reshape(g_ref[k].shape), g_ref[k], SCAN)
+    for k in ("skip", "z", "delta_bias", "h0"):
+        assert (gr["d" + k] is None) == (d[k] is None)
+
+    # through autograd, with the checkpoints of the forward and without: the same bits
+    leaves = {k: None if v is None else v.detach().requires_grad_(True) for k, v in dev.items()}
+    wrt = [v for v in leaves.values() if v is not None]
+    got = []
+    for save in (True, False):
+        y2, h2 = kla.kla_ssm(**leaves, softplus=softplus, save=save, **packed)
+        assert torch.equal(bits(y2.detach()), bits(y)) and torch.equal(bits(h2.detach()), bits(hT))
+        got.append(torch.autograd.grad((y2, h2), wrt, (dy.cuda(), dh.cuda())))
+    for k, p, q in zip((k for k, v in leaves.items() if v is not None), *got):
+        assert torch.equal(bits(p), bits(gr["d" + k])) and torch.equal(bits(q), bits(gr["d" + k])), k
+    y2, _ = kla.kla_ssm(**leaves, softplus=softplus, **packed)
+    a = torch.autograd.grad(y2, wrt, dy.cuda())
+    _, g_ref = lo.gradients(lambda **k: f(**k)[0], flat, (dy.flatten(0, 1),))
+    for (k, _), p in zip(((k, v) for k, v in leaves.items() if v is not None), a):
+        close("autograd " + k, p.reshape(g_ref[k].shape), g_ref[k], SCAN)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("wide", [False, "odd"])
+def test_step_by_step_is_the_whole(kla, dtype, S, wide):
+    N, T, D, G = 3, 7, 90, 2
+    g, d, dev = _inputs(dtype, (N, T), N, D, G, S, ALL, wide, S)
+    print("ssm step", dtype, S, wide, flush=True)
+    y, hT = kla.kla_ssm_fwd(**dev)
+    h = dev["h0"].clone()
+    ys = []
+    for t in range(T):
+        x = {k: v[:, t] for k, v in dev.items() if k in ("u", "delta", "z", "B", "C")}
+        ys.append(kla.kla_ssm_step(**x, A=dev["A"], skip=dev["skip"], delta_bias=dev["delta_bias"], h=h))
+    torch.cuda.synchronize()
+    close("y", torch.stack(ys, 1), y, SCAN)
+    close("h", h, hT, SCAN)
+    # the state may come back in the place of the one that went in
+    again = dev["h0"].clone()
+    y2, h2 = kla.kla_ssm_fwd(**dict(dev, h0=again), hT=again)
+    assert h2 is again and torch.equal(bits(again), bits(hT)) and torch.equal(bits(y2), bits(y))
+
+
+def test_extreme_steps(kla):
+    """Steps from nothing to a hundred and gates of any size: what is forgotten is forgotten, and softplus keeps its digits where it is small."""
+    D, S, T = 64, 16, 40
+    g, d, dev = _inputs(torch.float32, (1, T), 1, D, 1, S, ("z", "h0"), False, 77)
+    d["delta"] = torch.linspace(-30, 100, T)[None, :, None].expand(1, T, D).contiguous()
+    d["z"] = 40 * d["z"]
+    dev.update(delta=d["delta"].cuda(), z=d["z"].cuda())
+    flat = {k: v if v is None or k in ("A", "h0") else v.flatten(0, 1) for k, v in d.items()}
+    dy = randn(g, 1, T, D)
+    (y_ref, h_ref), g_ref = lo.gradients(lambda **k: lo.ssm(**k, softplus=True, seqs=[(0, T)]), flat, (dy[0], None))
+    y, hT = kla.kla_ssm_fwd(**dev)
+    gr = kla.kla_ssm_bwd(**dev, d_y=dy.cuda())
+    # row by row: the rows differ by thirteen orders of magnitude
+    for t in range(T):
+        close("y %d" % t, y[0, t], y_ref[t], SCAN)
+        close("du %d" % t, gr["du"][0, t], g_ref["u"][t], SCAN)
+        close("ddelta %d" % t, gr["ddelta"][0, t], g_ref["delta"][t], 10 * SCAN)     # differences of terms ten times its size
+    close("hT", hT, h_ref, SCAN)
+
+
+def test_other_sequences_do_not_reach_in(kla):
+    lens, D = [17, 40, 3, 64], 80
+    cu = offsets(lens)
+    g, d, dev = _inputs(torch.bfloat16, (1, sum(lens)), 4, D, 1, 16, ("z", "skip"), False, 8)
+    dy = randn(g, 1, sum(lens), D, dtype=torch.bfloat16).cuda()
+    bad = {k: None if v is None else v.clone() for k, v in dev.items()}
+    for k in ("u", "delta", "z", "B", "C"):
+        bad[k][:, 17:57] = float("nan")
+        bad[k][:, 57:60] = float("inf")
+    out = []
+    for x in (dev, bad):
+        y, h = kla.kla_ssm_fwd(**x, cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
+        gr = kla.kla_ssm_bwd(**x, d_y=dy, cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
+        out.append((y, gr["du"], gr["ddelta"], gr["dz"], gr["dB"], gr["dC"], h))
+    torch.cuda.synchronize()
+    for p, q in zip(out[0][:-1], out[1]):
+        for a, b in ((0, 17), (60, 124)):
+            assert torch.equal(bits(p[:, a:b]), bits(q[:, a:b]))
+    assert torch.equal(bits(out[0][-1][[0, 3]]), bits(out[1][-1][[0, 3]]))
+
+
+def test_no_tokens(kla):
+    for N, T in ((0, 4), (2, 0)):
+        g, d, dev = _inputs(torch.bfloat16, (N, T), N, 40, 1, 16, ALL, False, 3)
+        y, hT = kla.kla_ssm_fwd(**dev)
+        assert y.shape == (N, T, 40) and torch.equal(bits(hT), bits(dev["h0"]))
+        dh = torch.randn(N, 40, 16, device="cuda")
+        gr = kla.kla_ssm_bwd(**dev, d_y=y, d_hT=dh)
+        assert not gr["dA"].any() and not gr["dskip"].any() and not gr["ddelta_bias"].any() and torch.equal(bits(gr["dh0"]), bits(dh))
+
+
+def _close_runs(name, p, q):
+    """Two orders of the same sums, each within the bar of the definition."""
+    close(name, p, q, 2 * SCAN + (2.0 ** -8 if p.dtype == torch.bfloat16 else 0))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_long_few_channels(kla, packed):
+    """Few channels and many tokens, and the same tokens in pieces with the states handed on: the forward's, the backward's."""
+    D, S, T = 128, 16, 6000
+    g, d, dev = _inputs(torch.float32, (1, T), 1, D, 1, S, ALL, False, 31)
+    dev["delta_bias"] -= 3                               # states that remember hundreds of tokens
+    dy = randn(g, 1, T, D).cuda()
+    lens = [1000, 5000]
+    if packed:
+        cu = offsets(lens)
+        dev["h0"] = torch.cat([dev["h0"], randn(g, 1, D, S).cuda()])
+        kw = dict(cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
+    else:
+        kw = {}
+    print("ssm long", packed, flush=True)
+    y, hT = kla.kla_ssm_fwd(**dev, **kw)
+    gr = kla.kla_ssm_bwd(**dev, d_y=dy, **kw)
+
+    def piece(lo_, hi, h0, dh):
+        x = {k: v[:, lo_:hi].contiguous() if k in ("u", "delta", "z", "B", "C") else v for k, v in dev.items()}
+        x["h0"] = h0
+        return kla.kla_ssm_fwd(**x)[1], lambda dh: kla.kla_ssm_bwd(**x, d_y=dy[:, lo_:hi].contiguous(), d_hT=dh), kla.kla_ssm_fwd(**x)[0]
+    edges = [0, 1000, 1640, 2600, 4111, 6000]
+    h, back, ys = dev["h0"][:1].contiguous(), [], []
+    for a, b in zip(edges, edges[1:]):
+        if packed and a == 1000:
+            h = dev["h0"][1:].contiguous()
+        h, f, yy = piece(a, b, h, None)
+        back.append((a, b, f))
+        ys.append(yy)
+    _close_runs("y", y, torch.cat(ys, 1))
+    _close_runs("hT", hT[-1:], h)
+    dh, dA = None, 0
+    for a, b, f in reversed(back):
+        gp = f(dh)
+        dh = gp["dh0"]
+        if packed and a == 1000:
+            _close_runs("dh0 of the second", gr["dh0"][1:], dh)
+            dh = None
+        dA = dA + gp["dA"]
+        for k in ("du", "ddelta", "dz", "dB", "dC"):
+            _close_runs(k, gr[k][:, a:b], gp[k])
+    _close_runs("dh0", gr["dh0"][:1], dh)
+    _close_runs("dA", gr["dA"], dA)
+
+
+def test_offsets_beyond_32_bits(kla):
+    """The last tokens of a batch of more than 2^31 elements: as those tokens alone from the state before them."""
+    D, S, T = 4096, 16, 2 ** 19 + 1003
+    print("ssm", T, D, flush=True)
+    u = torch.empty(1, T, D, dtype=torch.bfloat16, device="cuda").normal_()
+    B, C = (torch.empty(1, T, 1, S, dtype=torch.bfloat16, device="cuda").normal_() for _ in range(2))
+    A = -torch.arange(1.0, S + 1, device="cuda").repeat(D, 1)
+    cut = T - 100
+    y, hT = kla.kla_ssm_fwd(u, u, A, B, C, z=u)
+    part = [t[:, cut:].contiguous() for t in (u, B, C)]
+    _, mid = kla.kla_ssm_fwd(u[:, :cut], u[:, :cut], A, B[:, :cut], C[:, :cut], z=u[:, :cut])
+    tail, end = kla.kla_ssm_fwd(part[0], part[0], A, part[1], part[2], z=part[0], h0=mid)
+    _close_runs("y", y[:, cut:], tail)
+    _close_runs("hT", hT, end)
+    g = kla.kla_ssm_bwd(u, u, A, B, C, y, z=u)
+    t = kla.kla_ssm_bwd(part[0], part[0], A, part[1], part[2], y[:, cut:].contiguous(), z=part[0], h0=mid)
+    for k in ("du", "ddelta", "dz", "dB", "dC"):
+        _close_runs(k, g[k][:, cut:], t[k])
