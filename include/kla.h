@@ -386,7 +386,7 @@ int kla_conv_step(const void *x, long ld_x, const float *weight, const float *bi
  *   h0          [n_states, D, S] fp32                                   in   or NULL for zeros
  *   y           [N, T, D] dt                                            out
  *   hT          [n_states, D, S] fp32                                   out  or NULL; may alias h0
- *   saved       kla_ssm_saved_bytes(...): the states at every 256/S-th token, for the backward; or NULL
+ *   saved       kla_ssm_saved_bytes(...): the states at every 16th token (every 8th from S = 32 on), for the backward; or NULL
  * S in {8, 16, 32, 64}; D a multiple of G; at most 65535 sequences.  The queries need only know whether the batch is packed and
  * of how many sequences.
  */

@@ -162,7 +162,7 @@ template <typename T> struct SsmArgs {
     float* part_p;                                       // [slot][D S + 2 D]: gradients of A, skip, delta_bias
 };
 constexpr int kSsmTile = 64;                             // channels per workgroup
-inline int ssm_checkpoint(int S) { return 256 / S; }     // tokens between checkpoints
+constexpr int ssm_checkpoint(int S) { return S > 16 ? 8 : 16; }     // tokens between checkpoints
 template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st);
 template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st);
 template <typename T> hipError_t launch_ssm_step(const SsmArgs<T>& a, float* h, int B, int S, hipStream_t st);

@@ -9,138 +9,119 @@ namespace kla {
 
 constexpr int kTok = 16;                                 // tokens per tile
 
-// The rows of B and C of a tile in LDS as fp32, filled by all threads of the workgroup one tile ahead.
-template <typename T, int S> struct TileBC {
-    static constexpr int N = kTok * S / 256 > 0 ? kTok * S / 256 : 1;    // elements per thread, of each
-    float b[N], c[N];
-    __device__ __forceinline__ void load(const SsmArgs<T>& a, int g, long t, long t1, bool with_c)
+// What a lane takes of a tile: tokens 8 i + o of its channel, raw until they are used.  Nothing is read beyond the segment.
+template <typename T, bool HASZ> struct TileTok {
+    T u[2], raw[2], z[2];
+    __device__ __forceinline__ void load(const SsmArgs<T>& a, int c, int o, long t, long t1)
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int e = threadIdx.x + 256 * i, tok = e / S, n = e % S;
-            b[i] = c[i] = 0.f;
-            if (tok < kTok && t + tok < t1) {
-                b[i] = to_float(a.B[(t + tok) * a.ld_B + g * S + n]);
-                if (with_c) c[i] = to_float(a.C[(t + tok) * a.ld_C + g * S + n]);
-            }
-        }
-    }
-    __device__ __forceinline__ void store(float* lds_b, float* lds_c) const
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            if (e < kTok * S) { lds_b[e] = b[i]; lds_c[e] = c[i]; }
-        }
-    }
-};
-
-// What a lane takes of a tile: token 4 i + q of its channel.  Nothing is read beyond the segment.
-template <typename T> struct TileTok {
-    float u[4], raw[4], z[4];
-    __device__ __forceinline__ void load(const SsmArgs<T>& a, int c, int q, long t, long t1, bool with_z)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const long at = min(t + 4 * i + q, t1 - 1);
-            u[i] = to_float(a.u[at * a.ld_u + c]);
-            raw[i] = to_float(a.delta[at * a.ld_delta + c]);
-            z[i] = with_z ? to_float(a.z[at * a.ld_z + c]) : 0.f;
+        for (int i = 0; i < 2; ++i) {
+            const long at = min(t + 8 * i + o, t1 - 1);
+            u[i] = a.u[at * a.ld_u + c];
+            raw[i] = a.delta[at * a.ld_delta + c];
+            if constexpr (HASZ) z[i] = a.z[at * a.ld_z + c];
         }
     }
 };
 
 enum SsmMode { kSsmOutputs, kSsmStates, kSsmMaps };      // y (and checkpoints); checkpoints alone; the maps of the segments
 
-// One workgroup: 64 channels of one segment, tiles of 16 tokens one after the other.
-template <typename T, int S, SsmMode MODE>
-__global__ __launch_bounds__(256) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
+// One workgroup: 64 channels of one segment, tiles of 16 tokens one after the other, two tiles on their way.
+template <typename T, int S, SsmMode MODE, bool HASZ>
+__global__ __launch_bounds__(kSsmThreads) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
 {
-    constexpr int K = S / 4, CK = 256 / S;
-    __shared__ float lds[2][2][kTok * S];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 3;
+    constexpr int K = S / 8, CK = ssm_checkpoint(S);
+    __shared__ __align__(16) float lds[2][2 * kTok * S];
+    const int o = threadIdx.x & 7;
     const int block = blockIdx.x % blocks_c;
     const long slot = blockIdx.x / blocks_c;
     Segment g;
     if (!segment_of(a, slot, &g)) return;
     if (MODE == kSsmMaps && g.last) return;              // nothing follows it
-    const Channels ch = channels_of(block, a.D, a.G, wave, lane);
+    const Channels ch = channels_of(block, a.D, a.G);
     const int c = ch.c;
+    const long mine = ((long)c * S) + o * K;             // this lane's states of [D][S]
 
     float A2[K], h[K];
+    load_states<K>(A2, a.A + mine);
 #pragma unroll
-    for (int k = 0; k < K; ++k) A2[k] = kLog2e * a.A[(long)c * S + q * K + k];
+    for (int k = 0; k < K; ++k) { A2[k] *= kLog2e; h[k] = 0.f; }
     const float skip = a.skip ? a.skip[c] : 0.f, bias = a.delta_bias ? a.delta_bias[c] : 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        h[k] = 0.f;
-        if (MODE != kSsmMaps) {
-            if (a.seg_state) h[k] = a.seg_state[(slot * a.D + c) * S + q * K + k];
-            else if (a.h0) h[k] = a.h0[((long)g.seq.n * a.D + c) * S + q * K + k];
-        }
+    if (MODE != kSsmMaps) {
+        if (a.seg_state) load_states<K>(h, a.seg_state + slot * a.D * S + mine);
+        else if (a.h0) load_states<K>(h, a.h0 + (long)g.seq.n * a.D * S + mine);
     }
     float sum_delta = 0.f;
 
-    TileBC<T, S> bc;
-    TileTok<T> tk;
-    if (g.t0 < g.t1) {
-        bc.load(a, ch.g, g.t0, g.t1, MODE == kSsmOutputs);
-        tk.load(a, c, q, g.t0, g.t1, MODE == kSsmOutputs && a.z);
-    }
-    int buf = 0;
-    for (long t = g.t0; t < g.t1; t += kTok, buf ^= 1) {
-        bc.store(lds[buf][0], lds[buf][1]);
+    TileBC<T, S, kTok> bc[2];
+    TileTok<T, HASZ> tk[2];
+    auto tile = [&](auto which, long t) {
+        constexpr int w = which.value;
+        bc[w].store(lds[w]);
+        const TileTok<T, HASZ> now = tk[w];
         __syncthreads();
-        const TileTok<T> now = tk;
-        if (t + kTok < g.t1) {
-            bc.load(a, ch.g, t + kTok, g.t1, MODE == kSsmOutputs);
-            tk.load(a, c, q, t + kTok, g.t1, MODE == kSsmOutputs && a.z);
+        if (t + 2 * kTok < g.t1) {
+            bc[w].load(a, ch.g, t + 2 * kTok, g.t1);
+            tk[w].load(a, c, o, t + 2 * kTok, g.t1);
         }
-        const float* lb = lds[buf][0] + q * K;
-        const float* lc = lds[buf][1] + q * K;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const long mine = t + 4 * i + q;
-            if (MODE != kSsmMaps && (4 * i) % CK == 0 && (CK <= kTok || (t - g.t0) % CK == 0) && a.saved && t + 4 * i < g.t1 && ch.mine) {
-                float* at = a.saved + (checkpoint_at(a, g.seq, t + 4 * i, CK) * a.D + c) * S + q * K;
-#pragma unroll
-                for (int k = 0; k < K; ++k) at[k] = h[k];
-            }
+        const float* row = lds[w] + o * 2 * K;
+        float y[2];
+        static_for<2>([&](auto i) {
+            if (MODE != kSsmMaps && (8 * i.value) % CK == 0 && a.saved && t + 8 * i.value < g.t1 && ch.mine)
+                store_states<K>(a.saved + checkpoint_at(a, g.seq, t + 8 * i.value, CK) * a.D * S + mine, h);
             // a token beyond the segment decays nothing and adds nothing
-            const bool in = mine < g.t1;
-            const float raw = now.raw[i] + bias;
-            const float delta = in ? (a.softplus ? softplus(raw) : raw) : 0.f;
-            const float du = in ? delta * now.u[i] : 0.f;
-            float acc[4];
-            static_for<4>([&](auto j) {
-                const float dj = quad_bcast<j.value>(delta), uj = quad_bcast<j.value>(du);
-                const float* b = lb + (4 * i + j.value) * S;
-                const float* cc = lc + (4 * i + j.value) * S;
+            const bool in = t + 8 * i.value + o < g.t1;
+            const float u = to_float(now.u[i.value]), raw = to_float(now.raw[i.value]) + bias, soft = softplus(raw);
+            const float delta = in ? (a.softplus ? soft : raw) : 0.f;
+            const Oct ds = oct_of(delta), us = oct_of(in ? delta * u : 0.f);
+            float acc[8];
+            static_for<8>([&](auto j) {
+                const float dj = oct_bcast<j.value>(ds), uj = oct_bcast<j.value>(us);
+                const StateBC<K> m = lds_bc<K>(row + (8 * i.value + j.value) * 2 * S);
                 float s = 0.f;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    h[k] = fmaf(exp2_hw(dj * A2[k]), h[k], uj * b[k]);
-                    if (MODE == kSsmOutputs) s = fmaf(cc[k], h[k], s);
+                    h[k] = fmaf(exp2_hw(dj * A2[k]), h[k], uj * m.b[k]);
+                    if (MODE == kSsmOutputs) s = k ? fmaf(m.c[k], h[k], s) : m.c[k] * h[k];
                 }
                 acc[j.value] = s;
             });
             if (MODE == kSsmMaps) sum_delta += delta;
             if (MODE == kSsmOutputs) {
-                float y = fmaf(skip, now.u[i], quad_sum_own(acc, q));
-                if (a.z) y *= now.z[i] * sigmoid(now.z[i]);
-                if (in && ch.mine) a.y[mine * a.D + c] = from_float<T>(y);
+                y[i.value] = fmaf(skip, u, oct_sum_own(acc, o));
+                if constexpr (HASZ) {
+                    const float z = to_float(now.z[i.value]);
+                    y[i.value] *= z * sigmoid(z);
+                }
+            }
+        });
+        if (MODE == kSsmOutputs && ch.mine) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const long at = t + 8 * i + o;
+                if (at < g.t1) a.y[at * a.D + c] = from_float<T>(y[i]);
             }
         }
+    };
+    if (g.t0 < g.t1) {
+        bc[0].load(a, ch.g, g.t0, g.t1);
+        tk[0].load(a, c, o, g.t0, g.t1);
+        if (g.t0 + kTok < g.t1) {
+            bc[1].load(a, ch.g, g.t0 + kTok, g.t1);
+            tk[1].load(a, c, o, g.t0 + kTok, g.t1);
+        }
     }
+    for (long t = g.t0; t < g.t1; t += 2 * kTok) {
+        tile(IntC<0>(), t);
+        if (t + kTok < g.t1) tile(IntC<1>(), t + kTok);
+    }
+    if (MODE == kSsmMaps) sum_delta = oct_sum(sum_delta);
     if (!ch.mine) return;
     if (MODE == kSsmMaps) {
-        sum_delta = quad_sum(sum_delta);
-#pragma unroll
-        for (int k = 0; k < K; ++k) a.seg_state[(slot * a.D + c) * S + q * K + k] = h[k];
-        if (q == 0) a.seg_delta[slot * a.D + c] = sum_delta;
+        store_states<K>(a.seg_state + slot * a.D * S + mine, h);
+        if (o == 0) a.seg_delta[slot * a.D + c] = sum_delta;
     } else if (a.hT && g.last) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) a.hT[((long)g.seq.n * a.D + c) * S + q * K + k] = h[k];
+        store_states<K>(a.hT + (long)g.seq.n * a.D * S + mine, h);
     }
 }
 
@@ -151,7 +132,7 @@ __global__ __launch_bounds__(256) void ssm_join_kernel(SsmArgs<T> a, int S)
     const long e = (long)blockIdx.x * 256 + threadIdx.x, DS = (long)a.D * S;
     if (e >= DS) return;
     const Place p = sequence(a.seqs, blockIdx.y);
-    const long base = a.seqs.cu ? p.first / a.Lseg + p.n : (long)p.n * max(1, (a.seqs.T + a.Lseg - 1) / a.Lseg);
+    const long base = first_slot(a, p);
     const long n = (p.end - p.first + a.Lseg - 1) / a.Lseg;
     const float A2 = kLog2e * a.A[e];
     const int c = (int)(e / S);
@@ -188,7 +169,8 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmArgs<T> a, float* __re
         s = fmaf(to_float(a.C[b * a.ld_C + g * S + n]), h[k], s);
         st[k] = h[k];
     }
-    s = quad_sum(s);
+    s += quad_xor1(s);
+    s += quad_xor2(s);
     if (q == 0) {
         s = fmaf(a.skip ? a.skip[c] : 0.f, u, s);
         if (a.z) { const float z = to_float(a.z[b * a.ld_z + c]); s *= z * sigmoid(z); }
@@ -202,15 +184,16 @@ template <typename T, int S> static hipError_t ssm_fwd(const SsmArgs<T>& a, bool
     const long blocks = blocks_c * a.slots;
     if (blocks == 0) return hipSuccess;
     if (blocks > 0x7fffffffL || a.seqs.n_seq > 65535) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 grid((unsigned)blocks), block(kSsmThreads);
     if (a.seg_state) {
-        hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmMaps>), grid, block, 0, st, a, blocks_c);
+        hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmMaps, false>), grid, block, 0, st, a, blocks_c);
         if (const hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL((ssm_join_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), block, 0, st, a, S);
+        hipLaunchKernelGGL((ssm_join_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    if (outputs) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs>), grid, block, 0, st, a, blocks_c);
-    else         hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmStates>), grid, block, 0, st, a, blocks_c);
+    if (!outputs) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmStates, false>), grid, block, 0, st, a, blocks_c);
+    else if (a.z) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, true>), grid, block, 0, st, a, blocks_c);
+    else          hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, false>), grid, block, 0, st, a, blocks_c);
     return hipGetLastError();
 }
 template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st)

@@ -5,14 +5,14 @@
 //   d_A[n] = sum_t e_t delta_t,   d_delta = sum_n e A + u sum_n g B,   d_raw = d_delta sigmoid(raw + bias),   d_bias = sum_t d_raw
 //   d_u = delta sum_n g B + skip d_c,   d_skip = sum_t d_c u,   d_z = d_y c (z sigmoid(z))'
 //   d_B_t[n] = sum over the group's channels of g delta u,   d_C_t[n] = the same of d_c h,   d_h0 = a_1 g_1
-// The states come from checkpoints 256/S tokens apart: from each the states and decays of its tokens are formed again and stay in
-// registers (64 of each per lane) for the way back.  Sums over channels go through the wave by lane swaps that halve what is left
+// The states come from checkpoints 16 tokens apart (8 from S = 32 on): from each the states and decays of its tokens are formed again and
+// stay in registers for the way back.  Sums over channels go through the wave by lane swaps that halve what is left
 // at every step, then over the four waves through LDS, then over the workgroups in a kernel of their own: no atomics.
 #include "kla_ssm_ops.hpp"
 
 namespace kla {
 
-// rows r = 0..3 of a wave hold, after two swaps, value 4 j + kRowValue[r] of sixteen
+// which of four values row r of the wave holds after two swaps
 __device__ __forceinline__ int row_value(int r) { return ((r & 1) << 1) | (r >> 1); }
 
 __device__ __forceinline__ float swap32_sum(float x, float y)
@@ -29,187 +29,196 @@ __device__ __forceinline__ float swap16_sum(float x, float y)
 }
 
 // MAPS: what a segment adds to the gradient that enters the one before it, from zeros (with the segment's sum of delta).
-template <typename T, int S, bool MAPS>
-__global__ __launch_bounds__(256) void ssm_bwd_kernel(SsmArgs<T> a, int blocks_c)
+template <typename T, int S, bool MAPS, bool HASZ>
+__global__ __launch_bounds__(kSsmThreads) void ssm_bwd_kernel(SsmArgs<T> a, int blocks_c)
 {
-    constexpr int K = S / 4, CK = 256 / S, NQ = CK / 4;  // tokens per checkpoint, in groups of four
-    constexpr int NE = CK * S / 256;                     // elements of a tile of B per thread
-    static_assert(NE == 1, "a tile of B or C has one element per thread");
-    __shared__ float lds[2][2][CK * S];
-    __shared__ float red[MAPS ? 1 : 4][MAPS ? 1 : CK][2 * S];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 3;
+    constexpr int K = S / 8, CK = ssm_checkpoint(S), NG = CK / 8;    // tokens per checkpoint and tile, in groups of eight
+    constexpr int WAVES = kSsmThreads / 64;
+    __shared__ __align__(16) float lds[2][2 * CK * S];
+    __shared__ float red[MAPS ? 1 : WAVES][MAPS ? 1 : CK][2 * S];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, o = lane & 7;
     const int block = blockIdx.x % blocks_c;
     const long slot = blockIdx.x / blocks_c;
     Segment g;
     if (!segment_of(a, slot, &g)) return;
     if (MAPS && g.t0 == g.seq.first) return;             // nothing stands before it
-    const Channels ch = channels_of(block, a.D, a.G, wave, lane);
+    const Channels ch = channels_of(block, a.D, a.G);
     const int c = ch.c;
+    const long mine = (long)c * S + o * K;
 
     float A2[K], dA[K], ag[K];                           // ag: a_{t+1} g_{t+1}
+    load_states<K>(A2, a.A + mine);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        A2[k] = kLog2e * a.A[(long)c * S + q * K + k];
-        dA[k] = ag[k] = 0.f;
-        if (!MAPS) {
-            if (a.seg_state) ag[k] = a.seg_state[(slot * a.D + c) * S + q * K + k];
-            else if (a.d_hT) ag[k] = a.d_hT[((long)g.seq.n * a.D + c) * S + q * K + k];
-        }
+    for (int k = 0; k < K; ++k) { A2[k] *= kLog2e; dA[k] = ag[k] = 0.f; }
+    if (!MAPS) {
+        if (a.seg_state) load_states<K>(ag, a.seg_state + slot * a.D * S + mine);
+        else if (a.d_hT) load_states<K>(ag, a.d_hT + (long)g.seq.n * a.D * S + mine);
     }
     const float skip = a.skip ? a.skip[c] : 0.f, bias = a.delta_bias ? a.delta_bias[c] : 0.f;
     float d_skip = 0.f, d_bias = 0.f, sum_delta = 0.f;
 
-    // this thread's element of the tile of B, C, and this lane's tokens 4 i + q
-    float in_b, in_c, in_u[NQ], in_raw[NQ], in_z[NQ], in_dy[NQ];
-    const int e_tok = threadIdx.x / S, e_n = threadIdx.x % S;
+    TileBC<T, S, CK> bc;
+    struct { T u[NG], raw[NG], z[NG], dy[NG]; float h[K]; } in;
     auto load = [&](long t) {
-        const bool in = t + e_tok < g.t1;
-        in_b = in ? to_float(a.B[(t + e_tok) * a.ld_B + ch.g * S + e_n]) : 0.f;
-        in_c = in ? to_float(a.C[(t + e_tok) * a.ld_C + ch.g * S + e_n]) : 0.f;
+        bc.load(a, ch.g, t, g.t1);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const long at = min(t + 4 * i + q, g.t1 - 1);
-            in_u[i] = to_float(a.u[at * a.ld_u + c]);
-            in_raw[i] = to_float(a.delta[at * a.ld_delta + c]);
-            in_z[i] = a.z ? to_float(a.z[at * a.ld_z + c]) : 0.f;
-            in_dy[i] = to_float(a.d_y[at * a.D + c]);
+        for (int i = 0; i < NG; ++i) {
+            const long at = min(t + 8 * i + o, g.t1 - 1);
+            in.u[i] = a.u[at * a.ld_u + c];
+            in.raw[i] = a.delta[at * a.ld_delta + c];
+            if constexpr (HASZ) in.z[i] = a.z[at * a.ld_z + c];
+            in.dy[i] = a.d_y[at * a.D + c];
         }
+        if constexpr (!MAPS) load_states<K>(in.h, a.saved + checkpoint_at(a, g.seq, t, CK) * a.D * S + mine);
     };
     const long tiles = (g.t1 - g.t0 + CK - 1) / CK;
     if (tiles > 0) load(g.t0 + (tiles - 1) * CK);
     int buf = 0;
     for (long tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
         const long t = g.t0 + tile * CK;
-        lds[buf][0][threadIdx.x] = in_b;
-        lds[buf][1][threadIdx.x] = in_c;
-        float u[NQ], raw[NQ], z[NQ], dy[NQ], delta[NQ], du[NQ], dc[NQ], core[NQ];
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) { u[i] = in_u[i]; raw[i] = in_raw[i] + bias; z[i] = in_z[i]; dy[i] = in_dy[i]; }
+        bc.store(lds[buf]);
+        const auto now = in;
         __syncthreads();
         if (tile > 0) load(t - CK);
         // a token beyond the segment decays nothing, adds nothing and has no gradient; nor has a lane without a channel of its own
+        float u[NG], raw[NG], dy[NG], delta[NG], dc[NG], core[NG];
+        Oct ds[NG], us[NG], cs[NG];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const bool in = t + 4 * i + q < g.t1;
-            delta[i] = in ? (a.softplus ? softplus(raw[i]) : raw[i]) : 0.f;
-            du[i] = in && ch.mine ? delta[i] * u[i] : 0.f;
-            dc[i] = in && ch.mine ? (a.z ? dy[i] * (z[i] * sigmoid(z[i])) : dy[i]) : 0.f;
+        for (int i = 0; i < NG; ++i) {
+            const bool live = t + 8 * i + o < g.t1, own = live && ch.mine;
+            u[i] = to_float(now.u[i]);
+            raw[i] = to_float(now.raw[i]) + bias;
+            dy[i] = to_float(now.dy[i]);
+            const float soft = softplus(raw[i]);
+            delta[i] = live ? (a.softplus ? soft : raw[i]) : 0.f;
+            float gate = 1.f;
+            if constexpr (HASZ) { const float z = to_float(now.z[i]); gate = z * sigmoid(z); }
+            dc[i] = own ? dy[i] * gate : 0.f;
+            ds[i] = oct_of(delta[i]);
+            us[i] = oct_of(own ? delta[i] * u[i] : 0.f);
+            cs[i] = oct_of(dc[i]);
             if (MAPS) sum_delta += delta[i];
         }
-        const float* lb = lds[buf][0] + q * K;
-        const float* lc = lds[buf][1] + q * K;
+        const float* row = lds[buf] + o * 2 * K;
         if constexpr (MAPS) {
-            static_for<NQ>([&](auto ii) {
-                constexpr int i = NQ - 1 - ii.value;
-                static_for<4>([&](auto jj) {
-                    constexpr int j = 3 - jj.value;
-                    const float dj = quad_bcast<j>(delta[i]), cj = quad_bcast<j>(dc[i]);
+            static_for<CK>([&](auto nn) {
+                constexpr int n = CK - 1 - nn.value, i = n / 8, j = n % 8;
+                const float dj = oct_bcast<j>(ds[i]), cj = oct_bcast<j>(cs[i]);
+                const StateBC<K> m = lds_bc<K>(row + n * 2 * S);
 #pragma unroll
-                    for (int k = 0; k < K; ++k) ag[k] = exp2_hw(dj * A2[k]) * fmaf(cj, lc[(4 * i + j) * S + k], ag[k]);
-                });
+                for (int k = 0; k < K; ++k) ag[k] = exp2_hw(dj * A2[k]) * fmaf(cj, m.c[k], ag[k]);
             });
         } else {
-            float h[CK + 1][K], dec[CK][K];
-            const float* from = a.saved + (checkpoint_at(a, g.seq, t, CK) * a.D + c) * S + q * K;
+            // (at S = 64 the decays would not fit the registers with the states: there they are formed a second time)
+            constexpr bool KEEP = K < 8;
+            float h[CK + 1][K], dec[KEEP ? CK : 1][K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) h[0][k] = from[k];
-            static_for<NQ>([&](auto i) {
-                float acc[4];
-                static_for<4>([&](auto j) {
-                    constexpr int n = 4 * i.value + j.value;
-                    const float dj = quad_bcast<j.value>(delta[i.value]), uj = quad_bcast<j.value>(du[i.value]);
+            for (int k = 0; k < K; ++k) h[0][k] = now.h[k];
+            static_for<NG>([&](auto i) {
+                float acc[8];
+                static_for<8>([&](auto j) {
+                    constexpr int n = 8 * i.value + j.value;
+                    const float dj = oct_bcast<j.value>(ds[i.value]), uj = oct_bcast<j.value>(us[i.value]);
+                    const StateBC<K> m = lds_bc<K>(row + n * 2 * S);
                     float s = 0.f;
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
-                        dec[n][k] = exp2_hw(dj * A2[k]);
-                        h[n + 1][k] = fmaf(dec[n][k], h[n][k], uj * lb[n * S + k]);
-                        s = fmaf(lc[n * S + k], h[n + 1][k], s);
+                        const float d = exp2_hw(dj * A2[k]);
+                        if constexpr (KEEP) dec[n][k] = d;
+                        h[n + 1][k] = fmaf(d, h[n][k], uj * m.b[k]);
+                        if constexpr (HASZ) s = k ? fmaf(m.c[k], h[n + 1][k], s) : m.c[k] * h[n + 1][k];
                     }
                     acc[j.value] = s;
                 });
-                if (a.z) core[i.value] = fmaf(skip, u[i.value], quad_sum_own(acc, q));
+                if constexpr (HASZ) core[i.value] = fmaf(skip, u[i.value], oct_sum_own(acc, o));
             });
-            static_for<NQ>([&](auto ii) {
-                constexpr int i = NQ - 1 - ii.value;
-                float via_a[4], via_b[4], own[K / 2];
-                static_for<4>([&](auto jj) {
-                    constexpr int j = 3 - jj.value, n = 4 * i + j;
-                    const float dj = quad_bcast<j>(delta[i]), uj = quad_bcast<j>(du[i]), cj = quad_bcast<j>(dc[i]);
+            static_for<NG>([&](auto ii) {
+                constexpr int i = NG - 1 - ii.value;
+                float via_a[8], via_b[8], pair[K < 2 ? 1 : K / 2];
+                static_for<8>([&](auto jj) {
+                    constexpr int j = 7 - jj.value, n = 8 * i + j;
+                    const float dj = oct_bcast<j>(ds[i]), uj = oct_bcast<j>(us[i]), cj = oct_bcast<j>(cs[i]);
+                    const StateBC<K> m = lds_bc<K>(row + n * 2 * S);
                     float val[2 * K], sa = 0.f, sb = 0.f;
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
-                        const float gk = fmaf(cj, lc[n * S + k], ag[k]);
-                        const float e = gk * (dec[n][k] * h[n][k]);
+                        const float gk = fmaf(cj, m.c[k], ag[k]);
+                        const float d = KEEP ? dec[KEEP ? n : 0][k] : exp2_hw(dj * A2[k]);
+                        const float e = gk * (d * h[n][k]);
                         val[k] = cj * h[n + 1][k];
                         val[K + k] = uj * gk;
-                        sb = fmaf(gk, lb[n * S + k], sb);
+                        sb = fmaf(gk, m.b[k], sb);
                         sa = fmaf(e, A2[k], sa);
                         dA[k] = fmaf(e, dj, dA[k]);
-                        ag[k] = dec[n][k] * gk;
+                        ag[k] = d * gk;
                     }
                     via_a[j] = sa;
                     via_b[j] = sb;
-                    // over the wave's 16 channels: lanes 4 c + q of a row keep the sums over all c, the lanes of c % 4 = j those of token j
+                    // Over the wave's 8 channels: two swaps that leave row r of 16 lanes with value 4 v + row_value(r), then over the row's two
+                    // octets; token j even stays in the first of them, odd in the second.
 #pragma unroll
-                    for (int v = 0; v < K / 2; ++v) {
-                        const float x = swap32_sum(val[4 * v], val[4 * v + 1]), y = swap32_sum(val[4 * v + 2], val[4 * v + 3]);
+                    for (int v = 0; v < (K < 2 ? 1 : K / 2); ++v) {
+                        float x, y;
+                        if constexpr (K == 1) x = y = swap32_sum(val[0], val[1]);
+                        else { x = swap32_sum(val[4 * v], val[4 * v + 1]); y = swap32_sum(val[4 * v + 2], val[4 * v + 3]); }
                         float s = swap16_sum(x, y);
                         s += dpp_mov<0x128>(s);          // row_ror:8
-                        s += dpp_mov<0x124>(s);          // row_ror:4
-                        own[v] = ((lane >> 2) & 3) == j ? s : (jj.value == 0 ? 0.f : own[v]);
+                        pair[v] = (j & 1) || (lane & 8) == 0 ? s : pair[v];
+                        if constexpr ((j & 1) == 0) {
+                            const int tok = n + ((lane >> 3) & 1);
+                            if constexpr (K == 1) {
+                                red[wave][tok][(lane >> 5) * S + o] = pair[v];       // (both rows of a half hold the same)
+                            } else {
+                                const int at = 4 * v + row_value(lane >> 4);         // < K: of C, else of B
+                                red[wave][tok][(at < K ? 0 : S) + o * K + (at < K ? at : at - K)] = pair[v];
+                            }
+                        }
                     }
                 });
-#pragma unroll
-                for (int v = 0; v < K / 2; ++v) {
-                    const int val = 4 * v + row_value(lane >> 4), kk = val < K ? val : val - K;     // < K: of C, else of B
-                    red[wave][4 * i + ((lane >> 2) & 3)][(val < K ? 0 : S) + q * K + kk] = own[v];
-                }
-                const float sa = quad_sum_own(via_a, q) * kLn2, sb = quad_sum_own(via_b, q);
-                const bool in = t + 4 * i + q < g.t1;
+                const float sa = oct_sum_own(via_a, o) * kLn2, sb = oct_sum_own(via_b, o);
+                const bool live = t + 8 * i + o < g.t1;
                 float d_raw = fmaf(u[i], sb, sa);
-                if (a.softplus) d_raw *= sigmoid(raw[i]);
-                if (in) {
+                d_raw *= a.softplus ? sigmoid(raw[i]) : 1.f;
+                if (live) {
                     d_bias += d_raw;
                     d_skip = fmaf(dc[i], u[i], d_skip);
                     if (ch.mine) {
-                        const long at = (t + 4 * i + q) * a.D + c;
+                        const long at = (t + 8 * i + o) * a.D + c;
                         a.du[at] = from_float<T>(fmaf(delta[i], sb, skip * dc[i]));
                         a.ddelta[at] = from_float<T>(d_raw);
-                        if (a.z) {
-                            const float s = sigmoid(z[i]);
-                            a.dz[at] = from_float<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f)));
+                        if constexpr (HASZ) {
+                            const float z = to_float(now.z[i]), s = sigmoid(z);
+                            a.dz[at] = from_float<T>(dy[i] * core[i] * (s * fmaf(z, 1.f - s, 1.f)));
                         }
                     }
                 }
             });
             __syncthreads();
-            // the four waves' channels together: [token][2 S], C first
+            // the waves' channels together: [token][2 S], C first
             float* out = a.part_bc + ((long)block * a.M + t) * (2 * S);
             const int n_out = (int)min((long)CK, g.t1 - t) * 2 * S;
-            for (int e = threadIdx.x; e < n_out; e += 256) {
+            for (int e = threadIdx.x; e < n_out; e += kSsmThreads) {
                 const float* r = &red[0][0][0] + e;
-                out[e] = (r[0] + r[CK * 2 * S]) + (r[2 * CK * 2 * S] + r[3 * CK * 2 * S]);
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) s += r[w * CK * 2 * S];
+                out[e] = s;
             }
             // (red is written again behind the next tile's barrier)
         }
     }
+    sum_delta = oct_sum(sum_delta);
+    d_skip = oct_sum(d_skip);
+    d_bias = oct_sum(d_bias);
     if (!ch.mine) return;
     if constexpr (MAPS) {
-        sum_delta = quad_sum(sum_delta);
-#pragma unroll
-        for (int k = 0; k < K; ++k) a.seg_state[(slot * a.D + c) * S + q * K + k] = ag[k];
-        if (q == 0) a.seg_delta[slot * a.D + c] = sum_delta;
+        store_states<K>(a.seg_state + slot * a.D * S + mine, ag);
+        if (o == 0) a.seg_delta[slot * a.D + c] = sum_delta;
     } else {
-        if (a.dh0 && g.t0 == g.seq.first) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) a.dh0[((long)g.seq.n * a.D + c) * S + q * K + k] = ag[k];
-        }
+        if (a.dh0 && g.t0 == g.seq.first) store_states<K>(a.dh0 + (long)g.seq.n * a.D * S + mine, ag);
         float* p = a.part_p + slot * ((long)a.D * (S + 2));
-#pragma unroll
-        for (int k = 0; k < K; ++k) p[(long)c * S + q * K + k] = dA[k];
-        d_skip = quad_sum(d_skip);
-        d_bias = quad_sum(d_bias);
-        if (q == 0) {
+        store_states<K>(p + mine, dA);
+        if (o == 0) {
             p[(long)a.D * S + c] = d_skip;
             p[(long)a.D * (S + 1) + c] = d_bias;
         }
@@ -223,7 +232,7 @@ __global__ __launch_bounds__(256) void ssm_join_bwd_kernel(SsmArgs<T> a, int S)
     const long e = (long)blockIdx.x * 256 + threadIdx.x, DS = (long)a.D * S;
     if (e >= DS) return;
     const Place p = sequence(a.seqs, blockIdx.y);
-    const long base = a.seqs.cu ? p.first / a.Lseg + p.n : (long)p.n * max(1, (a.seqs.T + a.Lseg - 1) / a.Lseg);
+    const long base = first_slot(a, p);
     const long n = (p.end - p.first + a.Lseg - 1) / a.Lseg;
     const float A2 = kLog2e * a.A[e];
     const int c = (int)(e / S);
@@ -267,18 +276,20 @@ template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, floa
     const long blocks = blocks_c * a.slots, row = (long)a.D * (S + 2);
     if (blocks > 0x7fffffffL || a.seqs.n_seq > 65535 || a.G > 65535 || (a.M * 2 * S + 255) / 256 > 0x7fffffffL) return hipErrorInvalidConfiguration;
     if (blocks > 0) {
-        const dim3 grid((unsigned)blocks), block(256);
+        const dim3 grid((unsigned)blocks), block(kSsmThreads);
         if (a.seg_state) {
-            hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true>), grid, block, 0, st, a, blocks_c);
+            if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, true>), grid, block, 0, st, a, blocks_c);
+            else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, false>), grid, block, 0, st, a, blocks_c);
             if (const hipError_t e = hipGetLastError()) return e;
-            hipLaunchKernelGGL((ssm_join_bwd_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), block, 0, st, a, S);
+            hipLaunchKernelGGL((ssm_join_bwd_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
             if (const hipError_t e = hipGetLastError()) return e;
         }
         if (a.seqs.cu) {
-            hipLaunchKernelGGL((ssm_clear_kernel<T>), dim3((unsigned)a.slots), block, 0, st, a, row);
+            hipLaunchKernelGGL((ssm_clear_kernel<T>), dim3((unsigned)a.slots), dim3(256), 0, st, a, row);
             if (const hipError_t e = hipGetLastError()) return e;
         }
-        hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false>), grid, block, 0, st, a, blocks_c);
+        if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, true>), grid, block, 0, st, a, blocks_c);
+        else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, false>), grid, block, 0, st, a, blocks_c);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     if (a.M > 0) {

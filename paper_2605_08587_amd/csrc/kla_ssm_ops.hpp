@@ -1,26 +1,51 @@
-// What the kernels of the selective scan share.  Lanes: a wave holds 16 channels, lane = 4 * channel + q, and lane q holds the
-// states n = q K ... q K + K - 1 of its channel (K = S / 4) in registers.  Per-token scalars of a channel (delta, u, z, ...) live with the
-// lane q of token 4 i + q of four: one load and one softplus per token and channel; the quad hands them round by DPP.
+// What the kernels of the selective scan share.  Lanes: a wave holds 8 channels, lane = 8 * channel + o, and lane o of the octet holds the
+// states n = o K ... o K + K - 1 of its channel (K = S / 8) in registers.  Per-token scalars of a channel (delta, u, z, ...) live with lane o
+// for token 8 i + o of eight: one load, one softplus per token and channel; DPP moves hand them round.
 #pragma once
 #include "kla_layer.hpp"
 
 namespace kla {
 
+constexpr int kSsmThreads = 512;                         // kSsmTile channels, eight lanes each
+
+template <int CTRL, int BANKS> __device__ __forceinline__ float dpp_into(float old, float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, 0xf, BANKS, false));
+}
 template <int I> __device__ __forceinline__ float quad_bcast(float x) { return dpp_mov<I * 0x55>(x); }    // lane I of the quad, in all four
 __device__ __forceinline__ float quad_xor1(float x) { return dpp_mov<0xB1>(x); }
 __device__ __forceinline__ float quad_xor2(float x) { return dpp_mov<0x4E>(x); }
-__device__ __forceinline__ float quad_sum(float x)
+
+// The scalars of the octet's eight tokens in both of its quads: of tokens 0-3 (half 0), of tokens 4-7 (half 1), lane q of a quad holding
+// that of token q (4 + q).  Rows of 16 lanes are two octets: the quads of tokens 0-3 are banks 0 and 2.
+struct Oct { float half[2]; };
+__device__ __forceinline__ Oct oct_of(float x)
+{
+    return {{dpp_into<0x114, 0xA>(x, x), dpp_into<0x104, 0x5>(x, x)}};        // row_shr:4 into banks 1, 3; row_shl:4 into banks 0, 2
+}
+template <int J> __device__ __forceinline__ float oct_bcast(const Oct& x) { return quad_bcast<(J & 3)>(x.half[J >> 2]); }
+
+// x[j] summed over the quad, for token j = q in lane q
+__device__ __forceinline__ float quad_sum_own(float x0, float x1, float x2, float x3, bool odd, bool high)
+{
+    const float a = (odd ? x1 : x0) + quad_xor1(odd ? x0 : x1);                // tokens 0, 1
+    const float b = (odd ? x3 : x2) + quad_xor1(odd ? x2 : x3);                // tokens 2, 3
+    return (high ? b : a) + quad_xor2(high ? a : b);
+}
+// x[j] summed over the octet, for token j = o in lane o
+__device__ __forceinline__ float oct_sum_own(const float (&x)[8], int o)
+{
+    const bool odd = o & 1, high = o & 2;
+    const float lo = quad_sum_own(x[0], x[1], x[2], x[3], odd, high), hi = quad_sum_own(x[4], x[5], x[6], x[7], odd, high);
+    const float other = dpp_into<0x114, 0xA>(dpp_into<0x104, 0x5>(lo, lo), hi);     // the other quad's: tokens 0-3 to banks 0, 2; 4-7 to 1, 3
+    return (o & 4 ? hi : lo) + other;
+}
+// the octet's sum, in all its lanes
+__device__ __forceinline__ float oct_sum(float x)
 {
     x += quad_xor1(x);
-    return x + quad_xor2(x);
-}
-// x[i] summed over the quad, for token i = q in lane q
-__device__ __forceinline__ float quad_sum_own(const float (&x)[4], int q)
-{
-    const bool odd = q & 1, high = q & 2;
-    const float a = (odd ? x[1] : x[0]) + quad_xor1(odd ? x[0] : x[1]);        // tokens 0, 1
-    const float b = (odd ? x[3] : x[2]) + quad_xor1(odd ? x[2] : x[3]);        // tokens 2, 3
-    return (high ? b : a) + quad_xor2(high ? a : b);
+    x += quad_xor2(x);
+    return x + dpp_mov<0x141>(x);                        // row_half_mirror: the quad's lanes are alike
 }
 
 // Slot -> the segment it stands for
@@ -38,8 +63,8 @@ template <typename T> __device__ __forceinline__ bool segment_of(const SsmArgs<T
         n = lo;
         base = a.seqs.cu[n] / a.Lseg + n;
     } else {
-        const int per = max(1, (a.seqs.T + a.Lseg - 1) / a.Lseg);
-        n = (int)(slot / per);
+        const int per = max(1, (int)(((long)a.seqs.T + a.Lseg - 1) / a.Lseg));
+        n = (int)slot / per;
         base = (long)n * per;
     }
     g->seq = sequence(a.seqs, n);
@@ -49,6 +74,11 @@ template <typename T> __device__ __forceinline__ bool segment_of(const SsmArgs<T
     // a sequence without a token has one segment without one: its state passes through
     return g->t0 < g->seq.end || (slot == base && g->seq.first == g->seq.end);
 }
+// Slot of a sequence's first segment, and its number of segments
+template <typename T> __device__ __forceinline__ long first_slot(const SsmArgs<T>& a, const Place& p)
+{
+    return a.seqs.cu ? p.first / a.Lseg + p.n : (long)p.n * max(1L, ((long)a.seqs.T + a.Lseg - 1) / a.Lseg);
+}
 // Where the checkpoint of token t stands (t - first a multiple of ck): like the slots, nothing has to be counted
 template <typename T> __device__ __forceinline__ long checkpoint_at(const SsmArgs<T>& a, const Place& p, long t, int ck)
 {
@@ -57,18 +87,84 @@ template <typename T> __device__ __forceinline__ long checkpoint_at(const SsmArg
 }
 
 // The channels of a workgroup: blocks of kSsmTile channels of one group each
-struct Channels { int g, c, most; bool mine; };          // group, this lane's channel (clamped), whether it is one
-__device__ __forceinline__ Channels channels_of(int block, int D, int G, int wave, int lane)
+struct Channels { int g, c; bool mine; };                // group, this lane's channel (clamped), whether it is one
+__device__ __forceinline__ Channels channels_of(int block, int D, int G)
 {
     const int per = D / G, blocks = (per + kSsmTile - 1) / kSsmTile;
     Channels r;
     r.g = block / blocks;
-    const int in = (block - r.g * blocks) * kSsmTile + wave * 16 + (lane >> 2);
+    const int in = (block - r.g * blocks) * kSsmTile + (threadIdx.x >> 3);
     r.mine = in < per;
     r.c = r.g * per + min(in, per - 1);
-    r.most = blocks;
     return r;
 }
 inline int ssm_channel_blocks(int D, int G) { return G * ((D / G + kSsmTile - 1) / kSsmTile); }
+
+// The rows of B and C of a tile of TOK tokens, in LDS as fp32: [token][o][B of the lane's K states, then C].  Every thread brings NE elements,
+// which stay raw until they are stored: converted where they are loaded they would be waited for there.
+template <typename T, int S, int TOK> struct TileBC {
+    static constexpr int K = S / 8, ALL = 2 * TOK * S, NE = (ALL + kSsmThreads - 1) / kSsmThreads;
+    T v[NE];
+    __device__ __forceinline__ void load(const SsmArgs<T>& a, int g, long t, long t1)
+    {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            const int e = min((int)threadIdx.x + kSsmThreads * i, ALL - 1), m = e / (TOK * S), tok = e / S % TOK, n = e % S;
+            // (rows beyond the segment repeat its last: their delta and u are taken for zero)
+            const long at = min(t + tok, t1 - 1);
+            v[i] = (m ? a.C + at * a.ld_C : a.B + at * a.ld_B)[(long)g * S + n];
+        }
+    }
+    __device__ __forceinline__ void store(float* lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            const int e = min((int)threadIdx.x + kSsmThreads * i, ALL - 1), m = e / (TOK * S), tok = e / S % TOK, n = e % S;
+            lds[tok * 2 * S + n / K * 2 * K + m * K + n % K] = to_float(v[i]);
+        }
+    }
+};
+template <int K> struct StateBC { float b[K], c[K]; };
+template <int K> __device__ __forceinline__ StateBC<K> lds_bc(const float* lane_row)
+{
+    StateBC<K> r;
+    if constexpr (K == 1) {
+        const float2 x = *reinterpret_cast<const float2*>(lane_row);
+        r.b[0] = x.x; r.c[0] = x.y;
+    } else if constexpr (K == 2) {
+        const float4 x = *reinterpret_cast<const float4*>(lane_row);
+        r.b[0] = x.x; r.b[1] = x.y; r.c[0] = x.z; r.c[1] = x.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; k += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(lane_row + k), y = *reinterpret_cast<const float4*>(lane_row + K + k);
+            r.b[k] = x.x; r.b[k + 1] = x.y; r.b[k + 2] = x.z; r.b[k + 3] = x.w;
+            r.c[k] = y.x; r.c[k + 1] = y.y; r.c[k + 2] = y.z; r.c[k + 3] = y.w;
+        }
+    }
+    return r;
+}
+// K states of a lane in memory, K * 4 bytes aligned so
+template <int K> __device__ __forceinline__ void load_states(float (&h)[K], const float* p)
+{
+    if constexpr (K == 1) h[0] = *p;
+    if constexpr (K == 2) { const float2 x = *reinterpret_cast<const float2*>(p); h[0] = x.x; h[1] = x.y; }
+    if constexpr (K >= 4) {
+#pragma unroll
+        for (int k = 0; k < K; k += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(p + k);
+            h[k] = x.x; h[k + 1] = x.y; h[k + 2] = x.z; h[k + 3] = x.w;
+        }
+    }
+}
+template <int K> __device__ __forceinline__ void store_states(float* p, const float (&h)[K])
+{
+    if constexpr (K == 1) *p = h[0];
+    if constexpr (K == 2) *reinterpret_cast<float2*>(p) = make_float2(h[0], h[1]);
+    if constexpr (K >= 4) {
+#pragma unroll
+        for (int k = 0; k < K; k += 4) *reinterpret_cast<float4*>(p + k) = make_float4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+    }
+}
 
 }  // namespace kla

@@ -331,8 +331,8 @@ class _Ssm(torch.autograd.Function):
 
 def kla_ssm(u, delta, A, B, C, skip=None, z=None, delta_bias=None, softplus=True, h0=None, cu_seqlens=None, cu_seqlens_host=None, save=True):
     """Differentiable kla_ssm_fwd: (y, hT), gradients with respect to every tensor argument.  Where a gradient is wanted the forward leaves
-    the states at every 256/S-th token behind for the backward (S^2/64 bytes per token and channel: 4 at S = 16); save=False: the backward forms them
-    again.  Same results either way."""
+    the states at every 16th token (every 8th from S = 32 on) behind for the backward, 4 bytes per token and channel at S = 16; save=False: the
+    backward forms them again.  Same results either way."""
     return _Ssm.apply(u, delta, A, B, C, skip, z, delta_bias, h0, bool(softplus), cu_seqlens, cu_seqlens_host,
                       bool(save) and torch.is_grad_enabled())
 

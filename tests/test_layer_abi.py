@@ -136,7 +136,8 @@ def test_queries():
     assert lib.kla_conv_bwd_workspace_bytes(0, 4096, 1024, 4) == 0
     for bad in ((-1, 1, 8, 4), (1, 1, 0, 4), (1, 1, 8, 5), (1, 1, 8, 1)):
         assert lib.kla_conv_bwd_workspace_bytes(*bad) == 0
-    # one checkpoint of [D, S] fp32 per 256/S tokens
+    # one checkpoint of [D, S] fp32 per 16 tokens (8 from S = 32 on)
+    assert lib.kla_ssm_saved_bytes(2, 64, 128, 1, 32, 0) == 2 * 8 * 128 * 32 * 4
     assert lib.kla_ssm_saved_bytes(2, 64, 128, 1, 16, 0) == 2 * 4 * 128 * 16 * 4
     assert lib.kla_ssm_saved_bytes(2, 65, 128, 1, 16, 0) == 2 * 5 * 128 * 16 * 4
     assert lib.kla_ssm_saved_bytes(1, 100, 128, 1, 16, 3) >= (100 // 16 + 3) * 128 * 16 * 4
