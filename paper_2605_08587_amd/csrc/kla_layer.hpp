@@ -155,13 +155,13 @@ template <typename T> struct SsmArgs {
     float* seg_state; float* seg_delta;                  // per slot: [D][S] and [D]; NULL: one segment per sequence
     Seqs seqs; long M; int D, G, Lseg; long slots;
     bool softplus;
+    int channels;                                        // per workgroup: 32 or 64
     // backward
     const T* d_y; const float* d_hT;
     T* du; T* ddelta; T* dz; float* dh0;
     float* part_bc;                                      // [channel block][token][2 S]: gradients of C, then of B
     float* part_p;                                       // [slot][D S + 2 D]: gradients of A, skip, delta_bias
 };
-constexpr int kSsmTile = 64;                             // channels per workgroup
 constexpr int ssm_checkpoint(int S) { return S > 16 ? 8 : 16; }     // tokens between checkpoints
 template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st);
 template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st);

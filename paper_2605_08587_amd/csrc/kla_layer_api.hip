@@ -90,11 +90,12 @@ int ssm_segment(long M, int n_states, int D, int G, int S)
     (void)M; (void)n_states; (void)D; (void)G; (void)S;
     return INT_MAX / 64 * 64;
 }
-struct SsmPlan { int Lseg; long slots, checkpoints; };
+struct SsmPlan { int Lseg; long slots, checkpoints; int channels; };
 SsmPlan ssm_plan(const kla::Seqs& s, long M, int D, int G, int S)
 {
     SsmPlan p;
     p.Lseg = ssm_segment(M, s.n_seq, D, G, S);
+    p.channels = 64;
     const int ck = kla::ssm_checkpoint(S);
     if (s.cu) {
         p.slots = M / p.Lseg + s.n_seq;
@@ -104,10 +105,15 @@ SsmPlan ssm_plan(const kla::Seqs& s, long M, int D, int G, int S)
         p.slots = (per > 0 ? per : 1) * s.n_seq;
         p.checkpoints = ((long)s.T + ck - 1) / ck * s.n_seq;
     }
+    // Workgroups of 64 channels leave half the sums for the gradients of B and C that those of 32 leave; where there are fewer of them
+    // than CUs the smaller ones keep more CUs at work.  At S = 64 the backward needs the registers of a CU for four waves.
+    if (S == 64 || (long)G * ((D / G + 63) / 64) * p.slots < 256) p.channels = 32;
     return p;
 }
 bool ssm_split(const kla::Seqs& s, const SsmPlan& p) { return p.slots > s.n_seq; }
-bool ssm_shape_ok(int D, int G, int S) { return D > 0 && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
+// (a lane's offset from the first of 16 rows fits 32 bits)
+constexpr int kMaxSsmRow = 1 << 24;
+bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
 size_t ssm_saved(const SsmPlan& p, int D, int S) { return round256((size_t)p.checkpoints * D * S * sizeof(float)); }
 struct SsmWork { float *seg_state, *seg_delta, *saved, *part_bc, *part_p; size_t bytes; };
 SsmWork ssm_work(char* base, const kla::Seqs& s, const SsmPlan& p, long M, int D, int G, int S, bool bwd, bool keeps)
@@ -119,7 +125,7 @@ SsmWork ssm_work(char* base, const kla::Seqs& s, const SsmPlan& p, long M, int D
         w.seg_delta = c.take<float>((size_t)p.slots * D);
     }
     if (bwd) {
-        const long blocks = (long)G * ((D / G + kla::kSsmTile - 1) / kla::kSsmTile);
+        const long blocks = (long)G * ((D / G + p.channels - 1) / p.channels);
         if (!keeps) w.saved = c.take<float>((size_t)p.checkpoints * D * S);
         w.part_bc = c.take<float>((size_t)blocks * M * 2 * S);
         w.part_p = c.take<float>((size_t)p.slots * D * (S + 2));
@@ -132,6 +138,7 @@ int ssm_check(const void* u, long ld_u, const void* delta, long ld_delta, const 
 {
     if (!dt_ok(dt)) return KLA_ERR_DTYPE;
     if (!ssm_shape_ok(D, G, S) || ld_u < D || ld_delta < D || ld_B < (long)G * S || ld_C < (long)G * S || (z && ld_z < D) ||
+        ld_u > kMaxSsmRow || ld_delta > kMaxSsmRow || ld_B > kMaxSsmRow || ld_C > kMaxSsmRow || ld_z > kMaxSsmRow ||
         (opts & ~(unsigned)KLA_LAYER_SOFTPLUS))
         return KLA_ERR_SHAPE;
     if (!A) return KLA_ERR_NULL;
@@ -147,7 +154,7 @@ kla::SsmArgs<T> ssm_args(const void* u, long ld_u, const void* delta, long ld_de
     a.u = static_cast<const T*>(u); a.ld_u = ld_u; a.delta = static_cast<const T*>(delta); a.ld_delta = ld_delta; a.A = A;
     a.B = static_cast<const T*>(B); a.ld_B = ld_B; a.C = static_cast<const T*>(C); a.ld_C = ld_C;
     a.skip = skip; a.z = static_cast<const T*>(z); a.ld_z = ld_z; a.delta_bias = delta_bias; a.h0 = h0;
-    a.seqs = s; a.M = M; a.D = D; a.G = G; a.Lseg = p.Lseg; a.slots = p.slots;
+    a.seqs = s; a.M = M; a.D = D; a.G = G; a.Lseg = p.Lseg; a.slots = p.slots; a.channels = p.channels;
     a.softplus = (opts & KLA_LAYER_SOFTPLUS) != 0;
     return a;
 }
@@ -353,7 +360,7 @@ int kla_ssm_step(const void* u, long ld_u, const void* delta, long ld_delta, con
     if (N > 0 && (!u || !delta || !B || !C || !h || !y)) return KLA_ERR_NULL;
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, y}) || !aligned(16, {A, h}) || !aligned(4, {skip, delta_bias})) return KLA_ERR_ALIGN;
     const kla::Seqs s = {nullptr, N, 1};
-    const SsmPlan p = {1, N, N};
+    const SsmPlan p = {1, N, N, 64};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.y = static_cast<decltype(a.y)>(y);

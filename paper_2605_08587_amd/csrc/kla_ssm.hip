@@ -9,26 +9,11 @@ namespace kla {
 
 constexpr int kTok = 16;                                 // tokens per tile
 
-// What a lane takes of a tile: tokens 8 i + o of its channel, raw until they are used.  Nothing is read beyond the segment.
-template <typename T, bool HASZ> struct TileTok {
-    T u[2], raw[2], z[2];
-    __device__ __forceinline__ void load(const SsmArgs<T>& a, int c, int o, long t, long t1)
-    {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const long at = min(t + 8 * i + o, t1 - 1);
-            u[i] = a.u[at * a.ld_u + c];
-            raw[i] = a.delta[at * a.ld_delta + c];
-            if constexpr (HASZ) z[i] = a.z[at * a.ld_z + c];
-        }
-    }
-};
-
 enum SsmMode { kSsmOutputs, kSsmStates, kSsmMaps };      // y (and checkpoints); checkpoints alone; the maps of the segments
 
-// One workgroup: 64 channels of one segment, tiles of 16 tokens one after the other, two tiles on their way.
-template <typename T, int S, SsmMode MODE, bool HASZ>
-__global__ __launch_bounds__(kSsmThreads) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
+// One workgroup: THREADS / 8 channels of one segment, tiles of 16 tokens one after the other, two tiles on their way.
+template <typename T, int S, SsmMode MODE, bool HASZ, int THREADS>
+__global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
 {
     constexpr int K = S / 8, CK = ssm_checkpoint(S);
     __shared__ __align__(16) float lds[2][2 * kTok * S];
@@ -38,9 +23,9 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_fwd_kernel(SsmArgs<T> a, int 
     Segment g;
     if (!segment_of(a, slot, &g)) return;
     if (MODE == kSsmMaps && g.last) return;              // nothing follows it
-    const Channels ch = channels_of(block, a.D, a.G);
+    const Channels ch = channels_of(block, a.D, a.G, THREADS / 8);
     const int c = ch.c;
-    const long mine = ((long)c * S) + o * K;             // this lane's states of [D][S]
+    const long mine = ((long)c * S) + o * K, DS = (long)a.D * S;         // this lane's states of [D][S]
 
     float A2[K], h[K];
     load_states<K>(A2, a.A + mine);
@@ -48,32 +33,53 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_fwd_kernel(SsmArgs<T> a, int 
     for (int k = 0; k < K; ++k) { A2[k] *= kLog2e; h[k] = 0.f; }
     const float skip = a.skip ? a.skip[c] : 0.f, bias = a.delta_bias ? a.delta_bias[c] : 0.f;
     if (MODE != kSsmMaps) {
-        if (a.seg_state) load_states<K>(h, a.seg_state + slot * a.D * S + mine);
-        else if (a.h0) load_states<K>(h, a.h0 + (long)g.seq.n * a.D * S + mine);
+        if (a.seg_state) load_states<K>(h, a.seg_state + slot * DS + mine);
+        else if (a.h0) load_states<K>(h, a.h0 + (long)g.seq.n * DS + mine);
     }
     float sum_delta = 0.f;
+    const bool saves = MODE != kSsmMaps && a.saved;
+    float* saved = saves ? a.saved + checkpoint_at(a, g.seq, g.t0, CK) * DS : nullptr;
 
-    TileBC<T, S, kTok> bc[2];
-    TileTok<T, HASZ> tk[2];
+    TileBC<T, S, kTok, THREADS> bc[2];
+    Tokens<const T, 2> pu, pd, pz;
+    Tokens<T, 2> py;
+    T in_u[2][2], in_d[2][2], in_z[2][2];
+    bc[0].init(a, ch.g);
+    bc[1].init(a, ch.g);
+    pu.init(a.u, a.ld_u, c, o);
+    pd.init(a.delta, a.ld_delta, c, o);
+    if constexpr (HASZ) pz.init(a.z, a.ld_z, c, o);
+    py.init(a.y, a.D, c, o);
+    auto load = [&](auto which, long t) {
+        constexpr int w = which.value;
+        bc[w].load(t, g.t1);
+        pu.load(in_u[w], t, g.t1);
+        pd.load(in_d[w], t, g.t1);
+        if constexpr (HASZ) pz.load(in_z[w], t, g.t1);
+    };
     auto tile = [&](auto which, long t) {
         constexpr int w = which.value;
         bc[w].store(lds[w]);
-        const TileTok<T, HASZ> now = tk[w];
-        __syncthreads();
-        if (t + 2 * kTok < g.t1) {
-            bc[w].load(a, ch.g, t + 2 * kTok, g.t1);
-            tk[w].load(a, c, o, t + 2 * kTok, g.t1);
+        float u[2], raw[2], z[2], y[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            u[i] = to_float(in_u[w][i]);
+            raw[i] = to_float(in_d[w][i]) + bias;
+            if constexpr (HASZ) z[i] = to_float(in_z[w][i]);
         }
+        __syncthreads();
+        if (t + 2 * kTok < g.t1) load(which, t + 2 * kTok);
+        const int left = (int)min(g.t1 - t, (long)kTok);
         const float* row = lds[w] + o * 2 * K;
-        float y[2];
         static_for<2>([&](auto i) {
-            if (MODE != kSsmMaps && (8 * i.value) % CK == 0 && a.saved && t + 8 * i.value < g.t1 && ch.mine)
-                store_states<K>(a.saved + checkpoint_at(a, g.seq, t + 8 * i.value, CK) * a.D * S + mine, h);
+            if (saves && (8 * i.value) % CK == 0) {
+                if (8 * i.value < left && ch.mine) store_states<K>(saved + mine, h);
+                saved += DS;
+            }
             // a token beyond the segment decays nothing and adds nothing
-            const bool in = t + 8 * i.value + o < g.t1;
-            const float u = to_float(now.u[i.value]), raw = to_float(now.raw[i.value]) + bias, soft = softplus(raw);
-            const float delta = in ? (a.softplus ? soft : raw) : 0.f;
-            const Oct ds = oct_of(delta), us = oct_of(in ? delta * u : 0.f);
+            const bool in = 8 * i.value + o < left;
+            const float soft = softplus(raw[i.value]), delta = in ? (a.softplus ? soft : raw[i.value]) : 0.f;
+            const Oct ds = oct_of(delta), us = oct_of(in ? delta * u[i.value] : 0.f);
             float acc[8];
             static_for<8>([&](auto j) {
                 const float dj = oct_bcast<j.value>(ds), uj = oct_bcast<j.value>(us);
@@ -88,29 +94,17 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_fwd_kernel(SsmArgs<T> a, int 
             });
             if (MODE == kSsmMaps) sum_delta += delta;
             if (MODE == kSsmOutputs) {
-                y[i.value] = fmaf(skip, u, oct_sum_own(acc, o));
-                if constexpr (HASZ) {
-                    const float z = to_float(now.z[i.value]);
-                    y[i.value] *= z * sigmoid(z);
-                }
+                y[i.value] = fmaf(skip, u[i.value], oct_sum_own(acc, o));
+                if constexpr (HASZ) y[i.value] *= z[i.value] * sigmoid(z[i.value]);
             }
         });
         if (MODE == kSsmOutputs && ch.mine) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const long at = t + 8 * i + o;
-                if (at < g.t1) a.y[at * a.D + c] = from_float<T>(y[i]);
-            }
+            for (int i = 0; i < 2; ++i) if (8 * i + o < left) py.store(i, t, from_float<T>(y[i]));
         }
     };
-    if (g.t0 < g.t1) {
-        bc[0].load(a, ch.g, g.t0, g.t1);
-        tk[0].load(a, c, o, g.t0, g.t1);
-        if (g.t0 + kTok < g.t1) {
-            bc[1].load(a, ch.g, g.t0 + kTok, g.t1);
-            tk[1].load(a, c, o, g.t0 + kTok, g.t1);
-        }
-    }
+    if (g.t0 < g.t1) load(IntC<0>(), g.t0);
+    if (g.t0 + kTok < g.t1) load(IntC<1>(), g.t0 + kTok);
     for (long t = g.t0; t < g.t1; t += 2 * kTok) {
         tile(IntC<0>(), t);
         if (t + kTok < g.t1) tile(IntC<1>(), t + kTok);
@@ -118,10 +112,10 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_fwd_kernel(SsmArgs<T> a, int 
     if (MODE == kSsmMaps) sum_delta = oct_sum(sum_delta);
     if (!ch.mine) return;
     if (MODE == kSsmMaps) {
-        store_states<K>(a.seg_state + slot * a.D * S + mine, h);
+        store_states<K>(a.seg_state + slot * DS + mine, h);
         if (o == 0) a.seg_delta[slot * a.D + c] = sum_delta;
     } else if (a.hT && g.last) {
-        store_states<K>(a.hT + (long)g.seq.n * a.D * S + mine, h);
+        store_states<K>(a.hT + (long)g.seq.n * DS + mine, h);
     }
 }
 
@@ -178,23 +172,30 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmArgs<T> a, float* __re
     }
 }
 
-template <typename T, int S> static hipError_t ssm_fwd(const SsmArgs<T>& a, bool outputs, hipStream_t st)
+template <typename T, int S, int THREADS> static hipError_t ssm_fwd_by(const SsmArgs<T>& a, bool outputs, hipStream_t st)
 {
-    const int blocks_c = ssm_channel_blocks(a.D, a.G);
+    const int blocks_c = ssm_channel_blocks(a.D, a.G, THREADS / 8);
     const long blocks = blocks_c * a.slots;
     if (blocks == 0) return hipSuccess;
     if (blocks > 0x7fffffffL || a.seqs.n_seq > 65535) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks), block(kSsmThreads);
+    const dim3 grid((unsigned)blocks), block(THREADS);
     if (a.seg_state) {
-        hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmMaps, false>), grid, block, 0, st, a, blocks_c);
+        hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmMaps, false, THREADS>), grid, block, 0, st, a, blocks_c);
         if (const hipError_t e = hipGetLastError()) return e;
         hipLaunchKernelGGL((ssm_join_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    if (!outputs) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmStates, false>), grid, block, 0, st, a, blocks_c);
-    else if (a.z) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, true>), grid, block, 0, st, a, blocks_c);
-    else          hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, false>), grid, block, 0, st, a, blocks_c);
+    if (!outputs) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmStates, false, THREADS>), grid, block, 0, st, a, blocks_c);
+    else if (a.z) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, true, THREADS>), grid, block, 0, st, a, blocks_c);
+    else          hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, false, THREADS>), grid, block, 0, st, a, blocks_c);
     return hipGetLastError();
+}
+template <typename T, int S> static hipError_t ssm_fwd(const SsmArgs<T>& a, bool outputs, hipStream_t st)
+{
+    if constexpr (S < 64) {
+        if (a.channels == 64) return ssm_fwd_by<T, S, 512>(a, outputs, st);
+    }
+    return ssm_fwd_by<T, S, 256>(a, outputs, st);
 }
 template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st)
 {

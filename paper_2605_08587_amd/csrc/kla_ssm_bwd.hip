@@ -29,11 +29,11 @@ __device__ __forceinline__ float swap16_sum(float x, float y)
 }
 
 // MAPS: what a segment adds to the gradient that enters the one before it, from zeros (with the segment's sum of delta).
-template <typename T, int S, bool MAPS, bool HASZ>
-__global__ __launch_bounds__(kSsmThreads) void ssm_bwd_kernel(SsmArgs<T> a, int blocks_c)
+template <typename T, int S, bool MAPS, bool HASZ, int THREADS>
+__global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int blocks_c)
 {
     constexpr int K = S / 8, CK = ssm_checkpoint(S), NG = CK / 8;    // tokens per checkpoint and tile, in groups of eight
-    constexpr int WAVES = kSsmThreads / 64;
+    constexpr int WAVES = THREADS / 64;
     __shared__ __align__(16) float lds[2][2 * CK * S];
     __shared__ float red[MAPS ? 1 : WAVES][MAPS ? 1 : CK][2 * S];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, o = lane & 7;
@@ -42,57 +42,77 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_bwd_kernel(SsmArgs<T> a, int 
     Segment g;
     if (!segment_of(a, slot, &g)) return;
     if (MAPS && g.t0 == g.seq.first) return;             // nothing stands before it
-    const Channels ch = channels_of(block, a.D, a.G);
+    const Channels ch = channels_of(block, a.D, a.G, THREADS / 8);
     const int c = ch.c;
-    const long mine = (long)c * S + o * K;
+    const long mine = (long)c * S + o * K, DS = (long)a.D * S;
 
     float A2[K], dA[K], ag[K];                           // ag: a_{t+1} g_{t+1}
     load_states<K>(A2, a.A + mine);
 #pragma unroll
     for (int k = 0; k < K; ++k) { A2[k] *= kLog2e; dA[k] = ag[k] = 0.f; }
     if (!MAPS) {
-        if (a.seg_state) load_states<K>(ag, a.seg_state + slot * a.D * S + mine);
-        else if (a.d_hT) load_states<K>(ag, a.d_hT + (long)g.seq.n * a.D * S + mine);
+        if (a.seg_state) load_states<K>(ag, a.seg_state + slot * DS + mine);
+        else if (a.d_hT) load_states<K>(ag, a.d_hT + (long)g.seq.n * DS + mine);
     }
     const float skip = a.skip ? a.skip[c] : 0.f, bias = a.delta_bias ? a.delta_bias[c] : 0.f;
     float d_skip = 0.f, d_bias = 0.f, sum_delta = 0.f;
 
-    TileBC<T, S, CK> bc;
-    struct { T u[NG], raw[NG], z[NG], dy[NG]; float h[K]; } in;
-    auto load = [&](long t) {
-        bc.load(a, ch.g, t, g.t1);
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-            const long at = min(t + 8 * i + o, g.t1 - 1);
-            in.u[i] = a.u[at * a.ld_u + c];
-            in.raw[i] = a.delta[at * a.ld_delta + c];
-            if constexpr (HASZ) in.z[i] = a.z[at * a.ld_z + c];
-            in.dy[i] = a.d_y[at * a.D + c];
-        }
-        if constexpr (!MAPS) load_states<K>(in.h, a.saved + checkpoint_at(a, g.seq, t, CK) * a.D * S + mine);
-    };
+    TileBC<T, S, CK, THREADS> bc;
+    Tokens<const T, NG> pu, pd, pz, py;
+    Tokens<T, NG> qu, qd, qz;
+    bc.init(a, ch.g);
+    pu.init(a.u, a.ld_u, c, o);
+    pd.init(a.delta, a.ld_delta, c, o);
+    if constexpr (HASZ) pz.init(a.z, a.ld_z, c, o);
+    py.init(a.d_y, a.D, c, o);
+    if constexpr (!MAPS) {
+        qu.init(a.du, a.D, c, o);
+        qd.init(a.ddelta, a.D, c, o);
+        if constexpr (HASZ) qz.init(a.dz, a.D, c, o);
+    }
     const long tiles = (g.t1 - g.t0 + CK - 1) / CK;
-    if (tiles > 0) load(g.t0 + (tiles - 1) * CK);
+    const float* saved = MAPS || tiles == 0 ? nullptr : a.saved + checkpoint_at(a, g.seq, g.t0, CK) * DS;
+    T in_u[NG], in_d[NG], in_z[NG], in_y[NG];
+    float in_h[K];
+    auto load = [&](long tile) {
+        const long t = g.t0 + tile * CK;
+        bc.load(t, g.t1);
+        pu.load(in_u, t, g.t1);
+        pd.load(in_d, t, g.t1);
+        if constexpr (HASZ) pz.load(in_z, t, g.t1);
+        py.load(in_y, t, g.t1);
+        if constexpr (!MAPS) load_states<K>(in_h, saved + tile * DS + mine);
+    };
+    if (tiles > 0) load(tiles - 1);
     int buf = 0;
     for (long tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
         const long t = g.t0 + tile * CK;
+        const int left = (int)min(g.t1 - t, (long)CK);
         bc.store(lds[buf]);
-        const auto now = in;
+        float u[NG], raw[NG], z[NG], dy[NG], delta[NG], dc[NG], core[NG];
+        float h[MAPS ? 1 : CK + 1][K];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            u[i] = to_float(in_u[i]);
+            raw[i] = to_float(in_d[i]) + bias;
+            if constexpr (HASZ) z[i] = to_float(in_z[i]);
+            dy[i] = to_float(in_y[i]);
+        }
+        if constexpr (!MAPS) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) h[0][k] = in_h[k];
+        }
         __syncthreads();
-        if (tile > 0) load(t - CK);
+        if (tile > 0) load(tile - 1);
         // a token beyond the segment decays nothing, adds nothing and has no gradient; nor has a lane without a channel of its own
-        float u[NG], raw[NG], dy[NG], delta[NG], dc[NG], core[NG];
         Oct ds[NG], us[NG], cs[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-            const bool live = t + 8 * i + o < g.t1, own = live && ch.mine;
-            u[i] = to_float(now.u[i]);
-            raw[i] = to_float(now.raw[i]) + bias;
-            dy[i] = to_float(now.dy[i]);
+            const bool live = 8 * i + o < left, own = live && ch.mine;
             const float soft = softplus(raw[i]);
             delta[i] = live ? (a.softplus ? soft : raw[i]) : 0.f;
             float gate = 1.f;
-            if constexpr (HASZ) { const float z = to_float(now.z[i]); gate = z * sigmoid(z); }
+            if constexpr (HASZ) gate = z[i] * sigmoid(z[i]);
             dc[i] = own ? dy[i] * gate : 0.f;
             ds[i] = oct_of(delta[i]);
             us[i] = oct_of(own ? delta[i] * u[i] : 0.f);
@@ -111,9 +131,7 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_bwd_kernel(SsmArgs<T> a, int 
         } else {
             // (at S = 64 the decays would not fit the registers with the states: there they are formed a second time)
             constexpr bool KEEP = K < 8;
-            float h[CK + 1][K], dec[KEEP ? CK : 1][K];
-#pragma unroll
-            for (int k = 0; k < K; ++k) h[0][k] = now.h[k];
+            float dec[KEEP ? CK : 1][K];
             static_for<NG>([&](auto i) {
                 float acc[8];
                 static_for<8>([&](auto j) {
@@ -176,28 +194,23 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_bwd_kernel(SsmArgs<T> a, int 
                     }
                 });
                 const float sa = oct_sum_own(via_a, o) * kLn2, sb = oct_sum_own(via_b, o);
-                const bool live = t + 8 * i + o < g.t1;
                 float d_raw = fmaf(u[i], sb, sa);
                 d_raw *= a.softplus ? sigmoid(raw[i]) : 1.f;
-                if (live) {
+                if (8 * i + o < left && ch.mine) {
                     d_bias += d_raw;
                     d_skip = fmaf(dc[i], u[i], d_skip);
-                    if (ch.mine) {
-                        const long at = (t + 8 * i + o) * a.D + c;
-                        a.du[at] = from_float<T>(fmaf(delta[i], sb, skip * dc[i]));
-                        a.ddelta[at] = from_float<T>(d_raw);
-                        if constexpr (HASZ) {
-                            const float z = to_float(now.z[i]), s = sigmoid(z);
-                            a.dz[at] = from_float<T>(dy[i] * core[i] * (s * fmaf(z, 1.f - s, 1.f)));
-                        }
+                    qu.store(i, t, from_float<T>(fmaf(delta[i], sb, skip * dc[i])));
+                    qd.store(i, t, from_float<T>(d_raw));
+                    if constexpr (HASZ) {
+                        const float s = sigmoid(z[i]);
+                        qz.store(i, t, from_float<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f))));
                     }
                 }
             });
             __syncthreads();
             // the waves' channels together: [token][2 S], C first
             float* out = a.part_bc + ((long)block * a.M + t) * (2 * S);
-            const int n_out = (int)min((long)CK, g.t1 - t) * 2 * S;
-            for (int e = threadIdx.x; e < n_out; e += kSsmThreads) {
+            for (int e = threadIdx.x; e < left * 2 * S; e += THREADS) {
                 const float* r = &red[0][0][0] + e;
                 float s = 0.f;
 #pragma unroll
@@ -212,10 +225,10 @@ __global__ __launch_bounds__(kSsmThreads) void ssm_bwd_kernel(SsmArgs<T> a, int 
     d_bias = oct_sum(d_bias);
     if (!ch.mine) return;
     if constexpr (MAPS) {
-        store_states<K>(a.seg_state + slot * a.D * S + mine, ag);
+        store_states<K>(a.seg_state + slot * DS + mine, ag);
         if (o == 0) a.seg_delta[slot * a.D + c] = sum_delta;
     } else {
-        if (a.dh0 && g.t0 == g.seq.first) store_states<K>(a.dh0 + (long)g.seq.n * a.D * S + mine, ag);
+        if (a.dh0 && g.t0 == g.seq.first) store_states<K>(a.dh0 + (long)g.seq.n * DS + mine, ag);
         float* p = a.part_p + slot * ((long)a.D * (S + 2));
         store_states<K>(p + mine, dA);
         if (o == 0) {
@@ -270,16 +283,16 @@ __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const float* __restrict
     else       dB[(tok * G + g) * S + n - S] = from_float<T>(s);
 }
 
-template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
+template <typename T, int S, int THREADS> static hipError_t ssm_bwd_by(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
 {
-    const int blocks_c = ssm_channel_blocks(a.D, a.G);
+    const int blocks_c = ssm_channel_blocks(a.D, a.G, THREADS / 8);
     const long blocks = blocks_c * a.slots, row = (long)a.D * (S + 2);
     if (blocks > 0x7fffffffL || a.seqs.n_seq > 65535 || a.G > 65535 || (a.M * 2 * S + 255) / 256 > 0x7fffffffL) return hipErrorInvalidConfiguration;
     if (blocks > 0) {
-        const dim3 grid((unsigned)blocks), block(kSsmThreads);
+        const dim3 grid((unsigned)blocks), block(THREADS);
         if (a.seg_state) {
-            if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, true>), grid, block, 0, st, a, blocks_c);
-            else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, false>), grid, block, 0, st, a, blocks_c);
+            if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, true, THREADS>), grid, block, 0, st, a, blocks_c);
+            else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, false, THREADS>), grid, block, 0, st, a, blocks_c);
             if (const hipError_t e = hipGetLastError()) return e;
             hipLaunchKernelGGL((ssm_join_bwd_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
             if (const hipError_t e = hipGetLastError()) return e;
@@ -288,8 +301,8 @@ template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, floa
             hipLaunchKernelGGL((ssm_clear_kernel<T>), dim3((unsigned)a.slots), dim3(256), 0, st, a, row);
             if (const hipError_t e = hipGetLastError()) return e;
         }
-        if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, true>), grid, block, 0, st, a, blocks_c);
-        else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, false>), grid, block, 0, st, a, blocks_c);
+        if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, true, THREADS>), grid, block, 0, st, a, blocks_c);
+        else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, false, THREADS>), grid, block, 0, st, a, blocks_c);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     if (a.M > 0) {
@@ -298,6 +311,13 @@ template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, floa
         if (const hipError_t e = hipGetLastError()) return e;
     }
     return launch_column_sums(a.part_p, a.slots, {{(long)a.D * S, a.D, a.D}, {dA, dskip, ddelta_bias}}, st);
+}
+template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
+{
+    if constexpr (S < 64) {
+        if (a.channels == 64) return ssm_bwd_by<T, S, 512>(a, dA, dB, dC, dskip, ddelta_bias, st);
+    }
+    return ssm_bwd_by<T, S, 256>(a, dA, dB, dC, dskip, ddelta_bias, st);
 }
 template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
 {

@@ -2,11 +2,11 @@
 // states n = o K ... o K + K - 1 of its channel (K = S / 8) in registers.  Per-token scalars of a channel (delta, u, z, ...) live with lane o
 // for token 8 i + o of eight: one load, one softplus per token and channel; DPP moves hand them round.
 #pragma once
+#include <type_traits>
+
 #include "kla_layer.hpp"
 
 namespace kla {
-
-constexpr int kSsmThreads = 512;                         // kSsmTile channels, eight lanes each
 
 template <int CTRL, int BANKS> __device__ __forceinline__ float dpp_into(float old, float x)
 {
@@ -67,6 +67,7 @@ template <typename T> __device__ __forceinline__ bool segment_of(const SsmArgs<T
         n = (int)slot / per;
         base = (long)n * per;
     }
+    n = __builtin_amdgcn_readfirstlane(n);               // (one slot per workgroup: all of this is the same for its lanes)
     g->seq = sequence(a.seqs, n);
     g->t0 = g->seq.first + (slot - base) * a.Lseg;
     g->t1 = min(g->t0 + a.Lseg, g->seq.end);
@@ -86,42 +87,87 @@ template <typename T> __device__ __forceinline__ long checkpoint_at(const SsmArg
     return base + (t - p.first) / ck;
 }
 
-// The channels of a workgroup: blocks of kSsmTile channels of one group each
+// The channels of a workgroup: blocks of `channels` of one group each
 struct Channels { int g, c; bool mine; };                // group, this lane's channel (clamped), whether it is one
-__device__ __forceinline__ Channels channels_of(int block, int D, int G)
+__device__ __forceinline__ Channels channels_of(int block, int D, int G, int channels)
 {
-    const int per = D / G, blocks = (per + kSsmTile - 1) / kSsmTile;
+    const int per = D / G, blocks = (per + channels - 1) / channels;
     Channels r;
     r.g = block / blocks;
-    const int in = (block - r.g * blocks) * kSsmTile + (threadIdx.x >> 3);
+    const int in = (block - r.g * blocks) * channels + (int)(threadIdx.x >> 3);
     r.mine = in < per;
     r.c = r.g * per + min(in, per - 1);
     return r;
 }
-inline int ssm_channel_blocks(int D, int G) { return G * ((D / G + kSsmTile - 1) / kSsmTile); }
+inline int ssm_channel_blocks(int D, int G, int channels) { return G * ((D / G + channels - 1) / channels); }
 
-// The rows of B and C of a tile of TOK tokens, in LDS as fp32: [token][o][B of the lane's K states, then C].  Every thread brings NE elements,
-// which stay raw until they are stored: converted where they are loaded they would be waited for there.
-template <typename T, int S, int TOK> struct TileBC {
-    static constexpr int K = S / 8, ALL = 2 * TOK * S, NE = (ALL + kSsmThreads - 1) / kSsmThreads;
+// An element by a base that is the same for the wave and this lane's offset in bytes: no address arithmetic in the vector unit
+template <typename T> __device__ __forceinline__ T load_at(const T* base, unsigned bytes)
+{
+    return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes);
+}
+template <typename T> __device__ __forceinline__ void store_at(T* base, unsigned bytes, T x)
+{
+    *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes) = x;
+}
+// A lane's tokens 8 i + o of a tile of one input [tokens][ld], raw: converted where they are loaded they would be waited for there.  In a tile
+// that the segment's end cuts the last row is repeated: nothing is read beyond it.
+template <typename T, int NG> struct Tokens {
+    T* p; long ld; unsigned off[NG]; int c, o;
+    __device__ __forceinline__ void init(T* base, long ld_, int c_, int o_)
+    {
+        p = base; ld = ld_; c = c_; o = o_;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) off[i] = (unsigned)((8 * i + o) * ld + c) * (unsigned)sizeof(T);
+    }
+    __device__ __forceinline__ void load(std::remove_const_t<T> (&v)[NG], long t, long t1) const
+    {
+        T* b = p + t * ld;
+        if (t + 8 * NG <= t1) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) v[i] = load_at(b, off[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) v[i] = load_at(b, (unsigned)(min(8 * i + o, (int)(t1 - 1 - t)) * ld + c) * (unsigned)sizeof(T));
+        }
+    }
+    __device__ __forceinline__ void store(int i, long t, T x) const { store_at(p + t * ld, off[i], x); }
+};
+
+// The rows of B and C of a tile of TOK tokens, in LDS as fp32: [token][o][B of the lane's K states, then C].  Every thread brings NE elements.
+template <typename T, int S, int TOK, int THREADS> struct TileBC {
+    static constexpr int K = S / 8, ALL = 2 * TOK * S, NE = (ALL + THREADS - 1) / THREADS;
+    static_assert(TOK * S % 64 == 0, "a wave's elements are of B or of C");
+    const T* p[NE]; long ld[NE]; unsigned off[NE]; int tok[NE], at[NE], n[NE];
     T v[NE];
-    __device__ __forceinline__ void load(const SsmArgs<T>& a, int g, long t, long t1)
+    __device__ __forceinline__ void init(const SsmArgs<T>& a, int g)
     {
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-            const int e = min((int)threadIdx.x + kSsmThreads * i, ALL - 1), m = e / (TOK * S), tok = e / S % TOK, n = e % S;
+            const int e = (int)threadIdx.x + THREADS * i;
+            const int m = __builtin_amdgcn_readfirstlane(e) / (TOK * S);         // 0: of B, 1: of C, 2: none
+            tok[i] = e / S % TOK;
+            n[i] = g * S + e % S;
+            p[i] = m == 1 ? a.C : a.B;
+            ld[i] = m == 1 ? a.ld_C : a.ld_B;
+            off[i] = (unsigned)(tok[i] * ld[i] + n[i]) * (unsigned)sizeof(T);
+            at[i] = m > 1 ? -1 : tok[i] * 2 * S + e % S / K * 2 * K + m * K + e % K;
+        }
+    }
+    __device__ __forceinline__ void load(long t, long t1)
+    {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            const T* b = p[i] + t * ld[i];
             // (rows beyond the segment repeat its last: their delta and u are taken for zero)
-            const long at = min(t + tok, t1 - 1);
-            v[i] = (m ? a.C + at * a.ld_C : a.B + at * a.ld_B)[(long)g * S + n];
+            if (t + TOK <= t1) v[i] = load_at(b, off[i]);
+            else v[i] = load_at(b, (unsigned)(min(tok[i], (int)(t1 - 1 - t)) * ld[i] + n[i]) * (unsigned)sizeof(T));
         }
     }
     __device__ __forceinline__ void store(float* lds) const
     {
 #pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            const int e = min((int)threadIdx.x + kSsmThreads * i, ALL - 1), m = e / (TOK * S), tok = e / S % TOK, n = e % S;
-            lds[tok * 2 * S + n / K * 2 * K + m * K + n % K] = to_float(v[i]);
-        }
+        for (int i = 0; i < NE; ++i) if (ALL % THREADS == 0 || at[i] >= 0) lds[at[i]] = to_float(v[i]);
     }
 };
 template <int K> struct StateBC { float b[K], c[K]; };
