@@ -40,26 +40,37 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
     const bool saves = MODE != kSsmMaps && a.saved;
     float* saved = saves ? a.saved + checkpoint_at(a, g.seq, g.t0, CK) * DS : nullptr;
 
-    TileBC<T, S, kTok, THREADS> bc[2];
+    TileBC<T, S, kTok, THREADS> bc;
     Tokens<const T, 2> pu, pd, pz;
     Tokens<T, 2> py;
-    T in_u[2][2], in_d[2][2], in_z[2][2];
-    bc[0].init(a, ch.g);
-    bc[1].init(a, ch.g);
-    pu.init(a.u, a.ld_u, c, o);
-    pd.init(a.delta, a.ld_delta, c, o);
-    if constexpr (HASZ) pz.init(a.z, a.ld_z, c, o);
-    py.init(a.y, a.D, c, o);
-    auto load = [&](auto which, long t) {
+    T in_bc[2][decltype(bc)::NE], in_u[2][2], in_d[2][2], in_z[2][2];
+    bc.init(a, ch.g, g.t0);
+    pu.init(a.u, g.t0, (int)a.ld_u, c, o);
+    pd.init(a.delta, g.t0, (int)a.ld_delta, c, o);
+    if constexpr (HASZ) pz.init(a.z, g.t0, (int)a.ld_z, c, o);
+    py.init(a.y, g.t0, a.D, c, o);
+    const int tokens = (int)(g.t1 - g.t0);
+    // the tile at token `at` of the segment, and the bases on to the next
+    auto load = [&](auto which, int at) {
         constexpr int w = which.value;
-        bc[w].load(t, g.t1);
-        pu.load(in_u[w], t, g.t1);
-        pd.load(in_d[w], t, g.t1);
-        if constexpr (HASZ) pz.load(in_z[w], t, g.t1);
+        auto rows = [&](auto full) {
+            constexpr bool FULL = full.value != 0;
+            const int last = tokens - 1 - at;
+            bc.template load<FULL>(in_bc[w], last);
+            pu.template load<FULL>(in_u[w], last, o);
+            pd.template load<FULL>(in_d[w], last, o);
+            if constexpr (HASZ) pz.template load<FULL>(in_z[w], last, o);
+        };
+        if (at + kTok <= tokens) rows(IntC<1>());
+        else rows(IntC<0>());
+        bc.move(kTok);
+        pu.move(kTok);
+        pd.move(kTok);
+        if constexpr (HASZ) pz.move(kTok);
     };
-    auto tile = [&](auto which, long t) {
+    auto tile = [&](auto which, int at) {
         constexpr int w = which.value;
-        bc[w].store(lds[w]);
+        bc.store(lds[w], in_bc[w]);
         float u[2], raw[2], z[2], y[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -68,29 +79,45 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
             if constexpr (HASZ) z[i] = to_float(in_z[w][i]);
         }
         __syncthreads();
-        if (t + 2 * kTok < g.t1) load(which, t + 2 * kTok);
-        const int left = (int)min(g.t1 - t, (long)kTok);
+        if (at + 2 * kTok < tokens) load(which, at + 2 * kTok);
+        const int left = tokens - at;
         const float* row = lds[w] + o * 2 * K;
         static_for<2>([&](auto i) {
             if (saves && (8 * i.value) % CK == 0) {
                 if (8 * i.value < left && ch.mine) store_states<K>(saved + mine, h);
                 saved += DS;
             }
+            // In three steps, in this order: what eight tokens need from LDS is on its way while their steps and decays are formed, and the
+            // chain of states finds everything at hand.  (Left to itself the compiler reads each row where it is used and waits.)
+            constexpr int AHEAD = K <= 4 ? 8 : 4;
+            StateBC<K> m[AHEAD];
+            static_for<AHEAD>([&](auto j) { m[j.value] = lds_bc<K>(row + (8 * i.value + j.value) * 2 * S); });
+            __builtin_amdgcn_sched_barrier(0);
             // a token beyond the segment decays nothing and adds nothing
             const bool in = 8 * i.value + o < left;
-            const float soft = softplus(raw[i.value]), delta = in ? (a.softplus ? soft : raw[i.value]) : 0.f;
-            const Oct ds = oct_of(delta), us = oct_of(in ? delta * u[i.value] : 0.f);
+            const float soft = softplus(raw[i.value]), delta = where(in, a.softplus ? soft : raw[i.value]);
+            const Oct ds = oct_of(delta), us = oct_of(where(in, delta * u[i.value]));
             float acc[8];
-            static_for<8>([&](auto j) {
-                const float dj = oct_bcast<j.value>(ds), uj = oct_bcast<j.value>(us);
-                const StateBC<K> m = lds_bc<K>(row + (8 * i.value + j.value) * 2 * S);
-                float s = 0.f;
+            static_for<8 / AHEAD>([&](auto part) {
+                constexpr int j0 = part.value * AHEAD;
+                if constexpr (j0 > 0) static_for<AHEAD>([&](auto j) { m[j.value] = lds_bc<K>(row + (8 * i.value + j0 + j.value) * 2 * S); });
+                float dec[AHEAD][K];
+                static_for<AHEAD>([&](auto j) {
+                    const float dj = oct_bcast<j0 + j.value>(ds);
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    h[k] = fmaf(exp2_hw(dj * A2[k]), h[k], uj * m.b[k]);
-                    if (MODE == kSsmOutputs) s = k ? fmaf(m.c[k], h[k], s) : m.c[k] * h[k];
-                }
-                acc[j.value] = s;
+                    for (int k = 0; k < K; ++k) dec[j.value][k] = exp2_hw(dj * A2[k]);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+                static_for<AHEAD>([&](auto j) {
+                    const float uj = oct_bcast<j0 + j.value>(us);
+                    float s = 0.f;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        h[k] = fmaf(dec[j.value][k], h[k], uj * m[j.value].b[k]);
+                        if (MODE == kSsmOutputs) s = k ? fmaf(m[j.value].c[k], h[k], s) : m[j.value].c[k] * h[k];
+                    }
+                    acc[j0 + j.value] = s;
+                });
             });
             if (MODE == kSsmMaps) sum_delta += delta;
             if (MODE == kSsmOutputs) {
@@ -98,16 +125,17 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
                 if constexpr (HASZ) y[i.value] *= z[i.value] * sigmoid(z[i.value]);
             }
         });
-        if (MODE == kSsmOutputs && ch.mine) {
+        if (MODE == kSsmOutputs) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) if (8 * i + o < left) py.store(i, t, from_float<T>(y[i]));
+            for (int i = 0; i < 2; ++i) if (8 * i + o < left && ch.mine) py.store(i, from_float<T>(y[i]));
+            py.move(kTok);
         }
     };
-    if (g.t0 < g.t1) load(IntC<0>(), g.t0);
-    if (g.t0 + kTok < g.t1) load(IntC<1>(), g.t0 + kTok);
-    for (long t = g.t0; t < g.t1; t += 2 * kTok) {
-        tile(IntC<0>(), t);
-        if (t + kTok < g.t1) tile(IntC<1>(), t + kTok);
+    if (tokens > 0) load(IntC<0>(), 0);
+    if (tokens > kTok) load(IntC<1>(), kTok);
+    for (int at = 0; at < tokens; at += 2 * kTok) {
+        tile(IntC<0>(), at);
+        if (at + kTok < tokens) tile(IntC<1>(), at + kTok);
     }
     if (MODE == kSsmMaps) sum_delta = oct_sum(sum_delta);
     if (!ch.mine) return;

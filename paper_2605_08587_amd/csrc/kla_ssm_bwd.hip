@@ -57,38 +57,52 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
     const float skip = a.skip ? a.skip[c] : 0.f, bias = a.delta_bias ? a.delta_bias[c] : 0.f;
     float d_skip = 0.f, d_bias = 0.f, sum_delta = 0.f;
 
+    const int tokens = (int)(g.t1 - g.t0), tiles = (tokens + CK - 1) / CK;
+    const long t_last = g.t0 + (long)(tiles - 1) * CK;   // the last tile comes first
     TileBC<T, S, CK, THREADS> bc;
     Tokens<const T, NG> pu, pd, pz, py;
     Tokens<T, NG> qu, qd, qz;
-    bc.init(a, ch.g);
-    pu.init(a.u, a.ld_u, c, o);
-    pd.init(a.delta, a.ld_delta, c, o);
-    if constexpr (HASZ) pz.init(a.z, a.ld_z, c, o);
-    py.init(a.d_y, a.D, c, o);
+    bc.init(a, ch.g, t_last);
+    pu.init(a.u, t_last, (int)a.ld_u, c, o);
+    pd.init(a.delta, t_last, (int)a.ld_delta, c, o);
+    if constexpr (HASZ) pz.init(a.z, t_last, (int)a.ld_z, c, o);
+    py.init(a.d_y, t_last, a.D, c, o);
     if constexpr (!MAPS) {
-        qu.init(a.du, a.D, c, o);
-        qd.init(a.ddelta, a.D, c, o);
-        if constexpr (HASZ) qz.init(a.dz, a.D, c, o);
+        qu.init(a.du, t_last, a.D, c, o);
+        qd.init(a.ddelta, t_last, a.D, c, o);
+        if constexpr (HASZ) qz.init(a.dz, t_last, a.D, c, o);
     }
-    const long tiles = (g.t1 - g.t0 + CK - 1) / CK;
-    const float* saved = MAPS || tiles == 0 ? nullptr : a.saved + checkpoint_at(a, g.seq, g.t0, CK) * DS;
-    T in_u[NG], in_d[NG], in_z[NG], in_y[NG];
+    const float* saved = MAPS || tiles == 0 ? nullptr : a.saved + (checkpoint_at(a, g.seq, g.t0, CK) + tiles - 1) * DS;
+    float* out_bc = MAPS ? nullptr : a.part_bc + ((long)block * a.M + t_last) * (2 * S);
+    T in_bc[decltype(bc)::NE], in_u[NG], in_d[NG], in_z[NG], in_y[NG];
     float in_h[K];
-    auto load = [&](long tile) {
-        const long t = g.t0 + tile * CK;
-        bc.load(t, g.t1);
-        pu.load(in_u, t, g.t1);
-        pd.load(in_d, t, g.t1);
-        if constexpr (HASZ) pz.load(in_z, t, g.t1);
-        py.load(in_y, t, g.t1);
-        if constexpr (!MAPS) load_states<K>(in_h, saved + tile * DS + mine);
+    // the tile of which `left` tokens are the segment's, and the bases on to the one before it
+    auto load = [&](int left) {
+        auto rows = [&](auto full) {
+            constexpr bool FULL = full.value != 0;
+            bc.template load<FULL>(in_bc, left - 1);
+            pu.template load<FULL>(in_u, left - 1, o);
+            pd.template load<FULL>(in_d, left - 1, o);
+            if constexpr (HASZ) pz.template load<FULL>(in_z, left - 1, o);
+            py.template load<FULL>(in_y, left - 1, o);
+        };
+        if (left >= CK) rows(IntC<1>());
+        else rows(IntC<0>());
+        if constexpr (!MAPS) {
+            load_states<K>(in_h, saved + mine);
+            saved -= DS;
+        }
+        bc.move(-CK);
+        pu.move(-CK);
+        pd.move(-CK);
+        if constexpr (HASZ) pz.move(-CK);
+        py.move(-CK);
     };
-    if (tiles > 0) load(tiles - 1);
+    if (tiles > 0) load(tokens - (tiles - 1) * CK);
     int buf = 0;
-    for (long tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
-        const long t = g.t0 + tile * CK;
-        const int left = (int)min(g.t1 - t, (long)CK);
-        bc.store(lds[buf]);
+    for (int tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
+        const int left = min(tokens - tile * CK, CK);
+        bc.store(lds[buf], in_bc);
         float u[NG], raw[NG], z[NG], dy[NG], delta[NG], dc[NG], core[NG];
         float h[MAPS ? 1 : CK + 1][K];
 #pragma unroll
@@ -103,19 +117,19 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
             for (int k = 0; k < K; ++k) h[0][k] = in_h[k];
         }
         __syncthreads();
-        if (tile > 0) load(tile - 1);
+        if (tile > 0) load(CK);
         // a token beyond the segment decays nothing, adds nothing and has no gradient; nor has a lane without a channel of its own
         Oct ds[NG], us[NG], cs[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const bool live = 8 * i + o < left, own = live && ch.mine;
             const float soft = softplus(raw[i]);
-            delta[i] = live ? (a.softplus ? soft : raw[i]) : 0.f;
+            delta[i] = where(live, a.softplus ? soft : raw[i]);
             float gate = 1.f;
             if constexpr (HASZ) gate = z[i] * sigmoid(z[i]);
-            dc[i] = own ? dy[i] * gate : 0.f;
+            dc[i] = where(own, dy[i] * gate);
             ds[i] = oct_of(delta[i]);
-            us[i] = oct_of(own ? delta[i] * u[i] : 0.f);
+            us[i] = oct_of(where(own, delta[i] * u[i]));
             cs[i] = oct_of(dc[i]);
             if (MAPS) sum_delta += delta[i];
         }
@@ -199,24 +213,27 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
                 if (8 * i + o < left && ch.mine) {
                     d_bias += d_raw;
                     d_skip = fmaf(dc[i], u[i], d_skip);
-                    qu.store(i, t, from_float<T>(fmaf(delta[i], sb, skip * dc[i])));
-                    qd.store(i, t, from_float<T>(d_raw));
+                    qu.store(i, from_float<T>(fmaf(delta[i], sb, skip * dc[i])));
+                    qd.store(i, from_float<T>(d_raw));
                     if constexpr (HASZ) {
                         const float s = sigmoid(z[i]);
-                        qz.store(i, t, from_float<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f))));
+                        qz.store(i, from_float<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f))));
                     }
                 }
             });
             __syncthreads();
             // the waves' channels together: [token][2 S], C first
-            float* out = a.part_bc + ((long)block * a.M + t) * (2 * S);
             for (int e = threadIdx.x; e < left * 2 * S; e += THREADS) {
                 const float* r = &red[0][0][0] + e;
                 float s = 0.f;
 #pragma unroll
                 for (int w = 0; w < WAVES; ++w) s += r[w * CK * 2 * S];
-                out[e] = s;
+                out_bc[e] = s;
             }
+            out_bc -= CK * 2 * S;
+            qu.move(-CK);
+            qd.move(-CK);
+            if constexpr (HASZ) qz.move(-CK);
             // (red is written again behind the next tile's barrier)
         }
     }

@@ -110,61 +110,62 @@ template <typename T> __device__ __forceinline__ void store_at(T* base, unsigned
 {
     *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes) = x;
 }
-// A lane's tokens 8 i + o of a tile of one input [tokens][ld], raw: converted where they are loaded they would be waited for there.  In a tile
-// that the segment's end cuts the last row is repeated: nothing is read beyond it.
+// x where the token is one of the segment, else 0: on the bits, so that no branch and no NaN comes of it
+__device__ __forceinline__ float where(bool in, float x) { return __int_as_float(__float_as_int(x) & (in ? -1 : 0)); }
+
+// A lane's tokens 8 i + o of the tiles of one input or output [tokens][ld], raw: converted where they are loaded they would be waited for
+// there.  The base moves by a tile at a time (a wave alone on its SIMD pays for scalar instructions as for others).  In a tile that the
+// segment's end cuts the last row is repeated: nothing is read beyond it.
 template <typename T, int NG> struct Tokens {
-    T* p; long ld; unsigned off[NG]; int c, o;
-    __device__ __forceinline__ void init(T* base, long ld_, int c_, int o_)
+    T* p; int ld; unsigned off[NG];
+    __device__ __forceinline__ void init(T* base, long t, int ld_, int c, int o)
     {
-        p = base; ld = ld_; c = c_; o = o_;
+        ld = ld_;
+        p = base + t * ld;
 #pragma unroll
         for (int i = 0; i < NG; ++i) off[i] = (unsigned)((8 * i + o) * ld + c) * (unsigned)sizeof(T);
     }
-    __device__ __forceinline__ void load(std::remove_const_t<T> (&v)[NG], long t, long t1) const
+    __device__ __forceinline__ void move(int tokens) { p += (long)tokens * ld; }
+    template <bool FULL> __device__ __forceinline__ void load(std::remove_const_t<T> (&v)[NG], int last, int o) const
     {
-        T* b = p + t * ld;
-        if (t + 8 * NG <= t1) {
 #pragma unroll
-            for (int i = 0; i < NG; ++i) v[i] = load_at(b, off[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NG; ++i) v[i] = load_at(b, (unsigned)(min(8 * i + o, (int)(t1 - 1 - t)) * ld + c) * (unsigned)sizeof(T));
-        }
+        for (int i = 0; i < NG; ++i)
+            v[i] = load_at(p, FULL ? off[i] : off[i] - (unsigned)(max(8 * i + o - last, 0) * ld) * (unsigned)sizeof(T));
     }
-    __device__ __forceinline__ void store(int i, long t, T x) const { store_at(p + t * ld, off[i], x); }
+    __device__ __forceinline__ void store(int i, T x) const { store_at(p, off[i], x); }
 };
 
 // The rows of B and C of a tile of TOK tokens, in LDS as fp32: [token][o][B of the lane's K states, then C].  Every thread brings NE elements.
 template <typename T, int S, int TOK, int THREADS> struct TileBC {
     static constexpr int K = S / 8, ALL = 2 * TOK * S, NE = (ALL + THREADS - 1) / THREADS;
     static_assert(TOK * S % 64 == 0, "a wave's elements are of B or of C");
-    const T* p[NE]; long ld[NE]; unsigned off[NE]; int tok[NE], at[NE], n[NE];
-    T v[NE];
-    __device__ __forceinline__ void init(const SsmArgs<T>& a, int g)
+    const T* p[NE]; int ld[NE]; unsigned off[NE]; int tok[NE], at[NE];
+    __device__ __forceinline__ void init(const SsmArgs<T>& a, int g, long t)
     {
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
             const int e = (int)threadIdx.x + THREADS * i;
             const int m = __builtin_amdgcn_readfirstlane(e) / (TOK * S);         // 0: of B, 1: of C, 2: none
+            ld[i] = (int)(m == 1 ? a.ld_C : a.ld_B);
+            p[i] = (m == 1 ? a.C : a.B) + t * ld[i] + g * S;
             tok[i] = e / S % TOK;
-            n[i] = g * S + e % S;
-            p[i] = m == 1 ? a.C : a.B;
-            ld[i] = m == 1 ? a.ld_C : a.ld_B;
-            off[i] = (unsigned)(tok[i] * ld[i] + n[i]) * (unsigned)sizeof(T);
+            off[i] = (unsigned)(tok[i] * ld[i] + e % S) * (unsigned)sizeof(T);
             at[i] = m > 1 ? -1 : tok[i] * 2 * S + e % S / K * 2 * K + m * K + e % K;
         }
     }
-    __device__ __forceinline__ void load(long t, long t1)
+    __device__ __forceinline__ void move(int tokens)
     {
 #pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            const T* b = p[i] + t * ld[i];
-            // (rows beyond the segment repeat its last: their delta and u are taken for zero)
-            if (t + TOK <= t1) v[i] = load_at(b, off[i]);
-            else v[i] = load_at(b, (unsigned)(min(tok[i], (int)(t1 - 1 - t)) * ld[i] + n[i]) * (unsigned)sizeof(T));
-        }
+        for (int i = 0; i < NE; ++i) p[i] += (long)tokens * ld[i];
     }
-    __device__ __forceinline__ void store(float* lds) const
+    // (rows beyond the segment repeat its last: their delta and u are taken for zero)
+    template <bool FULL> __device__ __forceinline__ void load(T (&v)[NE], int last) const
+    {
+#pragma unroll
+        for (int i = 0; i < NE; ++i)
+            v[i] = load_at(p[i], FULL ? off[i] : off[i] - (unsigned)(max(tok[i] - last, 0) * ld[i]) * (unsigned)sizeof(T));
+    }
+    __device__ __forceinline__ void store(float* lds, const T (&v)[NE]) const
     {
 #pragma unroll
         for (int i = 0; i < NE; ++i) if (ALL % THREADS == 0 || at[i] >= 0) lds[at[i]] = to_float(v[i]);
