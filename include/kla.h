@@ -387,11 +387,10 @@ int kla_conv_step(const void *x, long ld_x, const float *weight, const float *bi
  *   y           [N, T, D] dt                                            out
  *   hT          [n_states, D, S] fp32                                   out  or NULL; may alias h0
  *   saved       kla_ssm_saved_bytes(...): the states at every 16th token (every 8th from S = 32 on), for the backward; or NULL
- * S in {8, 16, 32, 64}; D a multiple of G; D and the row strides at most 2^24; at most 65535 sequences.  The queries need only know whether the batch is packed and
- * of how many sequences.
+ * S in {8, 16, 32, 64}; D a multiple of G; D and the row strides at most 2^24; at most 65535 sequences.
  */
-size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, int n_seq);
-size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, int n_seq);
+size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq);
+size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq);
 int kla_ssm_fwd(const void *u, long ld_u, const void *delta, long ld_delta, const float *A,
                 const void *B, long ld_B, const void *C, long ld_C,
                 const float *skip, const void *z, long ld_z, const float *delta_bias, const float *h0,
@@ -403,7 +402,8 @@ int kla_ssm_fwd(const void *u, long ld_u, const void *delta, long ld_delta, cons
 /* Gradients of sum <d_y, y> + sum <d_hT, hT> (d_hT NULL: zeros) from the inputs of the forward; saved: what a forward with these
  * arguments left, or NULL (it is formed again, in the workspace).  du, ddelta, dz [N, T, D], dB, dC [N, T, G, S] contiguous; dz
  * needed iff z; dskip, ddelta_bias, dh0 NULL if unwanted. */
-size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, int n_seq, int has_saved);
+size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq,
+                                   int has_saved);
 int kla_ssm_bwd(const void *u, long ld_u, const void *delta, long ld_delta, const float *A,
                 const void *B, long ld_B, const void *C, long ld_C,
                 const float *skip, const void *z, long ld_z, const float *delta_bias, const float *h0,

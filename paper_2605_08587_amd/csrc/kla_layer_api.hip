@@ -84,17 +84,32 @@ template <typename T> kla::ConvArgs<T> conv_args(const void* x, long ld_x, const
 }
 
 // ---- selective scan ---------------------------------------------------------------------------------------------------------------
-// Tokens per segment.  A workgroup takes 64 channels of one segment and its tokens one after the other.
-int ssm_segment(long M, int n_states, int D, int G, int S)
+// (a lane's offset from the first of 16 rows fits 32 bits)
+constexpr int kMaxSsmRow = 1 << 24;
+bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
+// Tokens per segment.  A wave takes 8 channels of one segment and its tokens one after the other, about 70 ns each when it has its SIMD to
+// itself; segments cost a second pass over most of the tokens for their maps.  4096 waves run at twice the tokens per second of 1024, one
+// for each SIMD (forward and backward of 2048 tokens x 2048 channels: 189 us in segments, 520 us whole; two such sequences 323 and 532
+// us, three 523 and 543 us, four 618 and 573 us).  So batches of fewer than 768 waves are cut into segments until 4096 run; up to 255
+// tokens the additional launches cost more than they save.  In a packed batch the longest sequence decides: it would run on alone.
+int ssm_segment(long M, int n_states, int D, long longest)
 {
-    (void)M; (void)n_states; (void)D; (void)G; (void)S;
-    return INT_MAX / 64 * 64;
+    const int whole = INT_MAX / 64 * 64;
+    const long per = ((long)D + 7) / 8;                  // waves of one sequence
+    if (n_states == 0 || longest < 256 || M * per >= 768 * longest) return whole;
+    const long len = (M * per / 4096 + 63) / 64 * 64;
+    return (int)(len < 64 ? 64 : len < whole ? len : whole);
 }
 struct SsmPlan { int Lseg; long slots, checkpoints; int channels; };
-SsmPlan ssm_plan(const kla::Seqs& s, long M, int D, int G, int S)
+SsmPlan ssm_plan(const kla::Seqs& s, const int32_t* cu_host, long M, int D, int G, int S)
 {
     SsmPlan p;
-    p.Lseg = ssm_segment(M, s.n_seq, D, G, S);
+    long longest = s.T;
+    if (s.cu) {
+        longest = 0;
+        for (int i = 0; i < s.n_seq; ++i) if (cu_host[i + 1] - cu_host[i] > longest) longest = cu_host[i + 1] - cu_host[i];
+    }
+    p.Lseg = ssm_segment(M, s.n_seq, D, longest);
     p.channels = 64;
     const int ck = kla::ssm_checkpoint(S);
     if (s.cu) {
@@ -110,10 +125,13 @@ SsmPlan ssm_plan(const kla::Seqs& s, long M, int D, int G, int S)
     if (S == 64 || (long)G * ((D / G + 63) / 64) * p.slots < 256) p.channels = 32;
     return p;
 }
+// What the queries know: the sizes, and the offsets of a packed batch on the host
+int ssm_sizes(int N, int T, int D, int G, int S, const int32_t* cu_host, int n_seq, kla::Seqs* s, long* M)
+{
+    if (!ssm_shape_ok(D, G, S)) return KLA_ERR_SHAPE;
+    return take_seqs(n_seq > 0 ? cu_host : nullptr, cu_host, n_seq, N, T, s, M);
+}
 bool ssm_split(const kla::Seqs& s, const SsmPlan& p) { return p.slots > s.n_seq; }
-// (a lane's offset from the first of 16 rows fits 32 bits)
-constexpr int kMaxSsmRow = 1 << 24;
-bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
 size_t ssm_saved(const SsmPlan& p, int D, int S) { return round256((size_t)p.checkpoints * D * S * sizeof(float)); }
 struct SsmWork { float *seg_state, *seg_delta, *saved, *part_bc, *part_p; size_t bytes; };
 SsmWork ssm_work(char* base, const kla::Seqs& s, const SsmPlan& p, long M, int D, int G, int S, bool bwd, bool keeps)
@@ -266,28 +284,26 @@ int kla_conv_step(const void* x, long ld_x, const float* weight, const float* bi
     return dt == KLA_BF16 ? run(static_cast<const bf16_t*>(x)) : run(static_cast<const float*>(x));
 }
 
-size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, int n_seq)
+size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t* cu_seqlens_host, int n_seq)
 {
-    if (N < 0 || T < 0 || n_seq < 0 || (n_seq > 0 && N != 1) || !ssm_shape_ok(D, G, S)) return 0;
-    const int32_t some = 0;                              // (packed or not is all that is asked of the offsets here)
-    const kla::Seqs s = {n_seq > 0 ? &some : nullptr, n_seq > 0 ? n_seq : N, T};
-    const long M = (long)N * T;
-    return ssm_work(nullptr, s, ssm_plan(s, M, D, G, S), M, D, G, S, false, false).bytes;
+    kla::Seqs s;
+    long M;
+    if (ssm_sizes(N, T, D, G, S, cu_seqlens_host, n_seq, &s, &M)) return 0;
+    return ssm_work(nullptr, s, ssm_plan(s, cu_seqlens_host, M, D, G, S), M, D, G, S, false, false).bytes;
 }
-size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, int n_seq)
+size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, const int32_t* cu_seqlens_host, int n_seq)
 {
-    if (N < 0 || T < 0 || n_seq < 0 || (n_seq > 0 && N != 1) || !ssm_shape_ok(D, G, S)) return 0;
-    const int32_t some = 0;
-    const kla::Seqs s = {n_seq > 0 ? &some : nullptr, n_seq > 0 ? n_seq : N, T};
-    return ssm_saved(ssm_plan(s, (long)N * T, D, G, S), D, S);
+    kla::Seqs s;
+    long M;
+    if (ssm_sizes(N, T, D, G, S, cu_seqlens_host, n_seq, &s, &M)) return 0;
+    return ssm_saved(ssm_plan(s, cu_seqlens_host, M, D, G, S), D, S);
 }
-size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, int n_seq, int has_saved)
+size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t* cu_seqlens_host, int n_seq, int has_saved)
 {
-    if (N < 0 || T < 0 || n_seq < 0 || (n_seq > 0 && N != 1) || !ssm_shape_ok(D, G, S)) return 0;
-    const int32_t some = 0;
-    const kla::Seqs s = {n_seq > 0 ? &some : nullptr, n_seq > 0 ? n_seq : N, T};
-    const long M = (long)N * T;
-    return ssm_work(nullptr, s, ssm_plan(s, M, D, G, S), M, D, G, S, true, has_saved != 0).bytes;
+    kla::Seqs s;
+    long M;
+    if (ssm_sizes(N, T, D, G, S, cu_seqlens_host, n_seq, &s, &M)) return 0;
+    return ssm_work(nullptr, s, ssm_plan(s, cu_seqlens_host, M, D, G, S), M, D, G, S, true, has_saved != 0).bytes;
 }
 
 int kla_ssm_fwd(const void* u, long ld_u, const void* delta, long ld_delta, const float* A, const void* B, long ld_B, const void* C, long ld_C,
@@ -301,7 +317,7 @@ int kla_ssm_fwd(const void* u, long ld_u, const void* delta, long ld_delta, cons
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (M > 0 && (!u || !delta || !B || !C || !y)) return KLA_ERR_NULL;
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, y}) || !aligned(16, {A, h0, hT, saved}) || !aligned(4, {skip, delta_bias})) return KLA_ERR_ALIGN;
-    const SsmPlan p = ssm_plan(s, M, D, G, S);
+    const SsmPlan p = ssm_plan(s, cu_seqlens_host, M, D, G, S);
     if (saved && saved_bytes < ssm_saved(p, D, S)) return KLA_ERR_WORKSPACE;
     const SsmWork w = ssm_work(static_cast<char*>(workspace), s, p, M, D, G, S, false, false);
     if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;
@@ -328,7 +344,7 @@ int kla_ssm_bwd(const void* u, long ld_u, const void* delta, long ld_delta, cons
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, d_y, du, ddelta, dB, dC, dz}) || !aligned(16, {A, h0, d_hT, saved, dA, dh0}) ||
         !aligned(4, {skip, delta_bias, dskip, ddelta_bias}))
         return KLA_ERR_ALIGN;
-    const SsmPlan p = ssm_plan(s, M, D, G, S);
+    const SsmPlan p = ssm_plan(s, cu_seqlens_host, M, D, G, S);
     if (saved && saved_bytes < ssm_saved(p, D, S)) return KLA_ERR_WORKSPACE;
     const SsmWork w = ssm_work(static_cast<char*>(workspace), s, p, M, D, G, S, true, saved != nullptr);
     if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;

@@ -159,10 +159,22 @@ __global__ __launch_bounds__(256) void ssm_join_kernel(SsmArgs<T> a, int S)
     const float A2 = kLog2e * a.A[e];
     const int c = (int)(e / S);
     float h = a.h0 ? a.h0[p.n * DS + e] : 0.f;
-    for (long k = 0; k + 1 < n; ++k) {                   // (of the last segment there is no map)
-        const float own = a.seg_state[(base + k) * DS + e], d = a.seg_delta[(base + k) * a.D + c];
-        a.seg_state[(base + k) * DS + e] = h;
-        h = fmaf(exp2_hw(A2 * d), h, own);
+    constexpr int AHEAD = 8;                             // reads of so many segments at once
+    for (long k0 = 0; k0 + 1 < n; k0 += AHEAD) {         // (of the last segment there is no map)
+        float own[AHEAD], d[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const long k = min(k0 + i, n - 2);
+            own[i] = a.seg_state[(base + k) * DS + e];
+            d[i] = a.seg_delta[(base + k) * a.D + c];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (k0 + i + 1 < n) {
+                a.seg_state[(base + k0 + i) * DS + e] = h;
+                h = fmaf(exp2_hw(A2 * d[i]), h, own[i]);
+            }
+        }
     }
     a.seg_state[(base + max(n - 1, 0L)) * DS + e] = h;
 }

@@ -176,13 +176,13 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
                     for (int k = 0; k < K; ++k) {
                         const float gk = fmaf(cj, m.c[k], ag[k]);
                         const float d = KEEP ? dec[KEEP ? n : 0][k] : exp2_hw(dj * A2[k]);
-                        const float e = gk * (d * h[n][k]);
+                        ag[k] = d * gk;
+                        const float e = ag[k] * h[n][k];
                         val[k] = cj * h[n + 1][k];
                         val[K + k] = uj * gk;
                         sb = fmaf(gk, m.b[k], sb);
                         sa = fmaf(e, A2[k], sa);
                         dA[k] = fmaf(e, dj, dA[k]);
-                        ag[k] = d * gk;
                     }
                     via_a[j] = sa;
                     via_b[j] = sb;
@@ -267,10 +267,22 @@ __global__ __launch_bounds__(256) void ssm_join_bwd_kernel(SsmArgs<T> a, int S)
     const float A2 = kLog2e * a.A[e];
     const int c = (int)(e / S);
     float g = a.d_hT ? a.d_hT[p.n * DS + e] : 0.f;
-    for (long k = n - 1; k > 0; --k) {
-        const float own = a.seg_state[(base + k) * DS + e], d = a.seg_delta[(base + k) * a.D + c];
-        a.seg_state[(base + k) * DS + e] = g;
-        g = fmaf(exp2_hw(A2 * d), g, own);
+    constexpr int AHEAD = 8;                             // reads of so many segments at once
+    for (long k0 = n - 1; k0 > 0; k0 -= AHEAD) {
+        float own[AHEAD], d[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const long k = max(k0 - i, 1L);
+            own[i] = a.seg_state[(base + k) * DS + e];
+            d[i] = a.seg_delta[(base + k) * a.D + c];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (k0 - i > 0) {
+                a.seg_state[(base + k0 - i) * DS + e] = g;
+                g = fmaf(exp2_hw(A2 * d[i]), g, own[i]);
+            }
+        }
     }
     a.seg_state[base * DS + e] = g;
 }

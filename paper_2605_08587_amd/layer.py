@@ -23,9 +23,9 @@ SIGNATURES = {
     "kla_conv_bwd_workspace_bytes": (_z, [_i] * 4),
     "kla_conv_bwd": (_i, [_vp, _l, *[_vp] * 9, *_SEQS, *[_i] * 5, _vp, _z, _vp, _u]),
     "kla_conv_step": (_i, [_vp, _l, _vp, _vp, _vp, _vp, *[_i] * 4, _vp, _u]),
-    "kla_ssm_fwd_workspace_bytes": (_z, [_i] * 6),
-    "kla_ssm_saved_bytes": (_z, [_i] * 6),
-    "kla_ssm_bwd_workspace_bytes": (_z, [_i] * 7),
+    "kla_ssm_fwd_workspace_bytes": (_z, [*[_i] * 5, _vp, _i]),
+    "kla_ssm_saved_bytes": (_z, [*[_i] * 5, _vp, _i]),
+    "kla_ssm_bwd_workspace_bytes": (_z, [*[_i] * 5, _vp, _i, _i]),
     "kla_ssm_fwd": (_i, [*_SSM_IN, _vp, _vp, _vp, _vp, _z, *_SEQS, *[_i] * 6, _vp, _z, _vp, _u]),
     "kla_ssm_bwd": (_i, [*_SSM_IN, *[_vp] * 4, _z, *[_vp] * 9, *_SEQS, *[_i] * 6, _vp, _z, _vp, _u]),
     "kla_ssm_step": (_i, [*_SSM_IN, _vp, _vp, *[_i] * 5, _vp, _u]),
@@ -250,7 +250,7 @@ def kla_ssm_fwd(u, delta, A, B, C, skip=None, z=None, delta_bias=None, softplus=
     _on_gpu(h0, cu_seqlens, out, hT, workspace)
     _dev(h0, cu_seqlens, out, hT, workspace)
     if workspace is None:
-        workspace = _workspace(int(lib().kla_ssm_fwd_workspace_bytes(N, T, D, G, S, n_seq)), u)
+        workspace = _workspace(int(lib().kla_ssm_fwd_workspace_bytes(N, T, D, G, S, cu_hp, n_seq)), u)
     if out is None:
         out = torch.empty((N, T, D), dtype=u.dtype, device=u.device)
     if hT is None and want_hT:
@@ -276,7 +276,7 @@ def kla_ssm_bwd(u, delta, A, B, C, d_y, skip=None, z=None, delta_bias=None, soft
     _on_gpu(h0, cu_seqlens, d_y, d_hT, workspace, _saved)
     _dev(h0, cu_seqlens, d_y, d_hT, workspace, _saved)
     if workspace is None:
-        workspace = _workspace(int(lib().kla_ssm_bwd_workspace_bytes(N, T, D, G, S, n_seq, _saved is not None)), u)
+        workspace = _workspace(int(lib().kla_ssm_bwd_workspace_bytes(N, T, D, G, S, cu_hp, n_seq, _saved is not None)), u)
 
     def new(t, wanted=True):
         return torch.empty(t.shape, dtype=t.dtype, device=t.device) if t is not None and wanted else None
@@ -309,7 +309,8 @@ class _Ssm(torch.autograd.Function):
         ctx.offsets = _Offsets(cu_seqlens, cu_seqlens_host)
         saved = None
         if save and any(ctx.needs_input_grad) and u.is_cuda and u.dim() == 3 and B.dim() == 4 and max(u.shape) < 2 ** 31:
-            keep = int(lib().kla_ssm_saved_bytes(*u.shape, *B.shape[-2:], 0 if cu_seqlens is None else cu_seqlens.numel() - 1))
+            _, cu_hp, n_seq = _host_cu(ctx.offsets.cu, ctx.offsets.host)
+            keep = int(lib().kla_ssm_saved_bytes(*u.shape, *B.shape[-2:], cu_hp, n_seq))
             try:
                 saved = _workspace(keep, u)
             except torch.OutOfMemoryError:               # the backward forms them again

@@ -137,16 +137,24 @@ def test_queries():
     for bad in ((-1, 1, 8, 4), (1, 1, 0, 4), (1, 1, 8, 5), (1, 1, 8, 1)):
         assert lib.kla_conv_bwd_workspace_bytes(*bad) == 0
     # one checkpoint of [D, S] fp32 per 16 tokens (8 from S = 32 on)
-    assert lib.kla_ssm_saved_bytes(2, 64, 128, 1, 32, 0) == 2 * 8 * 128 * 32 * 4
-    assert lib.kla_ssm_saved_bytes(2, 64, 128, 1, 16, 0) == 2 * 4 * 128 * 16 * 4
-    assert lib.kla_ssm_saved_bytes(2, 65, 128, 1, 16, 0) == 2 * 5 * 128 * 16 * 4
-    assert lib.kla_ssm_saved_bytes(1, 100, 128, 1, 16, 3) >= (100 // 16 + 3) * 128 * 16 * 4
+    assert lib.kla_ssm_saved_bytes(2, 64, 128, 1, 32, None, 0) == 2 * 8 * 128 * 32 * 4
+    assert lib.kla_ssm_saved_bytes(2, 64, 128, 1, 16, None, 0) == 2 * 4 * 128 * 16 * 4
+    assert lib.kla_ssm_saved_bytes(2, 65, 128, 1, 16, None, 0) == 2 * 5 * 128 * 16 * 4
+    cu = np.array([0, 30, 30, 100], dtype=np.int32).ctypes
+    assert lib.kla_ssm_saved_bytes(1, 100, 128, 1, 16, cu.data, 3) >= (2 + 5) * 128 * 16 * 4
     assert ssm_fwd(saved=0x10000, saved_bytes=4 * 64 * 16 * 4 - 4) == E_WS and ssm_bwd(saved=0x10000, saved_bytes=100) == E_WS
-    for q in (lib.kla_ssm_saved_bytes, lib.kla_ssm_fwd_workspace_bytes):
-        for bad in ((-1, 1, 64, 1, 16, 0), (1, 1, 64, 1, 15, 0), (1, 1, 64, 3, 16, 0), (2, 1, 64, 1, 16, 1)):
-            assert q(*bad) == 0
-    assert lib.kla_ssm_bwd_workspace_bytes(1, 64, 64, 1, 16, 0, 0) - lib.kla_ssm_bwd_workspace_bytes(1, 64, 64, 1, 16, 0, 1) == \
-        lib.kla_ssm_saved_bytes(1, 64, 64, 1, 16, 0)
+    wrong = np.array([0, 30, 99], dtype=np.int32).ctypes
+    for q, more in ((lib.kla_ssm_saved_bytes, ()), (lib.kla_ssm_fwd_workspace_bytes, ()), (lib.kla_ssm_bwd_workspace_bytes, (1,))):
+        for bad in ((-1, 1, 64, 1, 16, None, 0), (1, 1, 64, 1, 15, None, 0), (1, 1, 64, 3, 16, None, 0), (2, 100, 64, 1, 16, cu.data, 3),
+                    (1, 100, 64, 1, 16, None, 3), (1, 100, 64, 1, 16, wrong.data, 2)):
+            assert q(*bad, *more) == 0
+    assert lib.kla_ssm_bwd_workspace_bytes(1, 64, 64, 1, 16, None, 0, 0) - lib.kla_ssm_bwd_workspace_bytes(1, 64, 64, 1, 16, None, 0, 1) == \
+        lib.kla_ssm_saved_bytes(1, 64, 64, 1, 16, None, 0)
+    # few channels and many tokens are taken in segments, with states for each of them; so are a packed batch's where one is long
+    f = lib.kla_ssm_fwd_workspace_bytes
+    assert f(1, 255, 2048, 1, 16, None, 0) == 0 and f(1, 4096, 2048, 1, 16, None, 0) > 8 * 2048 * 16 * 4 and f(8, 4096, 2048, 1, 16, None, 0) == 0
+    even, odd = np.arange(0, 4097, 512, dtype=np.int32), np.array([0, 10, 20, 30, 40, 50, 60, 70, 4096], dtype=np.int32)
+    assert f(1, 4096, 2048, 1, 16, even.ctypes.data, 8) == 0 and f(1, 4096, 2048, 1, 16, odd.ctypes.data, 8) > 0
     assert lib.kla_add_norm_bwd_workspace_bytes(8, 64, BF16) > 0 and lib.kla_add_norm_bwd_workspace_bytes(8, 8193, BF16) == 0
     assert lib.kla_gated_norm_bwd_workspace_bytes(8, 2, 64, BF16) > 0 and lib.kla_gated_norm_bwd_workspace_bytes(8, 0, 64, BF16) == 0
     assert lib.kla_add_norm_bwd_workspace_bytes(0, 64, BF16) == 0
