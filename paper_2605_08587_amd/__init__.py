@@ -5,7 +5,7 @@ device memory and the current stream.  There is no CPU fallback: if the compiled
 missing, or a tensor is not on the GPU, the call raises.
 
 Calls with plain GPU tensors that fit each other are checked, given memory and launched by kla_binding.so
-(csrc/kla_binding.cpp), which hands back None for anything else; the code here then takes the same call step by step and
+(csrc/kla_binding.cpp, csrc/kla_layer_binding.cpp), which hands back None for anything else; the code here then takes the same call step by step and
 raises what there is to raise.  kla_binding.so is built against one PyTorch; without it, or with another one, every call goes
 step by step.
 """
@@ -112,6 +112,7 @@ def _load_native(l):
         "kla_chunk_fwd_diag_workspace_bytes", "kla_chunk_fwd_diag_opts", "kla_chunk_bwd_workspace_bytes_opts",
         "kla_chunk_bwd_opts", "kla_chunk_saved_bytes", "kla_chunk_fwd_save", "kla_chunk_bwd_saved_workspace_bytes",
         "kla_chunk_bwd_saved")), _bwd_by_steps)
+    m.bind_layer(*(ctypes.cast(getattr(l, n), ctypes.c_void_p).value for n in layer.NATIVE))
     return m
 
 

@@ -16,6 +16,7 @@ BINDING = os.path.join(HERE, "kla_binding.so")
 SOURCES = ["kla_api.hip", "kla_decode.hip", "kla_chunk_intra.hip", "kla_chunk_intra_bf16.hip", "kla_chunk_intra_f32.hip", "kla_chunk_scan.hip", "kla_chunk_sweeps_f32.hip",
            "kla_chunk_scan_bf16.hip", "kla_chunk_rows_bf16.hip", "kla_chunk_segments.hip", "kla_chunk_bwd.hip", "kla_chunk_bwd_bf16.hip", "kla_chunk_rev_bf16.hip", "kla_probe.hip",
            "kla_layer_api.hip", "kla_layer_sums.hip", "kla_conv.hip", "kla_norm.hip", "kla_ssm.hip", "kla_ssm_bwd.hip"]
+BINDING_SOURCES = ["kla_binding.cpp", "kla_layer_binding.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # hipcc -O3 must not form packed-fp32 instructions on the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -51,20 +52,32 @@ def build_lib(verbose: bool = False, extra=(), jobs: int = 8) -> str:
 
 
 def build_binding(verbose: bool = False) -> str:
-    """Compiles csrc/kla_binding.cpp (host code only) against the installed PyTorch."""
+    """Compiles csrc/kla_binding.cpp and csrc/kla_layer_binding.cpp (host code only) against the installed PyTorch."""
     import sysconfig
+    import tempfile
+    from concurrent.futures import ThreadPoolExecutor
     import torch
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     root = os.path.dirname(torch.__file__)
     tmp = BINDING + ".tmp.%d" % os.getpid()
-    cmd = [hipcc, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__=1",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
-           "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
-           "-I/opt/rocm/include", "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "kla_binding.cpp"), "-o", tmp,
-           "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    flags = ["-O2", "-std=c++17", "-fPIC", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__=1",
+             "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+             "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
+             "-I/opt/rocm/include", "-I" + sysconfig.get_paths()["include"]]
+    with tempfile.TemporaryDirectory(prefix="kla_build_") as tmpdir:
+        def compile_one(src):
+            obj = os.path.join(tmpdir, src + ".o")
+            cmd = [hipcc, "-x", "c++", *flags, "-c", os.path.join(CSRC, src), "-o", obj]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            subprocess.check_call(cmd)
+            return obj
+        with ThreadPoolExecutor() as pool:
+            objs = list(pool.map(compile_one, BINDING_SOURCES))
+        cmd = [hipcc, "-shared", "-fPIC", "-o", tmp, *objs, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd)
     os.replace(tmp, BINDING)
     return BINDING
 

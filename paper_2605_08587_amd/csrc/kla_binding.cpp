@@ -6,24 +6,11 @@
 // tensors, subclasses): the Python code then goes through the same call step by step and raises what there is to raise.
 // A refusal by the library itself comes back as its status code (an int).  The functions are called through the addresses
 // that bind() was given, so that they are those of the library the package has loaded.
-#include <Python.h>
-
-#include <pybind11/pybind11.h>
-
-#include <ATen/ATen.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/python_variable.h>
-#include <torch/version.h>
-
-#include <climits>
-#include <initializer_list>
-#include <optional>
-
-#include "../../include/kla.h"
+#include "kla_binding.hpp"
 
 namespace {
+
+using namespace kla_binding;
 
 struct Api {
     decltype(&kla_decode_step_opts) decode;
@@ -40,88 +27,6 @@ struct Api {
     decltype(&kla_chunk_bwd_saved) bwd_saved;
     PyObject* bwd_by_steps;                              // the Python module's function for a backward that is not taken here
 } api = {};
-
-// A plain, dense tensor: torch.Tensor or Parameter itself, strided and contiguous, with memory of its own.  (What
-// function transforms and fake modes pass around is not.)
-const at::Tensor* dense(const at::Tensor& t)
-{
-    if (!t.defined() || t.layout() != at::kStrided) return nullptr;
-    const c10::TensorImpl* impl = t.unsafeGetTensorImpl();
-    const c10::DispatchKeySet ks = impl->key_set();
-    if (!impl->has_storage() || impl->is_python_dispatch() || ks.has(c10::DispatchKey::FuncTorchBatched) ||
-        ks.has(c10::DispatchKey::FuncTorchGradWrapper) || ks.has(c10::DispatchKey::Functionalize))
-        return nullptr;
-    return t.is_contiguous() ? &t : nullptr;
-}
-const at::Tensor* dense(PyObject* o) { return THPVariable_CheckExact(o) ? dense(THPVariable_Unpack(o)) : nullptr; }
-template <typename O> const at::Tensor* on_gpu(const O& o)
-{
-    const at::Tensor* t = dense(o);
-    return t && t->is_cuda() ? t : nullptr;
-}
-// GPU tensor of this element type and these extents
-template <typename O> const at::Tensor* gpu(const O& o, at::ScalarType type, at::IntArrayRef shape)
-{
-    const at::Tensor* t = on_gpu(o);
-    return t && t->scalar_type() == type && t->sizes() == shape ? t : nullptr;
-}
-bool is_none(PyObject* o) { return o == Py_None; }
-bool is_none(const at::Tensor& t) { return !t.defined(); }
-// the same, or None (then *t stays null); false: neither
-template <typename O> bool gpu_or_none(const O& o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor** t)
-{
-    *t = nullptr;
-    if (is_none(o)) return true;
-    *t = gpu(o, type, shape);
-    return *t != nullptr;
-}
-// What a forward left behind for the backward of q: bytes on q's device, or none (then *t stays null); false: something else.
-// (It comes back through the caller's hands, a hook on saved tensors, and goes to the kernels as a bare pointer.)
-template <typename O> bool saved_or_none(const O& o, const at::Tensor& q, const at::Tensor** t)
-{
-    *t = nullptr;
-    if (is_none(o)) return true;
-    *t = on_gpu(o);
-    return *t && (*t)->scalar_type() == at::kByte && (*t)->device() == q.device();
-}
-void* ptr(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
-float* fptr(const at::Tensor* t) { return static_cast<float*>(ptr(t)); }
-
-bool type_of(const at::Tensor& q, kla_dtype* dt)
-{
-    if (q.scalar_type() == at::kBFloat16) *dt = KLA_BF16;
-    else if (q.scalar_type() == at::kFloat) *dt = KLA_F32;
-    else return false;
-    return true;
-}
-bool number(PyObject* o, double* x)
-{
-    *x = PyFloat_AsDouble(o);
-    if (*x == -1.0 && PyErr_Occurred()) { PyErr_Clear(); return false; }
-    return true;
-}
-bool integer(PyObject* o, long lo, long hi, long* x)
-{
-    *x = PyLong_AsLong(o);
-    if (*x == -1 && PyErr_Occurred()) { PyErr_Clear(); return false; }
-    return *x >= lo && *x <= hi;
-}
-bool ints(std::initializer_list<int64_t> xs)
-{
-    for (const int64_t x : xs) if (x > INT_MAX) return false;
-    return true;
-}
-void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
-// Other threads run while a call allocates and launches (and get their turn back if it throws).
-struct NoGil {
-    PyThreadState* state = PyEval_SaveThread();
-    ~NoGil() { PyEval_RestoreThread(state); }
-};
-PyObject* wrap(const std::optional<at::Tensor>& t)
-{
-    if (t) return THPVariable_Wrap(*t);
-    Py_RETURN_NONE;
-}
 
 // What the chunk entry points share.
 struct Chunk {
@@ -454,7 +359,6 @@ PyObject* train(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-#define KLA_FASTCALL(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KLA_FASTCALL(bind), KLA_FASTCALL(decode), KLA_FASTCALL(chunk_fwd), KLA_FASTCALL(chunk_bwd),
                          KLA_FASTCALL(train), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "kla_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -464,6 +368,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "kla_binding", nullptr, -1, methods
 PyMODINIT_FUNC PyInit_kla_binding()
 {
     PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, layer_methods) < 0) Py_CLEAR(m);
     if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);   // whose tensors it can read
     return m;
 }

@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from . import KlaError, _check, _dev, _dt, _host_cu, _ptr, _stream, _ws_bytes, lib
+from . import KlaError, _binding, _check, _dev, _dt, _host_cu, _ptr, _stream, _ws_bytes, lib
 
 KLA_LAYER_SILU, KLA_LAYER_SOFTPLUS, KLA_LAYER_SIGMOID, KLA_LAYER_GATE_FIRST = 1, 2, 4, 8
 
@@ -36,6 +36,33 @@ SIGNATURES = {
     "kla_gated_norm_bwd_workspace_bytes": (_z, [_l, _i, _i, _i]),
     "kla_gated_norm_bwd": (_i, [_vp, _l, _vp, _l, _vp, _f, *[_vp] * 4, _l, _i, _i, _i, _vp, _z, _vp, _u]),
 }
+# what kla_binding.so calls, in the order of its bind_layer
+NATIVE = ("kla_conv_fwd", "kla_conv_bwd_workspace_bytes", "kla_conv_bwd", "kla_conv_step", "kla_ssm_fwd_workspace_bytes", "kla_ssm_saved_bytes",
+          "kla_ssm_fwd", "kla_ssm_bwd_workspace_bytes", "kla_ssm_bwd", "kla_ssm_step", "kla_add_norm_fwd", "kla_add_norm_bwd_workspace_bytes",
+          "kla_add_norm_bwd", "kla_gated_norm_fwd", "kla_gated_norm_bwd_workspace_bytes", "kla_gated_norm_bwd")
+
+
+def _native(entry, name, *args):
+    """The call through the native half of the binding, or None if it does not take it."""
+    f = getattr(_binding(), entry, None)
+    r = None if f is None else f(*args)
+    if type(r) is int:
+        raise KlaError(r, name)
+    return r
+
+
+def _host(cu_seqlens, cu_seqlens_host):
+    return _host_cu(cu_seqlens)[0] if cu_seqlens is not None and cu_seqlens_host is None else cu_seqlens_host
+
+
+def _eager():
+    """Tracing, function transforms and forward-mode differentiation are for the Python functions to take or to refuse."""
+    return torch._C._get_tracing_state() is None and not torch._C._are_functorch_transforms_active() and torch.autograd.forward_ad._current_level < 0
+
+
+def _no_second(name):
+    if torch.is_grad_enabled():
+        raise RuntimeError("%s: the gradients have no gradients of their own (create_graph)" % name)
 
 
 def _rows(name, t, inner=1):
@@ -136,7 +163,11 @@ def kla_conv_fwd(x, weight, bias=None, state=None, cu_seqlens=None, cu_seqlens_h
     """Short causal convolution of every channel of x [N,T,D] (weight [D,W] fp32, W = 2..4, bias [D] fp32) with SiLU; returns
     (y, state_out): state_out [n_states,W-1,D] are the last W-1 inputs of every sequence (None unless want_state), what `state` of
     the call for the tokens that follow takes.  Packed batches by cu_seqlens as in kla_chunk_fwd."""
-    N, T, D, W, dt, st, (_, cu_hp, n_seq, _n) = _conv_check(x, weight, bias, state, cu_seqlens, cu_seqlens_host, out=(out, "y", None),
+    host = _host(cu_seqlens, cu_seqlens_host)
+    r = _native("conv_fwd", "kla_conv_fwd", x, weight, bias, state, cu_seqlens, host, bool(silu), bool(want_state), out, state_out)
+    if r is not None:
+        return r
+    N, T, D, W, dt, st, (_, cu_hp, n_seq, _n) = _conv_check(x, weight, bias, state, cu_seqlens, host, out=(out, "y", None),
                                                          state_out=(state_out, "state", None))
     ld = _rows("x", x)
     if out is None:
@@ -168,6 +199,9 @@ def kla_conv_bwd(x, weight, d_y, bias=None, state=None, d_state_out=None, cu_seq
 
 def kla_conv_step(x, weight, state, bias=None, silu=True, out=None):
     """One token of B sequences: x [B,D]; state [B,W-1,D] is updated in place; returns y [B,D]."""
+    r = _native("conv_step", "kla_conv_step", x, weight, state, bias, bool(silu), out)
+    if r is not None:
+        return r
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x must be [B, D] and weight [D, W]")
     (B, D), W, dt = x.shape, weight.shape[1], _dt(x)
@@ -197,6 +231,7 @@ class _Conv(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d_y, d_last):
+        _no_second("kla_conv")
         x, weight, bias, state = ctx.saved_tensors
         d_y = x.new_zeros(x.shape) if d_y is None else d_y.contiguous()
         g = kla_conv_bwd(x, weight, d_y, bias, state, None if d_last is None else d_last.contiguous(), silu=ctx.silu,
@@ -206,7 +241,12 @@ class _Conv(torch.autograd.Function):
 
 def kla_conv(x, weight, bias=None, state=None, cu_seqlens=None, cu_seqlens_host=None, silu=True, want_state=False):
     """Differentiable kla_conv_fwd: (y, state_out), gradients with respect to x, weight, bias and state."""
-    return _Conv.apply(x, weight, bias, state, cu_seqlens, cu_seqlens_host, bool(silu), bool(want_state))
+    host = _host(cu_seqlens, cu_seqlens_host)
+    if _eager():
+        r = _native("conv_train", "kla_conv_fwd", x, weight, bias, state, cu_seqlens, host, bool(silu), bool(want_state))
+        if r is not None:
+            return r
+    return _Conv.apply(x, weight, bias, state, cu_seqlens, host, bool(silu), bool(want_state))
 
 
 # ---- selective scan ------------------------------------------------------------------------------------------------------------------
@@ -241,9 +281,14 @@ def kla_ssm_fwd(u, delta, A, B, C, skip=None, z=None, delta_bias=None, softplus=
     """Selective state space scan of u [N,T,D] with steps softplus(delta + delta_bias), decay rates A [D,S] (fp32), input and output maps
     B, C [N,T,G,S] (G groups of D/G channels), skip [D] and gate z [N,T,D]; returns (y, hT), hT [n_states,D,S] fp32 the states after the
     last tokens, which h0 of the call for the tokens that follow takes.  Packed batches by cu_seqlens as in kla_chunk_fwd."""
+    host = _host(cu_seqlens, cu_seqlens_host)
+    if workspace is None and _saved is None:
+        r = _native("ssm_fwd", "kla_ssm_fwd", u, delta, A, B, C, skip, z, delta_bias, bool(softplus), h0, cu_seqlens, host, bool(want_hT), out, hT)
+        if r is not None:
+            return r
     D, G, S, dt, ld = _ssm_check(u, delta, A, B, C, skip, z, delta_bias, 2)
     N, T = u.shape[:2]
-    _, cu_hp, n_seq, n_states = _batch(u, cu_seqlens, cu_seqlens_host)
+    _, cu_hp, n_seq, n_states = _batch(u, cu_seqlens, host)
     _check("h0", h0, (n_states, D, S), torch.float32)
     _check("out", out, (N, T, D), u.dtype)
     _check("hT", hT, (n_states, D, S), torch.float32)
@@ -290,6 +335,9 @@ def kla_ssm_bwd(u, delta, A, B, C, d_y, skip=None, z=None, delta_bias=None, soft
 
 def kla_ssm_step(u, delta, A, B, C, h, skip=None, z=None, delta_bias=None, softplus=True, out=None):
     """One token of N sequences: u, delta, z [N,D], B, C [N,G,S]; h [N,D,S] fp32 is updated in place; returns y [N,D]."""
+    r = _native("ssm_step", "kla_ssm_step", u, delta, A, B, C, h, skip, z, delta_bias, bool(softplus), out)
+    if r is not None:
+        return r
     D, G, S, dt, ld = _ssm_check(u, delta, A, B, C, skip, z, delta_bias, 1)
     N = u.shape[0]
     _check("h", h, (N, D, S), torch.float32)
@@ -323,6 +371,7 @@ class _Ssm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d_y, d_hT):
+        _no_second("kla_ssm")
         u, delta, A, B, C, skip, z, delta_bias, h0, saved = ctx.saved_tensors
         d_y = u.new_zeros(u.shape) if d_y is None else d_y.contiguous()
         g = kla_ssm_bwd(u, delta, A, B, C, d_y, skip, z, delta_bias, ctx.softplus, h0, None if d_hT is None else d_hT.contiguous(),
@@ -334,7 +383,12 @@ def kla_ssm(u, delta, A, B, C, skip=None, z=None, delta_bias=None, softplus=True
     """Differentiable kla_ssm_fwd: (y, hT), gradients with respect to every tensor argument.  Where a gradient is wanted the forward leaves
     the states at every 16th token (every 8th from S = 32 on) behind for the backward, 4 bytes per token and channel at S = 16; save=False: the
     backward forms them again.  Same results either way."""
-    return _Ssm.apply(u, delta, A, B, C, skip, z, delta_bias, h0, bool(softplus), cu_seqlens, cu_seqlens_host,
+    host = _host(cu_seqlens, cu_seqlens_host)
+    if _eager():
+        r = _native("ssm_train", "kla_ssm_fwd", u, delta, A, B, C, skip, z, delta_bias, bool(softplus), h0, cu_seqlens, host, bool(save))
+        if r is not None:
+            return r
+    return _Ssm.apply(u, delta, A, B, C, skip, z, delta_bias, h0, bool(softplus), cu_seqlens, host,
                       bool(save) and torch.is_grad_enabled())
 
 
@@ -362,6 +416,10 @@ def _add_norm_check(x, weight, residual, scale, residual_dtype, **more):
 def kla_add_norm_fwd(x, weight, residual=None, scale=None, eps=1e-6, residual_dtype=None, out=None, residual_out=None):
     """r' = residual + scale x and y = weight * (RMS norm of r'), over the last dimension of x [...,D]; returns (y, r').  residual and r'
     are fp32 or of the type of x (residual_dtype where there is no residual yet: then r' = scale x)."""
+    if residual_dtype in (None, torch.float32):
+        r = _native("add_norm_fwd", "kla_add_norm_fwd", x, weight, residual, scale, eps, residual_dtype is not None, out, residual_out)
+        if r is not None:
+            return r
     D, dt, res_dt, res_type = _add_norm_check(x, weight, residual, scale, residual_dtype, out=(out, None), residual_out=(residual_out, "r"))
     ld = _rows("x", x)
     if out is None:
@@ -398,6 +456,7 @@ class _AddNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d_y, d_r):
+        _no_second("kla_add_norm")
         x, weight, residual, scale = ctx.saved_tensors
         eps, res_type = ctx.misc
         d_y = x.new_zeros(x.shape) if d_y is None else d_y.contiguous()
@@ -407,14 +466,23 @@ class _AddNorm(torch.autograd.Function):
 
 def kla_add_norm(x, weight, residual=None, scale=None, eps=1e-6, residual_dtype=None):
     """Differentiable kla_add_norm_fwd: (y, r'), gradients with respect to x, weight, residual and scale."""
+    if residual_dtype in (None, torch.float32) and _eager():
+        r = _native("add_norm_train", "kla_add_norm_fwd", x, weight, residual, scale, eps, residual_dtype is not None)
+        if r is not None:
+            return r
     return _AddNorm.apply(x, weight, residual, scale, float(eps), residual_dtype)
+
+
+def _gate_bits(activation, gate_first):
+    if activation not in ("silu", "sigmoid"):
+        raise ValueError("activation must be silu or sigmoid, got %r" % (activation,))
+    return (KLA_LAYER_SIGMOID if activation == "sigmoid" else 0) | (KLA_LAYER_GATE_FIRST if gate_first else 0)
 
 
 def _gated_norm_check(x, gate, weight, activation, gate_first, **more):
     if x.dim() < 2:
         raise ValueError("x, gate must be [..., H, D]")
-    if activation not in ("silu", "sigmoid"):
-        raise ValueError("activation must be silu or sigmoid, got %r" % (activation,))
+    bits = _gate_bits(activation, gate_first)
     H, D = x.shape[-2:]
     dt = _dt(x)
     _check("gate", gate, x.shape, x.dtype)
@@ -424,13 +492,16 @@ def _gated_norm_check(x, gate, weight, activation, gate_first, **more):
     _sizes(H, D)
     _on_gpu(x, gate, weight, *more.values())
     _dev(weight, *more.values())
-    bits = (KLA_LAYER_SIGMOID if activation == "sigmoid" else 0) | (KLA_LAYER_GATE_FIRST if gate_first else 0)
     return H, D, x.numel() // (H * D) if H * D else 0, dt, _rows("x", x, 2), _rows("gate", gate, 2), bits
 
 
 def kla_gated_norm_fwd(x, gate, weight, eps=1e-6, activation="silu", gate_first=False, out=None):
     """weight * (RMS norm of x over the last dimension) * act(gate) for x, gate [...,H,D], weight [D] fp32, act "silu" or "sigmoid";
     gate_first: weight * (RMS norm of x act(gate))."""
+    bits = _gate_bits(activation, gate_first)
+    r = _native("gated_norm_fwd", "kla_gated_norm_fwd", x, gate, weight, eps, bits, out)
+    if r is not None:
+        return r
     H, D, M, dt, ld_x, ld_gate, bits = _gated_norm_check(x, gate, weight, activation, gate_first, out=out)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -461,10 +532,15 @@ class _GatedNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d_y):
+        _no_second("kla_gated_norm")
         g = kla_gated_norm_bwd(*ctx.saved_tensors, d_y.contiguous(), *ctx.misc)
         return g["dx"], g["dgate"], g["dweight"], None, None, None
 
 
 def kla_gated_norm(x, gate, weight, eps=1e-6, activation="silu", gate_first=False):
     """Differentiable kla_gated_norm_fwd: gradients with respect to x, gate and weight."""
+    if _eager():
+        r = _native("gated_norm_train", "kla_gated_norm_fwd", x, gate, weight, eps, _gate_bits(activation, gate_first))
+        if r is not None:
+            return r
     return _GatedNorm.apply(x, gate, weight, float(eps), activation, bool(gate_first))
