@@ -36,38 +36,19 @@ __device__ __forceinline__ float softplus(float x)
     return fmaf(2.f * s, p, fmaxf(x, 0.f));
 }
 
-// V consecutive elements <-> fp32 registers; V * sizeof(T) is 16 or 8 bytes, aligned so, or V = 1.
+// V consecutive elements, as they are (a load is waited for where it is converted) and as fp32 registers; V * sizeof(T) is 16 or 8 bytes,
+// aligned so, or V = 1.
 template <int V> struct Floats { float v[V]; };
-template <typename T, int V> __device__ __forceinline__ Floats<V> load_vec(const T* p)
+template <typename T, int V> struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Raw { T v[V]; };
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p) { return *reinterpret_cast<const Raw<T, V>*>(p); }
+template <typename T, int V> __device__ __forceinline__ Floats<V> floats_of(const Raw<T, V>& x)
 {
     Floats<V> r;
-    if constexpr (V == 1) {
-        r.v[0] = to_float(*p);
-    } else if constexpr (sizeof(T) == 4) {
-        static_assert(V % 4 == 0, "whole float4");
 #pragma unroll
-        for (int i = 0; i < V / 4; ++i) {
-            const float4 f = reinterpret_cast<const float4*>(p)[i];
-            r.v[4 * i] = f.x; r.v[4 * i + 1] = f.y; r.v[4 * i + 2] = f.z; r.v[4 * i + 3] = f.w;
-        }
-    } else {
-        static_assert(V == 4 || V == 8, "8 or 16 bytes");
-        uint32_t w[V / 2];
-        if constexpr (V == 8) {
-            const uint4 u = *reinterpret_cast<const uint4*>(p);
-            w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-        } else {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
-            w[0] = u.x; w[1] = u.y;
-        }
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            r.v[2 * i] = __uint_as_float(w[i] << 16);
-            r.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
+    for (int i = 0; i < V; ++i) r.v[i] = to_float(x.v[i]);
     return r;
 }
+template <typename T, int V> __device__ __forceinline__ Floats<V> load_vec(const T* p) { return floats_of<T, V>(load_raw<T, V>(p)); }
 template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, const Floats<V>& r)
 {
     if constexpr (V == 1) {
@@ -97,7 +78,7 @@ __device__ __forceinline__ Place sequence(const Seqs& s, int n)
 // the sequence of token t (sequences without a token hold none)
 __device__ __forceinline__ Place sequence_of(const Seqs& s, long t)
 {
-    if (!s.cu) return sequence(s, (int)(t / s.T));
+    if (!s.cu) return sequence(s, t >> 31 ? (int)(t / s.T) : (int)((unsigned)t / (unsigned)s.T));     // (32 bits divide faster)
     int lo = 0, hi = s.n_seq - 1;                        // last n with cu[n] <= t
     while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (s.cu[mid] <= t) lo = mid; else hi = mid - 1; }
     return sequence(s, lo);
