@@ -36,6 +36,11 @@ __device__ __forceinline__ float softplus(float x)
     return fmaf(2.f * s, p, fmaxf(x, 0.f));
 }
 
+// One value of T: bf16 by the hardware's conversion (nearest even), of which it makes pairs
+template <typename T> __device__ __forceinline__ T rounded(float x);
+template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16_t rounded<bf16_t>(float x) { return {(uint16_t)pack_bf16x2(x, x)}; }
+
 // V consecutive elements, as they are (a load is waited for where it is converted) and as fp32 registers; V * sizeof(T) is 16 or 8 bytes,
 // aligned so, or V = 1.
 template <int V> struct Floats { float v[V]; };
@@ -52,7 +57,7 @@ template <typename T, int V> __device__ __forceinline__ Floats<V> load_vec(const
 template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, const Floats<V>& r)
 {
     if constexpr (V == 1) {
-        *p = from_float<T>(r.v[0]);
+        *p = rounded<T>(r.v[0]);
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < V / 4; ++i)

@@ -50,23 +50,29 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
     if constexpr (HASZ) pz.init(a.z, g.t0, (int)a.ld_z, c, o);
     py.init(a.y, g.t0, a.D, c, o);
     const int tokens = (int)(g.t1 - g.t0);
-    // the tile at token `at` of the segment, and the bases on to the next
-    auto load = [&](auto which, int at) {
+    // The next tile of the segment, and the bases on to the one behind it.  The last tile is asked for again where there is none behind it
+    // (the bases stay: an offset from them may not be negative): the number of loads on their way is then known, and a wait for the older
+    // ones does not wait for the newer.
+    int next = 0;                                        // the token at which that tile begins, <= tokens - 1
+    auto load = [&](auto which) {
         constexpr int w = which.value;
         auto rows = [&](auto full) {
             constexpr bool FULL = full.value != 0;
-            const int last = tokens - 1 - at;
+            const int last = tokens - 1 - next;
             bc.template load<FULL>(in_bc[w], last);
             pu.template load<FULL>(in_u[w], last, o);
             pd.template load<FULL>(in_d[w], last, o);
             if constexpr (HASZ) pz.template load<FULL>(in_z[w], last, o);
         };
-        if (at + kTok <= tokens) rows(IntC<1>());
+        if (next + kTok <= tokens) rows(IntC<1>());
         else rows(IntC<0>());
-        bc.move(kTok);
-        pu.move(kTok);
-        pd.move(kTok);
-        if constexpr (HASZ) pz.move(kTok);
+        if (next + kTok < tokens) {
+            next += kTok;
+            bc.move(kTok);
+            pu.move(kTok);
+            pd.move(kTok);
+            if constexpr (HASZ) pz.move(kTok);
+        }
     };
     auto tile = [&](auto which, int at) {
         constexpr int w = which.value;
@@ -76,10 +82,15 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
         for (int i = 0; i < 2; ++i) {
             u[i] = to_float(in_u[w][i]);
             raw[i] = to_float(in_d[w][i]) + bias;
-            if constexpr (HASZ) z[i] = to_float(in_z[w][i]);
+            settle(u[i]);
+            settle(raw[i]);
+            if constexpr (HASZ) {
+                z[i] = to_float(in_z[w][i]);
+                settle(z[i]);
+            }
         }
         __syncthreads();
-        if (at + 2 * kTok < tokens) load(which, at + 2 * kTok);
+        load(which);
         const int left = tokens - at;
         const float* row = lds[w] + o * 2 * K;
         static_for<2>([&](auto i) {
@@ -127,15 +138,22 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
         });
         if (MODE == kSsmOutputs) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) if (8 * i + o < left && ch.mine) py.store(i, from_float<T>(y[i]));
+            for (int i = 0; i < 2; ++i) {
+                const T out = rounded<T>(y[i]);
+                if (8 * i + o < left && ch.mine) py.store(i, out);
+            }
             py.move(kTok);
         }
     };
-    if (tokens > 0) load(IntC<0>(), 0);
-    if (tokens > kTok) load(IntC<1>(), kTok);
-    for (int at = 0; at < tokens; at += 2 * kTok) {
-        tile(IntC<0>(), at);
-        if (at + kTok < tokens) tile(IntC<1>(), at + kTok);
+    if (tokens > 0) {
+        load(IntC<0>());
+        load(IntC<1>());
+        int at = 0;
+        for (; at + kTok < tokens; at += 2 * kTok) {     // (no way out between the two: the compiler would count its loads as the last)
+            tile(IntC<0>(), at);
+            tile(IntC<1>(), at + kTok);
+        }
+        if (at < tokens) tile(IntC<0>(), at);
     }
     if (MODE == kSsmMaps) sum_delta = oct_sum(sum_delta);
     if (!ch.mine) return;
@@ -208,7 +226,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmArgs<T> a, float* __re
     if (q == 0) {
         s = fmaf(a.skip ? a.skip[c] : 0.f, u, s);
         if (a.z) { const float z = to_float(a.z[b * a.ld_z + c]); s *= z * sigmoid(z); }
-        a.y[b * a.D + c] = from_float<T>(s);
+        a.y[b * a.D + c] = rounded<T>(s);
     }
 }
 

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
     if (!segment_of(a, slot, &g)) return;
     if (MAPS && g.t0 == g.seq.first) return;             // nothing stands before it
     const Channels ch = channels_of(block, a.D, a.G, THREADS / 8);
-    const int c = ch.c;
+    const int c = ch.c, per_group = blocks_c / a.G;
     const long mine = (long)c * S + o * K, DS = (long)a.D * S;
 
     float A2[K], dA[K], ag[K];                           // ag: a_{t+1} g_{t+1}
@@ -76,53 +76,60 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
     float* out_bc = MAPS ? nullptr : a.part_bc + ((long)block * a.M + t_last) * (2 * S);
     T in_bc[decltype(bc)::NE], in_u[NG], in_d[NG], in_z[NG], in_y[NG];
     float in_h[K];
-    // the tile of which `left` tokens are the segment's, and the bases on to the one before it
-    auto load = [&](int left) {
-        auto rows = [&](auto full) {
-            constexpr bool FULL = full.value != 0;
-            bc.template load<FULL>(in_bc, left - 1);
-            pu.template load<FULL>(in_u, left - 1, o);
-            pd.template load<FULL>(in_d, left - 1, o);
-            if constexpr (HASZ) pz.template load<FULL>(in_z, left - 1, o);
-            py.template load<FULL>(in_y, left - 1, o);
-        };
-        if (left >= CK) rows(IntC<1>());
-        else rows(IntC<0>());
-        if constexpr (!MAPS) {
-            load_states<K>(in_h, saved + mine);
-            saved -= DS;
-        }
-        bc.move(-CK);
-        pu.move(-CK);
-        pd.move(-CK);
-        if constexpr (HASZ) pz.move(-CK);
-        py.move(-CK);
+    // the tile at the bases, with `last` the last of its tokens
+    auto load = [&](auto full, int last) {
+        constexpr bool FULL = full.value != 0;
+        bc.template load<FULL>(in_bc, last);
+        pu.template load<FULL>(in_u, last, o);
+        pd.template load<FULL>(in_d, last, o);
+        if constexpr (HASZ) pz.template load<FULL>(in_z, last, o);
+        py.template load<FULL>(in_y, last, o);
+        if constexpr (!MAPS) load_states<K>(in_h, saved + mine);
     };
-    if (tiles > 0) load(tokens - (tiles - 1) * CK);
-    int buf = 0;
-    for (int tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
-        const int left = min(tokens - tile * CK, CK);
-        bc.store(lds[buf], in_bc);
+    // One tile.  FULL: all of its tokens and of the workgroup's channels are there, so that nothing is masked and the number of stores is
+    // known: the wait for the loads before them does not wait for them too.
+    auto step = [&](auto full, int tile) {
+        constexpr bool FULL = full.value != 0;
+        const int w = tile & 1, left = FULL ? CK : min(tokens - tile * CK, CK);
+        bc.store(lds[w], in_bc);
         float u[NG], raw[NG], z[NG], dy[NG], delta[NG], dc[NG], core[NG];
         float h[MAPS ? 1 : CK + 1][K];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             u[i] = to_float(in_u[i]);
             raw[i] = to_float(in_d[i]) + bias;
-            if constexpr (HASZ) z[i] = to_float(in_z[i]);
             dy[i] = to_float(in_y[i]);
+            settle(u[i]);
+            settle(raw[i]);
+            settle(dy[i]);
+            if constexpr (HASZ) {
+                z[i] = to_float(in_z[i]);
+                settle(z[i]);
+            }
         }
         if constexpr (!MAPS) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) h[0][k] = in_h[k];
+            for (int k = 0; k < K; ++k) {
+                h[0][k] = in_h[k];
+                settle(h[0][k]);
+            }
         }
         __syncthreads();
-        if (tile > 0) load(CK);
+        if (tile > 0) {                                  // the tiles before the last have all their tokens
+            if constexpr (!MAPS) saved -= DS;
+            bc.move(-CK);
+            pu.move(-CK);
+            pd.move(-CK);
+            if constexpr (HASZ) pz.move(-CK);
+            py.move(-CK);
+        }
+        // (where a tile is full the first one is too, and is asked for a second time when it is reached)
+        if (FULL || tile > 0) load(IntC<1>(), 0);
         // a token beyond the segment decays nothing, adds nothing and has no gradient; nor has a lane without a channel of its own
         Oct ds[NG], us[NG], cs[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-            const bool live = 8 * i + o < left, own = live && ch.mine;
+            const bool live = FULL || 8 * i + o < left, own = FULL || (live && ch.mine);
             const float soft = softplus(raw[i]);
             delta[i] = where(live, a.softplus ? soft : raw[i]);
             float gate = 1.f;
@@ -133,7 +140,7 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
             cs[i] = oct_of(dc[i]);
             if (MAPS) sum_delta += delta[i];
         }
-        const float* row = lds[buf] + o * 2 * K;
+        const float* row = lds[w] + o * 2 * K;
         if constexpr (MAPS) {
             static_for<CK>([&](auto nn) {
                 constexpr int n = CK - 1 - nn.value, i = n / 8, j = n % 8;
@@ -210,25 +217,31 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
                 const float sa = oct_sum_own(via_a, o) * kLn2, sb = oct_sum_own(via_b, o);
                 float d_raw = fmaf(u[i], sb, sa);
                 d_raw *= a.softplus ? sigmoid(raw[i]) : 1.f;
-                if (8 * i + o < left && ch.mine) {
+                const T out_u = rounded<T>(fmaf(delta[i], sb, skip * dc[i])), out_d = rounded<T>(d_raw);
+                T out_z = {};
+                if constexpr (HASZ) {
+                    const float s = sigmoid(z[i]);
+                    out_z = rounded<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f)));
+                }
+                d_skip = fmaf(dc[i], u[i], d_skip);      // (0 where there is no token or channel)
+                if (FULL || (8 * i + o < left && ch.mine)) {
                     d_bias += d_raw;
-                    d_skip = fmaf(dc[i], u[i], d_skip);
-                    qu.store(i, from_float<T>(fmaf(delta[i], sb, skip * dc[i])));
-                    qd.store(i, from_float<T>(d_raw));
-                    if constexpr (HASZ) {
-                        const float s = sigmoid(z[i]);
-                        qz.store(i, from_float<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f))));
-                    }
+                    qu.store(i, out_u);
+                    qd.store(i, out_d);
+                    if constexpr (HASZ) qz.store(i, out_z);
                 }
             });
             __syncthreads();
             // the waves' channels together: [token][2 S], C first
-            for (int e = threadIdx.x; e < left * 2 * S; e += THREADS) {
-                const float* r = &red[0][0][0] + e;
+#pragma unroll
+            for (int i = 0; i < (CK * 2 * S + THREADS - 1) / THREADS; ++i) {
+                const int e = threadIdx.x + i * THREADS;
+                const float* r = &red[0][0][0] + min(e, CK * 2 * S - 1);
                 float s = 0.f;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) s += r[w * CK * 2 * S];
-                out_bc[e] = s;
+                for (int v = 0; v < WAVES; ++v) s += r[v * CK * 2 * S];
+                if (FULL && CK * 2 * S % THREADS == 0) out_bc[e] = s;
+                else if (e < left * 2 * S) out_bc[e] = s;
             }
             out_bc -= CK * 2 * S;
             qu.move(-CK);
@@ -236,6 +249,13 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
             if constexpr (HASZ) qz.move(-CK);
             // (red is written again behind the next tile's barrier)
         }
+    };
+    if (tiles > 0) {
+        const bool whole = (block % per_group + 1) * (THREADS / 8) <= a.D / a.G;     // the workgroup's channels
+        load(IntC<0>(), tokens - 1 - (tiles - 1) * CK);
+        int tile = tiles - 1;
+        for (; tile >= 0 && !(whole && (tile + 1) * CK <= tokens); --tile) step(IntC<0>(), tile);
+        for (; tile >= 0; --tile) step(IntC<1>(), tile);
     }
     sum_delta = oct_sum(sum_delta);
     d_skip = oct_sum(d_skip);
@@ -308,8 +328,8 @@ __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const float* __restrict
     for (int b = 0; b < blocks; ++b) s += part[((long)g * blocks + b) * M * 2 * S + e];
     const long tok = e / (2 * S);
     const int n = (int)(e % (2 * S));
-    if (n < S) dC[(tok * G + g) * S + n] = from_float<T>(s);
-    else       dB[(tok * G + g) * S + n - S] = from_float<T>(s);
+    if (n < S) dC[(tok * G + g) * S + n] = rounded<T>(s);
+    else       dB[(tok * G + g) * S + n - S] = rounded<T>(s);
 }
 
 template <typename T, int S, int THREADS> static hipError_t ssm_bwd_by(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)

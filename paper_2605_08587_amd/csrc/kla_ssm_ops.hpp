@@ -101,6 +101,10 @@ __device__ __forceinline__ Channels channels_of(int block, int D, int G, int cha
 }
 inline int ssm_channel_blocks(int D, int G, int channels) { return G * ((D / G + channels - 1) / channels); }
 
+// A value that has to be there at this point: a register that a load is about to fill anew must not be read later, or the load goes
+// elsewhere and its result has to be moved, and waited for, at the end of the loop's body.
+__device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
+
 // An element by a base that is the same for the wave and this lane's offset in bytes: no address arithmetic in the vector unit
 template <typename T> __device__ __forceinline__ T load_at(const T* base, unsigned bytes)
 {
