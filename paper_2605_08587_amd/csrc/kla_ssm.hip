@@ -7,7 +7,7 @@
 
 namespace kla {
 
-constexpr int kTok = 16;                                 // tokens per tile
+constexpr int kTok = 16;                                 // tokens per tile (32: 7 to 20 % slower, the code then exceeds what the instruction cache keeps)
 
 enum SsmMode { kSsmOutputs, kSsmStates, kSsmMaps };      // y (and checkpoints); checkpoints alone; the maps of the segments
 
@@ -15,7 +15,7 @@ enum SsmMode { kSsmOutputs, kSsmStates, kSsmMaps };      // y (and checkpoints);
 template <typename T, int S, SsmMode MODE, bool HASZ, int THREADS>
 __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
 {
-    constexpr int K = S / 8, CK = ssm_checkpoint(S);
+    constexpr int K = S / 8, CK = ssm_checkpoint(S), NG = kTok / 8;
     __shared__ __align__(16) float lds[2][2 * kTok * S];
     const int o = threadIdx.x & 7;
     const int block = blockIdx.x % blocks_c;
@@ -41,9 +41,9 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
     float* saved = saves ? a.saved + checkpoint_at(a, g.seq, g.t0, CK) * DS : nullptr;
 
     TileBC<T, S, kTok, THREADS> bc;
-    Tokens<const T, 2> pu, pd, pz;
-    Tokens<T, 2> py;
-    T in_bc[2][decltype(bc)::NE], in_u[2][2], in_d[2][2], in_z[2][2];
+    Tokens<const T, NG> pu, pd, pz;
+    Tokens<T, NG> py;
+    T in_bc[2][decltype(bc)::NE], in_u[2][NG], in_d[2][NG], in_z[2][NG];
     bc.init(a, ch.g, g.t0);
     pu.init(a.u, g.t0, (int)a.ld_u, c, o);
     pd.init(a.delta, g.t0, (int)a.ld_delta, c, o);
@@ -77,9 +77,9 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
     auto tile = [&](auto which, int at) {
         constexpr int w = which.value;
         bc.store(lds[w], in_bc[w]);
-        float u[2], raw[2], z[2], y[2];
+        float u[NG], raw[NG], z[NG], y[NG];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < NG; ++i) {
             u[i] = to_float(in_u[w][i]);
             raw[i] = to_float(in_d[w][i]) + bias;
             settle(u[i]);
@@ -93,25 +93,32 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
         load(which);
         const int left = tokens - at;
         const float* row = lds[w] + o * 2 * K;
-        static_for<2>([&](auto i) {
+        // In steps, in this order: what eight tokens need from LDS is on its way while steps, gates and decays are formed, and the chain of
+        // states finds everything at hand.  (Left to itself the compiler reads each row where it is used and waits.)
+        constexpr int AHEAD = K <= 4 ? 8 : 4;
+        StateBC<K> m[AHEAD];
+        static_for<AHEAD>([&](auto j) { m[j.value] = lds_bc<K>(row + j.value * 2 * S); });
+        __builtin_amdgcn_sched_barrier(0);
+        // a token beyond the segment decays nothing and adds nothing
+        float delta[NG], du[NG], gate[NG];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            const bool in = 8 * i + o < left;
+            const float soft = softplus(raw[i]);
+            delta[i] = where(in, a.softplus ? soft : raw[i]);
+            du[i] = where(in, delta[i] * u[i]);
+            if constexpr (HASZ) gate[i] = z[i] * sigmoid(z[i]);
+            if (MODE == kSsmMaps) sum_delta += delta[i];
+        }
+        static_for<NG>([&](auto i) {
             if (saves && (8 * i.value) % CK == 0) {
                 if (8 * i.value < left && ch.mine) store_states<K>(saved + mine, h);
                 saved += DS;
             }
-            // In three steps, in this order: what eight tokens need from LDS is on its way while their steps and decays are formed, and the
-            // chain of states finds everything at hand.  (Left to itself the compiler reads each row where it is used and waits.)
-            constexpr int AHEAD = K <= 4 ? 8 : 4;
-            StateBC<K> m[AHEAD];
-            static_for<AHEAD>([&](auto j) { m[j.value] = lds_bc<K>(row + (8 * i.value + j.value) * 2 * S); });
-            __builtin_amdgcn_sched_barrier(0);
-            // a token beyond the segment decays nothing and adds nothing
-            const bool in = 8 * i.value + o < left;
-            const float soft = softplus(raw[i.value]), delta = where(in, a.softplus ? soft : raw[i.value]);
-            const Oct ds = oct_of(delta), us = oct_of(where(in, delta * u[i.value]));
+            const Oct ds = oct_of(delta[i.value]), us = oct_of(du[i.value]);
             float acc[8];
             static_for<8 / AHEAD>([&](auto part) {
                 constexpr int j0 = part.value * AHEAD;
-                if constexpr (j0 > 0) static_for<AHEAD>([&](auto j) { m[j.value] = lds_bc<K>(row + (8 * i.value + j0 + j.value) * 2 * S); });
                 float dec[AHEAD][K];
                 static_for<AHEAD>([&](auto j) {
                     const float dj = oct_bcast<j0 + j.value>(ds);
@@ -128,17 +135,19 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
                         if (MODE == kSsmOutputs) s = k ? fmaf(m[j.value].c[k], h[k], s) : m[j.value].c[k] * h[k];
                     }
                     acc[j0 + j.value] = s;
+                    // the row in its place for the tokens that follow
+                    constexpr int n = 8 * i.value + j0 + j.value + AHEAD;
+                    if constexpr (n < kTok) m[j.value] = lds_bc<K>(row + n * 2 * S);
                 });
             });
-            if (MODE == kSsmMaps) sum_delta += delta;
             if (MODE == kSsmOutputs) {
                 y[i.value] = fmaf(skip, u[i.value], oct_sum_own(acc, o));
-                if constexpr (HASZ) y[i.value] *= z[i.value] * sigmoid(z[i.value]);
+                if constexpr (HASZ) y[i.value] *= gate[i.value];
             }
         });
         if (MODE == kSsmOutputs) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < NG; ++i) {
                 const T out = rounded<T>(y[i]);
                 if (8 * i + o < left && ch.mine) py.store(i, out);
             }
