@@ -352,7 +352,7 @@ enum { KLA_LAYER_SILU = 1,        /* kla_conv_*: y = p sigmoid(p) instead of y =
  *   weight      [D, W], bias [D] or NULL            in
  *   state       [n_states, W-1, D] dt or NULL       in   n_states, packed batches: as in kla_chunk_fwd
  *   y           [N, T, D] dt                        out
- *   state_out   [n_states, W-1, D] dt or NULL       out  the last W - 1 inputs; must not alias state
+ *   state_out   [n_states, W-1, D] dt or NULL       out  the last W - 1 inputs; must not alias state (KLA_ERR_SHAPE)
  * W in 2..4, any D >= 1.
  */
 int kla_conv_fwd(const void *x, long ld_x, const float *weight, const float *bias, const void *state,
@@ -387,7 +387,7 @@ int kla_conv_step(const void *x, long ld_x, const float *weight, const float *bi
  *   y           [N, T, D] dt                                            out
  *   hT          [n_states, D, S] fp32                                   out  or NULL; may alias h0
  *   saved       kla_ssm_saved_bytes(...): the states at every 16th token (every 8th from S = 32 on), for the backward; or NULL
- * S in {8, 16, 32, 64}; D a multiple of G; D and the row strides at most 2^24; at most 65535 sequences.
+ * S in {8, 16, 32, 64}; D a multiple of G; D and the row strides at most 2^24; at most 65535 sequences and groups.
  */
 size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq);
 size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq);
@@ -399,7 +399,8 @@ int kla_ssm_fwd(const void *u, long ld_u, const void *delta, long ld_delta, cons
                 int N, int T, int D, int G, int S, kla_dtype dt,
                 void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
 
-/* Gradients of sum <d_y, y> + sum <d_hT, hT> (d_hT NULL: zeros) from the inputs of the forward; saved: what a forward with these
+/* Gradients of sum <d_y, y> + sum <d_hT, hT> (d_hT NULL: zeros) from the inputs of the forward.  The workspace holds the parts of dB
+ * and dC that 32 or 64 channels give each: 8 S bytes per token for each such block of channels.  saved: what a forward with these
  * arguments left, or NULL (it is formed again, in the workspace).  du, ddelta, dz [N, T, D], dB, dC [N, T, G, S] contiguous; dz
  * needed iff z; dskip, ddelta_bias, dh0 NULL if unwanted. */
 size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq,

@@ -86,6 +86,7 @@ template <typename T> kla::ConvArgs<T> conv_args(const void* x, long ld_x, const
 // ---- selective scan ---------------------------------------------------------------------------------------------------------------
 // (a lane's offset from the first of 16 rows fits 32 bits)
 constexpr int kMaxSsmRow = 1 << 24;
+constexpr int kMaxSsmSeqs = 65535;                       // sequences, and groups: a launch's second dimension
 bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
 // Tokens per segment.  A wave takes 8 channels of one segment and its tokens one after the other, about 70 ns each when it has its SIMD to
 // itself; segments cost a second pass over most of the tokens for their maps.  4096 waves run at twice the tokens per second of 1024, one
@@ -128,7 +129,7 @@ SsmPlan ssm_plan(const kla::Seqs& s, const int32_t* cu_host, long M, int D, int 
 // What the queries know: the sizes, and the offsets of a packed batch on the host
 int ssm_sizes(int N, int T, int D, int G, int S, const int32_t* cu_host, int n_seq, kla::Seqs* s, long* M)
 {
-    if (!ssm_shape_ok(D, G, S)) return KLA_ERR_SHAPE;
+    if (!ssm_shape_ok(D, G, S) || N > kMaxSsmSeqs || n_seq > kMaxSsmSeqs || G > kMaxSsmSeqs) return KLA_ERR_SHAPE;
     return take_seqs(n_seq > 0 ? cu_host : nullptr, cu_host, n_seq, N, T, s, M);
 }
 bool ssm_split(const kla::Seqs& s, const SsmPlan& p) { return p.slots > s.n_seq; }
@@ -226,6 +227,7 @@ int kla_conv_fwd(const void* x, long ld_x, const float* weight, const float* bia
     if (const int e = conv_check(x, ld_x, weight, D, W, dt, opts)) return e;
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (M > 0 && (!x || !y)) return KLA_ERR_NULL;
+    if (state_out && state_out == state) return KLA_ERR_SHAPE;       // one is written while the other is read
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, state, y, state_out}) || !aligned(4, {weight, bias})) return KLA_ERR_ALIGN;
     const bool vec = wide_rows(e, {x, state, y, state_out}, {ld_x, D}), silu = opts & KLA_LAYER_SILU;
@@ -317,6 +319,7 @@ int kla_ssm_fwd(const void* u, long ld_u, const void* delta, long ld_delta, cons
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (M > 0 && (!u || !delta || !B || !C || !y)) return KLA_ERR_NULL;
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, y}) || !aligned(16, {A, h0, hT, saved}) || !aligned(4, {skip, delta_bias})) return KLA_ERR_ALIGN;
+    if (s.n_seq > kMaxSsmSeqs || G > kMaxSsmSeqs) return KLA_ERR_SHAPE;
     const SsmPlan p = ssm_plan(s, cu_seqlens_host, M, D, G, S);
     if (saved && saved_bytes < ssm_saved(p, D, S)) return KLA_ERR_WORKSPACE;
     const SsmWork w = ssm_work(static_cast<char*>(workspace), s, p, M, D, G, S, false, false);
@@ -344,6 +347,7 @@ int kla_ssm_bwd(const void* u, long ld_u, const void* delta, long ld_delta, cons
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, d_y, du, ddelta, dB, dC, dz}) || !aligned(16, {A, h0, d_hT, saved, dA, dh0}) ||
         !aligned(4, {skip, delta_bias, dskip, ddelta_bias}))
         return KLA_ERR_ALIGN;
+    if (s.n_seq > kMaxSsmSeqs || G > kMaxSsmSeqs) return KLA_ERR_SHAPE;
     const SsmPlan p = ssm_plan(s, cu_seqlens_host, M, D, G, S);
     if (saved && saved_bytes < ssm_saved(p, D, S)) return KLA_ERR_WORKSPACE;
     const SsmWork w = ssm_work(static_cast<char*>(workspace), s, p, M, D, G, S, true, saved != nullptr);

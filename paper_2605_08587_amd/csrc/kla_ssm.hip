@@ -244,7 +244,7 @@ template <typename T, int S, int THREADS> static hipError_t ssm_fwd_by(const Ssm
     const int blocks_c = ssm_channel_blocks(a.D, a.G, THREADS / 8);
     const long blocks = blocks_c * a.slots;
     if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffL || a.seqs.n_seq > 65535) return hipErrorInvalidConfiguration;
+    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks), block(THREADS);
     if (a.seg_state) {
         hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmMaps, false, THREADS>), grid, block, 0, st, a, blocks_c);

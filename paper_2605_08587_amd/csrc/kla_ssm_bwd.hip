@@ -336,7 +336,7 @@ template <typename T, int S, int THREADS> static hipError_t ssm_bwd_by(const Ssm
 {
     const int blocks_c = ssm_channel_blocks(a.D, a.G, THREADS / 8);
     const long blocks = blocks_c * a.slots, row = (long)a.D * (S + 2);
-    if (blocks > 0x7fffffffL || a.seqs.n_seq > 65535 || a.G > 65535 || (a.M * 2 * S + 255) / 256 > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (blocks > 0x7fffffffL || (a.M * 2 * S + 255) / 256 > 0x7fffffffL) return hipErrorInvalidConfiguration;
     if (blocks > 0) {
         const dim3 grid((unsigned)blocks), block(THREADS);
         if (a.seg_state) {

@@ -125,6 +125,17 @@ def test_offsets(f):
         assert f(cu_dev=dev, cu_host=w.ctypes.data, n_seq=2) == E_SEQ, wrong
 
 
+def test_limits():
+    many = np.zeros(65537, dtype=np.int32)
+    many[-1] = 64
+    for f in (ssm_fwd, ssm_bwd):
+        assert f(cu_dev=0xc000, cu_host=many.ctypes.data, n_seq=65536) == E_SHAPE
+        assert f(N=65536, T=0) == E_SHAPE
+        for ld in ("ld_u", "ld_d", "ld_B", "ld_C"):
+            assert f(**{ld: (1 << 24) + 1}) == E_SHAPE
+    assert conv_fwd(st=0x4000, last=0x4000) == E_SHAPE          # read and written at once
+
+
 @pytest.mark.parametrize("f", [conv_bwd, ssm_bwd, add_bwd, gated_bwd])
 def test_workspace(f):
     assert f(ws=None) == E_WS and f(ws=0x100010) == E_WS and f(ws_bytes=100) == E_WS
