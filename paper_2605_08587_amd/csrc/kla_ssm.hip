@@ -28,9 +28,9 @@ __global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int bloc
     const long mine = ((long)c * S) + o * K, DS = (long)a.D * S;         // this lane's states of [D][S]
 
     float A2[K], h[K];
-    load_states<K>(A2, a.A + mine);
+    load_rates<K>(A2, a.A + mine);
 #pragma unroll
-    for (int k = 0; k < K; ++k) { A2[k] *= kLog2e; h[k] = 0.f; }
+    for (int k = 0; k < K; ++k) h[k] = 0.f;
     const float skip = a.skip ? a.skip[c] : 0.f, bias = a.delta_bias ? a.delta_bias[c] : 0.f;
     if (MODE != kSsmMaps) {
         if (a.seg_state) load_states<K>(h, a.seg_state + slot * DS + mine);

@@ -47,9 +47,9 @@ __global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int bloc
     const long mine = (long)c * S + o * K, DS = (long)a.D * S;
 
     float A2[K], dA[K], ag[K];                           // ag: a_{t+1} g_{t+1}
-    load_states<K>(A2, a.A + mine);
+    load_rates<K>(A2, a.A + mine);
 #pragma unroll
-    for (int k = 0; k < K; ++k) { A2[k] *= kLog2e; dA[k] = ag[k] = 0.f; }
+    for (int k = 0; k < K; ++k) dA[k] = ag[k] = 0.f;
     if (!MAPS) {
         if (a.seg_state) load_states<K>(ag, a.seg_state + slot * DS + mine);
         else if (a.d_hT) load_states<K>(ag, a.d_hT + (long)g.seq.n * DS + mine);

@@ -208,6 +208,18 @@ template <int K> __device__ __forceinline__ void load_states(float (&h)[K], cons
         }
     }
 }
+// log2(e) A of a lane's states.  A state that forgets at once (A = -inf) has the lowest number in its place: a token that is none, with a
+// step of 0, then leaves it as it is and does not make it 0 * inf.
+template <int K> __device__ __forceinline__ void load_rates(float (&A2)[K], const float* p)
+{
+    constexpr float kMost = 3.402823466e38f;
+    load_states<K>(A2, p);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        A2[k] *= kLog2e;
+        if (fabsf(A2[k]) > kMost) A2[k] = copysignf(kMost, A2[k]);       // (false for NaN)
+    }
+}
 template <int K> __device__ __forceinline__ void store_states(float* p, const float (&h)[K])
 {
     if constexpr (K == 1) *p = h[0];

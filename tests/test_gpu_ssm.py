@@ -148,6 +148,25 @@ def test_extreme_steps(kla):
     close("hT", hT, h_ref, SCAN)
 
 
+def test_states_that_forget_at_once(kla):
+    """A = -inf in some places: such a state is its last token's alone, also behind the end of a sequence that ends inside a tile."""
+    D, S, T = 40, 16, 21
+    g, d, dev = _inputs(torch.float32, (1, T), 1, D, 1, S, ALL, False, 78)
+    flat = {k: v if k in ("A", "skip", "delta_bias", "h0") else v.flatten(0, 1) for k, v in d.items()}
+    flat["A"] = d["A"].clone()
+    flat["A"][::3, 5:] = -1e30                           # (the same in 64 bits, and with gradients that exist)
+    dev["A"] = flat["A"].clamp(min=-1e29).cuda()
+    dev["A"][dev["A"] < -1e28] = float("-inf")
+    dy, dh = randn(g, 1, T, D), randn(g, 1, D, S)
+    (y_ref, h_ref), g_ref = lo.gradients(lambda **k: lo.ssm(**k, softplus=True, seqs=[(0, T)]), flat, (dy[0], dh))
+    y, hT = kla.kla_ssm_fwd(**dev)
+    gr = kla.kla_ssm_bwd(**dev, d_y=dy.cuda(), d_hT=dh.cuda())
+    close("y", y[0], y_ref, SCAN)
+    close("hT", hT, h_ref, SCAN)
+    for k in g_ref:
+        close("d" + k, gr["d" + k].reshape(g_ref[k].shape), g_ref[k], SCAN)
+
+
 def test_other_sequences_do_not_reach_in(kla):
     lens, D = [17, 40, 3, 64], 80
     cu = offsets(lens)
