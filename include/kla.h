@@ -400,7 +400,7 @@ int kla_ssm_fwd(const void *u, long ld_u, const void *delta, long ld_delta, cons
                 void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
 
 /* Gradients of sum <d_y, y> + sum <d_hT, hT> (d_hT NULL: zeros) from the inputs of the forward.  The workspace holds the parts of dB
- * and dC that 32 or 64 channels give each: 8 S bytes per token for each such block of channels.  saved: what a forward with these
+ * and dC that 32 channels give each: 8 S bytes per token for each 32 channels.  saved: what a forward with these
  * arguments left, or NULL (it is formed again, in the workspace).  du, ddelta, dz [N, T, D], dB, dC [N, T, G, S] contiguous; dz
  * needed iff z; dskip, ddelta_bias, dh0 NULL if unwanted. */
 size_t kla_ssm_bwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq,

@@ -141,13 +141,17 @@ template <typename T> struct SsmArgs {
     float* seg_state; float* seg_delta;                  // per slot: [D][S] and [D]; NULL: one segment per sequence
     Seqs seqs; long M; int D, G, Lseg; long slots;
     bool softplus;
-    int channels;                                        // per workgroup: 32 or 64
+    int channels;                                        // of a workgroup of the forward: 32 or 64
     // backward
     const T* d_y; const float* d_hT;
     T* du; T* ddelta; T* dz; float* dh0;
     float* part_bc;                                      // [channel block][token][2 S]: gradients of C, then of B
     float* part_p;                                       // [slot][D S + 2 D]: gradients of A, skip, delta_bias
 };
+// Channels of a workgroup of the backward.  With 64 there are half the sums for the gradients of B and C, but eight waves at once that wait for
+// each other and take all registers of a CU (bf16, S = 16, 2048 channels, 2048 tokens, both kernels: 8 sequences 548 us with 32 and 573 with
+// 64, 12 sequences 798 and 1079; at S = 8 454 and 430).
+constexpr int kSsmBwdChannels = 32;
 constexpr int ssm_checkpoint(int S) { return S > 16 ? 8 : 16; }     // tokens between checkpoints
 template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st);
 template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st);

@@ -90,8 +90,8 @@ constexpr int kMaxSsmSeqs = 65535;                       // sequences, and group
 bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
 // Tokens per segment.  A wave takes 8 channels of one segment and its tokens one after the other, about 70 ns each when it has its SIMD to
 // itself; segments cost a second pass over most of the tokens for their maps.  4096 waves run at twice the tokens per second of 1024, one
-// for each SIMD (forward and backward of 2048 tokens x 2048 channels: 189 us in segments, 520 us whole; two such sequences 323 and 532
-// us, three 523 and 543 us, four 618 and 573 us).  So batches of fewer than 768 waves are cut into segments until 4096 run; up to 255
+// for each SIMD (kernels of forward and backward, 2048 tokens x 2048 channels: 168 us in segments, 443 us whole; two such sequences 297
+// and 447 us, three 435 and 462 us, four 551 and 490 us).  So batches of fewer than 768 waves are cut into segments until 4096 run; up to 255
 // tokens the additional launches cost more than they save.  In a packed batch the longest sequence decides: it would run on alone.
 int ssm_segment(long M, int n_states, int D, long longest)
 {
@@ -121,9 +121,11 @@ SsmPlan ssm_plan(const kla::Seqs& s, const int32_t* cu_host, long M, int D, int 
         p.slots = (per > 0 ? per : 1) * s.n_seq;
         p.checkpoints = ((long)s.T + ck - 1) / ck * s.n_seq;
     }
-    // Workgroups of 64 channels leave half the sums for the gradients of B and C that those of 32 leave; where there are fewer of them
-    // than CUs the smaller ones keep more CUs at work.  At S = 64 the backward needs the registers of a CU for four waves.
-    if (S == 64 || (long)G * ((D / G + 63) / 64) * p.slots < 256) p.channels = 32;
+    // The forward's workgroups have 64 channels (half as many bring in the rows of B and C) unless 32 spread more evenly over the CUs, where
+    // they may be more than a tenth slower.  (bf16, 2048 channels, 2048 tokens, 64 and 32: 8 sequences 225 and 244 us, 16 sequences 404
+    // and 456 us, 12 sequences 378 and 334 us, 4 sequences 205 and 142 us; 8 sequences with 64 states 579 and 548 us: there it is 32.)
+    auto rounds = [&](int channels) { return ((long)G * ((D / G + channels - 1) / channels) * p.slots + 255) / 256; };
+    if (S == 64 || 20 * rounds(64) > 11 * rounds(32)) p.channels = 32;
     return p;
 }
 // What the queries know: the sizes, and the offsets of a packed batch on the host
@@ -144,7 +146,7 @@ SsmWork ssm_work(char* base, const kla::Seqs& s, const SsmPlan& p, long M, int D
         w.seg_delta = c.take<float>((size_t)p.slots * D);
     }
     if (bwd) {
-        const long blocks = (long)G * ((D / G + p.channels - 1) / p.channels);
+        const long blocks = (long)G * ((D / G + kla::kSsmBwdChannels - 1) / kla::kSsmBwdChannels);
         if (!keeps) w.saved = c.take<float>((size_t)p.checkpoints * D * S);
         w.part_bc = c.take<float>((size_t)blocks * M * 2 * S);
         w.part_p = c.take<float>((size_t)p.slots * D * (S + 2));

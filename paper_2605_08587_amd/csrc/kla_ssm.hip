@@ -11,9 +11,10 @@ constexpr int kTok = 16;                                 // tokens per tile (32:
 
 enum SsmMode { kSsmOutputs, kSsmStates, kSsmMaps };      // y (and checkpoints); checkpoints alone; the maps of the segments
 
-// One workgroup: THREADS / 8 channels of one segment, tiles of 16 tokens one after the other, two tiles on their way.
+// One workgroup: THREADS / 8 channels of one segment, tiles of 16 tokens one after the other, two tiles on their way.  (The bound of two waves per
+// SIMD: the compiler would give the maps at S = 64 more registers than two waves have; 16384 tokens x 1024 channels 221 against 260 us.)
 template <typename T, int S, SsmMode MODE, bool HASZ, int THREADS>
-__global__ __launch_bounds__(THREADS) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
+__global__ __launch_bounds__(THREADS, MODE == kSsmMaps && S == 64 ? 2 : 1) void ssm_fwd_kernel(SsmArgs<T> a, int blocks_c)
 {
     constexpr int K = S / 8, CK = ssm_checkpoint(S), NG = kTok / 8;
     __shared__ __align__(16) float lds[2][2 * kTok * S];

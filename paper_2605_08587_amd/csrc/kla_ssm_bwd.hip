@@ -28,12 +28,14 @@ __device__ __forceinline__ float swap16_sum(float x, float y)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// (Bound to two waves per SIMD in fp32 up to S = 32, where the compiler would take more registers: at S = 16, 8 x 999 tokens x 2048 channels,
+// 284 against 330 us.  At S = 64 the bound spills and costs twice the time; in bf16 it only moves code, 5 % the worse.)
 // MAPS: what a segment adds to the gradient that enters the one before it, from zeros (with the segment's sum of delta).
-template <typename T, int S, bool MAPS, bool HASZ, int THREADS>
-__global__ __launch_bounds__(THREADS) void ssm_bwd_kernel(SsmArgs<T> a, int blocks_c)
+template <typename T, int S, bool MAPS, bool HASZ>
+__global__ __launch_bounds__(kSsmBwdChannels * 8, S < 64 && sizeof(T) == 4 ? 2 : 1) void ssm_bwd_kernel(SsmArgs<T> a, int blocks_c)
 {
     constexpr int K = S / 8, CK = ssm_checkpoint(S), NG = CK / 8;    // tokens per checkpoint and tile, in groups of eight
-    constexpr int WAVES = THREADS / 64;
+    constexpr int THREADS = kSsmBwdChannels * 8, WAVES = THREADS / 64;
     __shared__ __align__(16) float lds[2][2 * CK * S];
     __shared__ float red[MAPS ? 1 : WAVES][MAPS ? 1 : CK][2 * S];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, o = lane & 7;
@@ -332,16 +334,16 @@ __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const float* __restrict
     else       dB[(tok * G + g) * S + n - S] = rounded<T>(s);
 }
 
-template <typename T, int S, int THREADS> static hipError_t ssm_bwd_by(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
+template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
 {
-    const int blocks_c = ssm_channel_blocks(a.D, a.G, THREADS / 8);
+    const int blocks_c = ssm_channel_blocks(a.D, a.G, kSsmBwdChannels);
     const long blocks = blocks_c * a.slots, row = (long)a.D * (S + 2);
     if (blocks > 0x7fffffffL || (a.M * 2 * S + 255) / 256 > 0x7fffffffL) return hipErrorInvalidConfiguration;
     if (blocks > 0) {
-        const dim3 grid((unsigned)blocks), block(THREADS);
+        const dim3 grid((unsigned)blocks), block(kSsmBwdChannels * 8);
         if (a.seg_state) {
-            if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, true, THREADS>), grid, block, 0, st, a, blocks_c);
-            else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, false, THREADS>), grid, block, 0, st, a, blocks_c);
+            if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, true>), grid, block, 0, st, a, blocks_c);
+            else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, false>), grid, block, 0, st, a, blocks_c);
             if (const hipError_t e = hipGetLastError()) return e;
             hipLaunchKernelGGL((ssm_join_bwd_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
             if (const hipError_t e = hipGetLastError()) return e;
@@ -350,8 +352,8 @@ template <typename T, int S, int THREADS> static hipError_t ssm_bwd_by(const Ssm
             hipLaunchKernelGGL((ssm_clear_kernel<T>), dim3((unsigned)a.slots), dim3(256), 0, st, a, row);
             if (const hipError_t e = hipGetLastError()) return e;
         }
-        if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, true, THREADS>), grid, block, 0, st, a, blocks_c);
-        else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, false, THREADS>), grid, block, 0, st, a, blocks_c);
+        if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, true>), grid, block, 0, st, a, blocks_c);
+        else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, false>), grid, block, 0, st, a, blocks_c);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     if (a.M > 0) {
@@ -360,13 +362,6 @@ template <typename T, int S, int THREADS> static hipError_t ssm_bwd_by(const Ssm
         if (const hipError_t e = hipGetLastError()) return e;
     }
     return launch_column_sums(a.part_p, a.slots, {{(long)a.D * S, a.D, a.D}, {dA, dskip, ddelta_bias}}, st);
-}
-template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
-{
-    if constexpr (S < 64) {
-        if (a.channels == 64) return ssm_bwd_by<T, S, 512>(a, dA, dB, dC, dskip, ddelta_bias, st);
-    }
-    return ssm_bwd_by<T, S, 256>(a, dA, dB, dC, dskip, ddelta_bias, st);
 }
 template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
 {
