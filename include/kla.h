@@ -335,8 +335,8 @@ int kla_beta(const void *k, const float *eta, float eps, float *beta,
  *   - Inputs whose row stride ld_* (elements from one token to the next) is an argument may be column ranges of a wider
  *     tensor, e.g. of the output of one projection for several of them; a row itself is contiguous.  Everything else is
  *     contiguous, and so are all outputs.
- *   - Data pointers have to be aligned to their element only (A, states and checkpoints: 16 bytes).  Rows that start on
- *     16-byte boundaries are taken 16 bytes at a time, others element by element, with the same results.
+ *   - Data pointers have to be aligned to their element only (A, states and checkpoints: 16 bytes);
+ *     rows may start at any element and have any width.
  *   - Parameters (weights, biases, scales) and their gradients are fp32.
  * All sums, states and norms are fp32; an output is rounded to dt once.  Results are deterministic (no atomics).
  * ------------------------------------------------------------------------------------------------------------------ */

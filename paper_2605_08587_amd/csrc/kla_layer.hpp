@@ -41,11 +41,16 @@ template <typename T> __device__ __forceinline__ T rounded(float x);
 template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16_t rounded<bf16_t>(float x) { return {(uint16_t)pack_bf16x2(x, x)}; }
 
-// V consecutive elements, as they are (a load is waited for where it is converted) and as fp32 registers; V * sizeof(T) is 16 or 8 bytes,
-// aligned so, or V = 1.
+// V consecutive elements, as they are (a load is waited for where it is converted) and as fp32 registers.  They stand at any element: rows
+// of odd widths and column ranges of wider tensors are no different, and one load or store of up to 16 bytes takes them all the same.
 template <int V> struct Floats { float v[V]; };
 template <typename T, int V> struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Raw { T v[V]; };
-template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p) { return *reinterpret_cast<const Raw<T, V>*>(p); }
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p) 
+{
+    Raw<T, V> r;
+    __builtin_memcpy(&r, p, sizeof r);
+    return r;
+}
 template <typename T, int V> __device__ __forceinline__ Floats<V> floats_of(const Raw<T, V>& x)
 {
     Floats<V> r;
@@ -59,14 +64,12 @@ template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, con
     if constexpr (V == 1) {
         *p = rounded<T>(r.v[0]);
     } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i)
-            reinterpret_cast<float4*>(p)[i] = make_float4(r.v[4 * i], r.v[4 * i + 1], r.v[4 * i + 2], r.v[4 * i + 3]);
-    } else if constexpr (V == 8) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(r.v[0], r.v[1]), pack_bf16x2(r.v[2], r.v[3]),
-                                                  pack_bf16x2(r.v[4], r.v[5]), pack_bf16x2(r.v[6], r.v[7]));
+        __builtin_memcpy(p, r.v, sizeof r.v);
     } else {
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(r.v[0], r.v[1]), pack_bf16x2(r.v[2], r.v[3]));
+        uint32_t pairs[V / 2];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) pairs[i] = pack_bf16x2(r.v[2 * i], r.v[2 * i + 1]);
+        __builtin_memcpy(p, pairs, sizeof pairs);
     }
 }
 // Elements of T in 16 bytes
@@ -104,8 +107,8 @@ template <typename T> struct ConvArgs {
 // lays out the partial sums.
 struct ConvBwdPlan { int tx, ty, L; long blocks_t; };
 ConvBwdPlan conv_bwd_plan(long M, int D);
-template <typename T> hipError_t launch_conv_fwd(const ConvArgs<T>& a, int W, bool silu, bool vec, hipStream_t st);
-template <typename T> hipError_t launch_conv_bwd(const ConvArgs<T>& a, int W, bool silu, bool vec, float* dweight, float* dbias, hipStream_t st);
+template <typename T> hipError_t launch_conv_fwd(const ConvArgs<T>& a, int W, bool silu, hipStream_t st);
+template <typename T> hipError_t launch_conv_bwd(const ConvArgs<T>& a, int W, bool silu, float* dweight, float* dbias, hipStream_t st);
 template <typename T> hipError_t launch_conv_step(const T* x, long ld_x, const float* weight, const float* bias, T* state, T* y, int B, int D, int W,
                                                   bool silu, hipStream_t st);
 
@@ -124,11 +127,11 @@ template <typename T> struct GatedNormArgs {
     unsigned opts;                                       // kLayerSigmoid | kLayerGateFirst
 };
 // Workgroups of a norm's backward, each of which leaves a row of partial sums
-int norm_bwd_blocks(long rows, int D, bool vec, int vec_len);
-template <typename T, typename R> hipError_t launch_add_norm_fwd(const AddNormArgs<T, R>& a, bool vec, hipStream_t st);
-template <typename T, typename R> hipError_t launch_add_norm_bwd(const AddNormArgs<T, R>& a, bool vec, float* dweight, float* dscale, hipStream_t st);
-template <typename T> hipError_t launch_gated_norm_fwd(const GatedNormArgs<T>& a, bool vec, hipStream_t st);
-template <typename T> hipError_t launch_gated_norm_bwd(const GatedNormArgs<T>& a, bool vec, float* dweight, hipStream_t st);
+int norm_bwd_blocks(long rows, int D, int vec_len);
+template <typename T, typename R> hipError_t launch_add_norm_fwd(const AddNormArgs<T, R>& a, hipStream_t st);
+template <typename T, typename R> hipError_t launch_add_norm_bwd(const AddNormArgs<T, R>& a, float* dweight, float* dscale, hipStream_t st);
+template <typename T> hipError_t launch_gated_norm_fwd(const GatedNormArgs<T>& a, hipStream_t st);
+template <typename T> hipError_t launch_gated_norm_bwd(const GatedNormArgs<T>& a, float* dweight, hipStream_t st);
 
 // Selective scan.  The tokens of a sequence are taken in segments of Lseg (a multiple of the checkpoint distance); segment k of
 // sequence n has the slot first/Lseg + n + k (packed) or n * ceil(T/Lseg) + k, which nothing has to count: a few slots stay empty.

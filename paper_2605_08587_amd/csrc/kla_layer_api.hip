@@ -68,12 +68,6 @@ int conv_check(const void* x, long ld_x, const float* weight, int D, int W, int 
     (void)x;
     return KLA_OK;
 }
-// rows that can be taken 16 bytes at a time
-bool wide_rows(size_t e, std::initializer_list<const void*> ps, std::initializer_list<long> lds)
-{
-    for (const long ld : lds) if (ld * (long)e % 16) return false;
-    return aligned(16, ps);
-}
 template <typename T> kla::ConvArgs<T> conv_args(const void* x, long ld_x, const float* weight, const float* bias, const void* state, const kla::Seqs& s,
                                                  long M, int D)
 {
@@ -232,12 +226,12 @@ int kla_conv_fwd(const void* x, long ld_x, const float* weight, const float* bia
     if (state_out && state_out == state) return KLA_ERR_SHAPE;       // one is written while the other is read
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, state, y, state_out}) || !aligned(4, {weight, bias})) return KLA_ERR_ALIGN;
-    const bool vec = wide_rows(e, {x, state, y, state_out}, {ld_x, D}), silu = opts & KLA_LAYER_SILU;
+    const bool silu = opts & KLA_LAYER_SILU;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.y = static_cast<decltype(a.y)>(y);
         a.state_out = static_cast<decltype(a.y)>(state_out);
-        return status(kla::launch_conv_fwd(a, W, silu, vec, st));
+        return status(kla::launch_conv_fwd(a, W, silu, st));
     };
     return dt == KLA_BF16 ? run(conv_args<bf16_t>(x, ld_x, weight, bias, state, s, M, D)) : run(conv_args<float>(x, ld_x, weight, bias, state, s, M, D));
 }
@@ -260,14 +254,14 @@ int kla_conv_bwd(const void* x, long ld_x, const float* weight, const float* bia
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, state, d_y, d_state_out, dx, d_state}) || !aligned(4, {weight, bias, dweight, dbias})) return KLA_ERR_ALIGN;
     if (const int r = take_workspace(workspace, workspace_bytes, kla_conv_bwd_workspace_bytes(N, T, D, W))) return r;
-    const bool vec = wide_rows(e, {x, state, d_y, d_state_out, dx, d_state}, {ld_x, D}), silu = opts & KLA_LAYER_SILU;
+    const bool silu = opts & KLA_LAYER_SILU;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         using P = decltype(a.x);
         using Q = decltype(a.y);
         a.d_y = static_cast<P>(d_y); a.d_state_out = static_cast<P>(d_state_out); a.dx = static_cast<Q>(dx); a.d_state = static_cast<Q>(d_state);
         a.partial = static_cast<float*>(workspace);
-        return status(kla::launch_conv_bwd(a, W, silu, vec, dweight, dbias, st));
+        return status(kla::launch_conv_bwd(a, W, silu, dweight, dbias, st));
     };
     return dt == KLA_BF16 ? run(conv_args<bf16_t>(x, ld_x, weight, bias, state, s, M, D)) : run(conv_args<float>(x, ld_x, weight, bias, state, s, M, D));
 }
@@ -399,24 +393,18 @@ int kla_add_norm_fwd(const void* x, long ld_x, const void* residual, const float
     if (M > 0 && !y) return KLA_ERR_NULL;
     const size_t e = elem_bytes(dt), r = elem_bytes(res_dt);
     if (!aligned(e, {x, y}) || !aligned(r, {residual, residual_out}) || !aligned(4, {scale, weight})) return KLA_ERR_ALIGN;
-    const bool vec = wide_rows(e, {x, y, scale, weight, residual, residual_out}, {ld_x, D});
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.y = static_cast<decltype(a.y)>(y);
         a.residual_out = static_cast<decltype(a.residual_out)>(residual_out);
-        return status(kla::launch_add_norm_fwd(a, vec, st));
+        return status(kla::launch_add_norm_fwd(a, st));
     };
     if (dt == KLA_F32) return run(add_norm_args<float, float>(x, ld_x, residual, scale, weight, eps, M, D));
     return res_dt == KLA_F32 ? run(add_norm_args<bf16_t, float>(x, ld_x, residual, scale, weight, eps, M, D))
                              : run(add_norm_args<bf16_t, bf16_t>(x, ld_x, residual, scale, weight, eps, M, D));
 }
 
-// (without vectors there are as many workgroups or fewer)
-static int norm_blocks(long rows, int D, int dt)
-{
-    const int n = dt == KLA_BF16 ? 8 : 4, v = kla::norm_bwd_blocks(rows, D, true, n), s = kla::norm_bwd_blocks(rows, D, false, n);
-    return v > s ? v : s;
-}
+static int norm_blocks(long rows, int D, int dt) { return kla::norm_bwd_blocks(rows, D, dt == KLA_BF16 ? 8 : 4); }
 size_t kla_add_norm_bwd_workspace_bytes(long M, int D, kla_dtype dt)
 {
     if (!dt_ok(dt) || !norm_shape_ok(M, D, 0.f)) return 0;
@@ -433,7 +421,6 @@ int kla_add_norm_bwd(const void* x, long ld_x, const void* residual, const float
     if (!aligned(e, {x, d_y, dx}) || !aligned(r, {residual, d_residual_out, d_residual}) || !aligned(4, {scale, weight, dscale, dweight}))
         return KLA_ERR_ALIGN;
     if (const int q = take_workspace(workspace, workspace_bytes, kla_add_norm_bwd_workspace_bytes(M, D, dt))) return q;
-    const bool vec = wide_rows(e, {x, d_y, dx, scale, weight, residual, d_residual_out, d_residual}, {ld_x, D});
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.d_y = static_cast<decltype(a.d_y)>(d_y);
@@ -441,7 +428,7 @@ int kla_add_norm_bwd(const void* x, long ld_x, const void* residual, const float
         a.dx = static_cast<decltype(a.dx)>(dx);
         a.d_residual = static_cast<decltype(a.d_residual)>(d_residual);
         a.partial = static_cast<float*>(workspace);
-        return status(kla::launch_add_norm_bwd(a, vec, dweight, dscale, st));
+        return status(kla::launch_add_norm_bwd(a, dweight, dscale, st));
     };
     if (dt == KLA_F32) return run(add_norm_args<float, float>(x, ld_x, residual, scale, weight, eps, M, D));
     return res_dt == KLA_F32 ? run(add_norm_args<bf16_t, float>(x, ld_x, residual, scale, weight, eps, M, D))
@@ -455,11 +442,10 @@ int kla_gated_norm_fwd(const void* x, long ld_x, const void* gate, long ld_gate,
     if (M > 0 && !y) return KLA_ERR_NULL;
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, gate, y}) || !aligned(4, {weight})) return KLA_ERR_ALIGN;
-    const bool vec = wide_rows(e, {x, gate, y, weight}, {ld_x, ld_gate, D});
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.y = static_cast<decltype(a.y)>(y);
-        return status(kla::launch_gated_norm_fwd(a, vec, st));
+        return status(kla::launch_gated_norm_fwd(a, st));
     };
     return dt == KLA_BF16 ? run(gated_norm_args<bf16_t>(x, ld_x, gate, ld_gate, weight, eps, M, H, D, opts))
                           : run(gated_norm_args<float>(x, ld_x, gate, ld_gate, weight, eps, M, H, D, opts));
@@ -479,14 +465,13 @@ int kla_gated_norm_bwd(const void* x, long ld_x, const void* gate, long ld_gate,
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, gate, d_y, dx, d_gate}) || !aligned(4, {weight, dweight})) return KLA_ERR_ALIGN;
     if (const int q = take_workspace(workspace, workspace_bytes, kla_gated_norm_bwd_workspace_bytes(M, H, D, dt))) return q;
-    const bool vec = wide_rows(e, {x, gate, d_y, dx, d_gate, weight}, {ld_x, ld_gate, D});
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.d_y = static_cast<decltype(a.d_y)>(d_y);
         a.dx = static_cast<decltype(a.dx)>(dx);
         a.d_gate = static_cast<decltype(a.dx)>(d_gate);
         a.partial = static_cast<float*>(workspace);
-        return status(kla::launch_gated_norm_bwd(a, vec, dweight, st));
+        return status(kla::launch_gated_norm_bwd(a, dweight, st));
     };
     return dt == KLA_BF16 ? run(gated_norm_args<bf16_t>(x, ld_x, gate, ld_gate, weight, eps, M, H, D, opts))
                           : run(gated_norm_args<float>(x, ld_x, gate, ld_gate, weight, eps, M, H, D, opts));

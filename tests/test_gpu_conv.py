@@ -154,3 +154,24 @@ def test_offsets_beyond_32_bits(kla):
     g = kla.kla_conv_bwd(x, w, x)
     t = kla.kla_conv_bwd(x[:, -40:].contiguous(), w, x[:, -40:].contiguous(), state=x[:, -43:-40].contiguous())
     assert torch.equal(bits(g["dx"][:, -40:]), bits(t["dx"]))
+
+
+@pytest.mark.parametrize("D", [1, 3, 4, 5, 8, 9, 13, 255, 517, 1027])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_widths_around_vectors(kla, D, dtype):
+    """Rows whose last vector begins within the one before it, or that have none: alike, every value written twice included."""
+    g = torch.Generator().manual_seed(D)
+    lens = [3, 0, 70, 1, 40]
+    cu, M = offsets(lens), sum(lens)
+    x, w, b = randn(g, 1, M, D, dtype=dtype), randn(g, D, 4), randn(g, D)
+    st, dy, ds = randn(g, 5, 3, D, dtype=dtype), randn(g, 1, M, D, dtype=dtype), randn(g, 5, 3, D, dtype=dtype)
+    print("conv", D, dtype, flush=True)
+    seqs = lo.sequences(1, M, cu)
+    (y_ref, last_ref), ref = lo.gradients(lambda **k: lo.conv(**k, seqs=seqs, silu=True), dict(x=x[0], weight=w, bias=b, state=st), (dy[0], ds))
+    packed = dict(cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
+    y, last = kla.kla_conv_fwd(x.cuda(), w.cuda(), b.cuda(), st.cuda(), **packed)
+    got = kla.kla_conv_bwd(x.cuda(), w.cuda(), dy.cuda(), b.cuda(), st.cuda(), ds.cuda(), **packed)
+    close("y", y[0], y_ref, SUMS)
+    assert torch.equal(last.cpu().double(), last_ref)
+    for k, v in (("x", got["dx"][0]), ("weight", got["dweight"]), ("bias", got["dbias"]), ("state", got["dstate"])):
+        close("d" + k, v, ref[k], SUMS)

@@ -157,3 +157,11 @@ def test_offsets_beyond_32_bits(kla):
     z = kla.kla_gated_norm_fwd(x.view(M, 16, 128), y.view(M, 16, 128), w[:128].contiguous())
     u = kla.kla_gated_norm_fwd(x[-9:].reshape(9, 16, 128), y[-9:].reshape(9, 16, 128), w[:128].contiguous())
     assert torch.equal(bits(z[-9:]), bits(u))
+
+
+@pytest.mark.parametrize("D", [3, 4, 5, 8, 9, 15, 127, 129, 1025, 2047, 4099, 8191])
+def test_widths_around_vectors(kla, D):
+    """Rows whose last vector is short, or that have none."""
+    for dtype, res in ((b16, f32), (f32, f32)):
+        test_add_norm(kla, D, dtype, res)
+        test_gated_norm(kla, D, dtype)
