@@ -86,13 +86,14 @@ bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 
 // itself; segments cost a second pass over most of the tokens for their maps.  4096 waves run at twice the tokens per second of 1024, one
 // for each SIMD (kernels of forward and backward, 2048 tokens x 2048 channels: 168 us in segments, 443 us whole; two such sequences 297
 // and 447 us, three 435 and 462 us, four 551 and 490 us).  So batches of fewer than 768 waves are cut into segments until 4096 run; up to 255
-// tokens the additional launches cost more than they save.  In a packed batch the longest sequence decides: it would run on alone.
+// tokens the additional launches cost more than they save.  Segments are whole pairs of tiles, and 64 tokens at least (in multiples of 64 one sequence
+// of 7000 tokens x 1024 channels took 82 us forward instead of 74).  In a packed batch the longest sequence decides: it would run on alone.
 int ssm_segment(long M, int n_states, int D, long longest)
 {
-    const int whole = INT_MAX / 64 * 64;
+    const int whole = INT_MAX / 32 * 32;
     const long per = ((long)D + 7) / 8;                  // waves of one sequence
     if (n_states == 0 || longest < 256 || M * per >= 768 * longest) return whole;
-    const long len = (M * per / 4096 + 63) / 64 * 64;
+    const long len = (M * per / 4096 + 31) / 32 * 32;
     return (int)(len < 64 ? 64 : len < whole ? len : whole);
 }
 struct SsmPlan { int Lseg; long slots, checkpoints; int channels; };
