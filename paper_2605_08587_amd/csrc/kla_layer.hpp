@@ -18,19 +18,17 @@ constexpr float kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float rcp_hw(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ __forceinline__ float sigmoid(float x) { return rcp_hw(1.f + exp2_hw(-kLog2e * x)); }
-// log(1 + e^x) = max(x, 0) + log1p(e^-|x|), the second term as 2 atanh(s) = 2 (s + s^3/3 + ...), s = e/(2 + e) <= 1/3: full
-// relative precision also where the result is as small as e^x itself (a logarithm of 1 + e loses it there).
+// log(1 + e^x) = max(x, 0) + log1p(e^-|x|), the second term as 2 atanh(s) = 2 s (1 + s^2/3 + ...), s = e/(2 + e) <= 1/3: full
+// relative precision also where the result is as small as e^x itself (a logarithm of 1 + e loses it there).  The coefficients are a least
+// largest relative error's over s^2 <= 1/9, 5e-9 before rounding.
 __device__ __forceinline__ float softplus(float x)
 {
     const float e = exp2_hw(-kLog2e * fabsf(x));
     const float s = e * rcp_hw(2.f + e), q = s * s;
-    float p = 1.f / 15.f;
-    p = fmaf(p, q, 1.f / 13.f);
-    p = fmaf(p, q, 1.f / 11.f);
-    p = fmaf(p, q, 1.f / 9.f);
-    p = fmaf(p, q, 1.f / 7.f);
-    p = fmaf(p, q, 1.f / 5.f);
-    p = fmaf(p, q, 1.f / 3.f);
+    float p = 0.140059933f;
+    p = fmaf(p, q, 0.140009031f);
+    p = fmaf(p, q, 0.200107634f);
+    p = fmaf(p, q, 0.333332092f);
     p = fmaf(p, q, 1.f);
     // (a NaN stays one: fmaxf alone would drop it, the sum with p does not)
     return fmaf(2.f * s, p, fmaxf(x, 0.f));
