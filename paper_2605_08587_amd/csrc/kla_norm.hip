@@ -116,10 +116,12 @@ __global__ __launch_bounds__(block_threads(TPR)) void add_norm_fwd_kernel(AddNor
         KLA_EACH(v, i) x.v[v][i] *= s.v[v][i];
     }
     const Row<V, NV> w = at.load(a.weight);
-    if (a.residual_out) at.store(a.residual_out + row * a.D, x);
     float sum = 0.f;
     KLA_EACH(v, i) sum = fmaf(at.once(v, i, x.v[v][i]), x.v[v][i], sum);
     const float f = inv_rms(row_sum<TPR>(sum, red), 1.f / (float)a.D, a.eps);
+    // Behind the sum's barrier: residual_out may be residual, and the row's last vector has columns of another wave's, which has to have read
+    // them by then (up to TPR = 64 one wave has the row, and its loads stand ahead of its stores).
+    if (a.residual_out) at.store(a.residual_out + row * a.D, x);
     KLA_EACH(v, i) x.v[v][i] *= f * w.v[v][i];
     at.store(a.y + row * a.D, x);
 }

@@ -165,3 +165,30 @@ def test_widths_around_vectors(kla, D):
     for dtype, res in ((b16, f32), (f32, f32)):
         test_add_norm(kla, D, dtype, res)
         test_gated_norm(kla, D, dtype)
+
+
+def test_in_place_where_waves_share_columns(kla):
+    """The stream updated in place at widths whose last vector begins within one of another wave's: the bits of the call with a stream of
+    its own, in many rows at once."""
+    for dtype, res, widths in ((b16, b16, (1025, 1031, 1537, 2047, 2049, 4097, 8185)), (b16, f32, (1025, 1031, 1537, 2047, 2049, 8185)),
+                               (f32, f32, (513, 1025, 1027, 2047, 2049, 4097, 8189))):
+        for D in widths:
+            print("add_norm in place", dtype, res, D, flush=True)
+            g = torch.Generator().manual_seed(D)
+            x, w, s = randn(g, 700, D, dtype=dtype).cuda(), randn(g, D).cuda(), randn(g, D).cuda()
+            r, dy, dr = randn(g, 700, D).to(res).cuda(), randn(g, 700, D, dtype=dtype).cuda(), randn(g, 700, D).to(res).cuda()
+            y, r2 = kla.kla_add_norm_fwd(x, w, r, s, eps=EPS)
+            same = r.clone()
+            y3, r3 = kla.kla_add_norm_fwd(x, w, same, s, eps=EPS, residual_out=same)
+            assert r3 is same and torch.equal(bits(r2), bits(r3)) and torch.equal(bits(y), bits(y3))
+            close("r", r3, r.double() + s.double() * x.double(), SUMS)
+            # and the gradient of the stream in the place of the one that comes in, which the C ABI permits
+            own = kla.kla_add_norm_bwd(x, w, dy, r, s, EPS, dr)
+            ws = torch.empty(kla.lib().kla_add_norm_bwd_workspace_bytes(700, D, 1 if dtype == b16 else 0), dtype=torch.uint8, device="cuda")
+            dx, dw, ds = torch.empty_like(x), torch.empty_like(w), torch.empty_like(s)
+            rc = kla.lib().kla_add_norm_bwd(*(v.data_ptr() if torch.is_tensor(v) else v for v in (
+                x, D, r, s, w, EPS, dy, dr, dx, dr, ds, dw, 700, D, 1 if dtype == b16 else 0, 1 if res == b16 else 0, ws, ws.numel(),
+                torch.cuda.current_stream().cuda_stream)))
+            assert rc == 0
+            for k, t in (("dx", dx), ("dresidual", dr), ("dscale", ds), ("dweight", dw)):
+                assert torch.equal(bits(own[k]), bits(t)), k
