@@ -155,6 +155,14 @@ def _dev(*ts):
                 raise ValueError("tensors must be contiguous")
 
 
+def _written(*ts):
+    """Tensors of the caller's that a call has written through their bare pointers: what the graph saved of them has changed, and its
+    backward has to find out.  (An inference tensor does not count its changes.)"""
+    for t in ts:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 

@@ -71,6 +71,13 @@ template <typename O> bool saved_or_none(const O& o, const at::Tensor& q, const 
 inline void* ptr(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 inline float* fptr(const at::Tensor* t) { return static_cast<float*>(ptr(t)); }
 
+// Tensors of the caller's that a call has written through their bare pointers (null: not given): what the graph saved of them has
+// changed, and its backward has to find out.  (An inference tensor does not count its changes.)
+inline void written(std::initializer_list<const at::Tensor*> ts)
+{
+    for (const at::Tensor* t : ts) if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 inline bool type_of(const at::Tensor& q, kla_dtype* dt)
 {
     if (q.scalar_type() == at::kBFloat16) *dt = KLA_BF16;

@@ -255,6 +255,7 @@ PyObject* conv_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
         const NoGil no_gil;
         c.fwd(y, l, a[7] == Py_True);
     } catch (const Refused& e) { return PyLong_FromLong(e.code); }
+    written({out, last});
     return pair(y, l);
     END_HANDLE_TH_ERRORS
 }
@@ -299,6 +300,7 @@ PyObject* conv_step(PyObject*, PyObject* const* a, Py_ssize_t n)
         rc = api.conv_step(ptr(x), ld, fptr(w), fptr(b), ptr(st), at_of(y), (int)B, (int)D, (int)W, dt, stream(), a[4] == Py_True ? KLA_LAYER_SILU : 0);
     }
     if (rc != KLA_OK) return PyLong_FromLong(rc);
+    written({st, out});
     return wrap(y);
     END_HANDLE_TH_ERRORS
 }
@@ -409,6 +411,7 @@ PyObject* ssm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
         const NoGil no_gil;
         c.fwd(y, hT, a[12] == Py_True, at::Tensor());
     } catch (const Refused& e) { return PyLong_FromLong(e.code); }
+    written({out, last});
     return pair(y, hT);
     END_HANDLE_TH_ERRORS
 }
@@ -450,6 +453,7 @@ PyObject* ssm_step(PyObject*, PyObject* const* a, Py_ssize_t n)
                           fptr(h), at_of(y), (int)c.N, (int)c.D, (int)c.G, (int)c.S, c.dt, stream(), c.opts);
     }
     if (rc != KLA_OK) return PyLong_FromLong(rc);
+    written({h, out});
     return wrap(y);
     END_HANDLE_TH_ERRORS
 }
@@ -543,6 +547,7 @@ PyObject* add_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
         const NoGil no_gil;
         c.fwd(y, r);
     } catch (const Refused& e) { return PyLong_FromLong(e.code); }
+    written({out, r2});
     return pair(y, r);
     END_HANDLE_TH_ERRORS
 }
@@ -641,6 +646,7 @@ PyObject* gated_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
         const NoGil no_gil;
         c.fwd(y);
     } catch (const Refused& e) { return PyLong_FromLong(e.code); }
+    written({out});
     return wrap(y);
     END_HANDLE_TH_ERRORS
 }

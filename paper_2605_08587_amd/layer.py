@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from . import KlaError, _binding, _check, _dev, _dt, _host_cu, _ptr, _stream, _ws_bytes, lib
+from . import KlaError, _binding, _check, _dev, _dt, _host_cu, _ptr, _stream, _written, _ws_bytes, lib
 
 KLA_LAYER_SILU, KLA_LAYER_SOFTPLUS, KLA_LAYER_SIGMOID, KLA_LAYER_GATE_FIRST = 1, 2, 4, 8
 
@@ -170,12 +170,14 @@ def kla_conv_fwd(x, weight, bias=None, state=None, cu_seqlens=None, cu_seqlens_h
     N, T, D, W, dt, st, (_, cu_hp, n_seq, _n) = _conv_check(x, weight, bias, state, cu_seqlens, host, out=(out, "y", None),
                                                          state_out=(state_out, "state", None))
     ld = _rows("x", x)
+    given = out, state_out
     if out is None:
         out = torch.empty((N, T, D), dtype=x.dtype, device=x.device)
     if state_out is None and want_state:
         state_out = torch.empty(st, dtype=x.dtype, device=x.device)
     _call("kla_conv_fwd", _ptr(x), ld, _ptr(weight), _ptr(bias), _ptr(state), _ptr(out), _ptr(state_out), _ptr(cu_seqlens), cu_hp, n_seq,
           N, T, D, W, dt, _stream(), KLA_LAYER_SILU if silu else 0)
+    _written(*given)
     return out, state_out
 
 
@@ -213,9 +215,11 @@ def kla_conv_step(x, weight, state, bias=None, silu=True, out=None):
     _on_gpu(x, weight, bias, state, out)
     _dev(weight, bias, state, out)
     ld = _rows("x", x)
+    given = out
     if out is None:
         out = torch.empty((B, D), dtype=x.dtype, device=x.device)
     _call("kla_conv_step", _ptr(x), ld, _ptr(weight), _ptr(bias), _ptr(state), _ptr(out), B, D, W, dt, _stream(), KLA_LAYER_SILU if silu else 0)
+    _written(state, given)
     return out
 
 
@@ -296,6 +300,7 @@ def kla_ssm_fwd(u, delta, A, B, C, skip=None, z=None, delta_bias=None, softplus=
     _dev(h0, cu_seqlens, out, hT, workspace)
     if workspace is None:
         workspace = _workspace(int(lib().kla_ssm_fwd_workspace_bytes(N, T, D, G, S, cu_hp, n_seq)), u)
+    given = out, hT
     if out is None:
         out = torch.empty((N, T, D), dtype=u.dtype, device=u.device)
     if hT is None and want_hT:
@@ -303,6 +308,7 @@ def kla_ssm_fwd(u, delta, A, B, C, skip=None, z=None, delta_bias=None, softplus=
     _call("kla_ssm_fwd", *_ssm_in(u, delta, A, B, C, skip, z, delta_bias, ld), _ptr(h0), _ptr(out), _ptr(hT), _ptr(_saved), _ws_bytes(_saved),
           _ptr(cu_seqlens), cu_hp, n_seq, N, T, D, G, S, dt, _ptr(workspace), _ws_bytes(workspace), _stream(),
           KLA_LAYER_SOFTPLUS if softplus else 0)
+    _written(*given)
     return out, hT
 
 
@@ -344,10 +350,12 @@ def kla_ssm_step(u, delta, A, B, C, h, skip=None, z=None, delta_bias=None, softp
     _check("out", out, (N, D), u.dtype)
     _on_gpu(h, out)
     _dev(h, out)
+    given = out
     if out is None:
         out = torch.empty((N, D), dtype=u.dtype, device=u.device)
     _call("kla_ssm_step", *_ssm_in(u, delta, A, B, C, skip, z, delta_bias, ld), _ptr(h), _ptr(out), N, D, G, S, dt, _stream(),
           KLA_LAYER_SOFTPLUS if softplus else 0)
+    _written(h, given)
     return out
 
 
@@ -422,12 +430,14 @@ def kla_add_norm_fwd(x, weight, residual=None, scale=None, eps=1e-6, residual_dt
             return r
     D, dt, res_dt, res_type = _add_norm_check(x, weight, residual, scale, residual_dtype, out=(out, None), residual_out=(residual_out, "r"))
     ld = _rows("x", x)
+    given = out, residual_out
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if residual_out is None:
         residual_out = torch.empty(x.shape, dtype=res_type, device=x.device)
     _call("kla_add_norm_fwd", _ptr(x), ld, _ptr(residual), _ptr(scale), _ptr(weight), float(eps), _ptr(out), _ptr(residual_out),
           x.numel() // D if D else 0, D, dt, res_dt, _stream())
+    _written(*given)
     return out, residual_out
 
 
@@ -503,9 +513,11 @@ def kla_gated_norm_fwd(x, gate, weight, eps=1e-6, activation="silu", gate_first=
     if r is not None:
         return r
     H, D, M, dt, ld_x, ld_gate, bits = _gated_norm_check(x, gate, weight, activation, gate_first, out=out)
+    given = out
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     _call("kla_gated_norm_fwd", _ptr(x), ld_x, _ptr(gate), ld_gate, _ptr(weight), float(eps), _ptr(out), M, H, D, dt, _stream(), bits)
+    _written(given)
     return out
 
 

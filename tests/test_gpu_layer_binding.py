@@ -144,3 +144,56 @@ def test_inputs_changed_before_the_backward(kla):
     z.mul_(2)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_what_a_call_writes_counts_as_changed(kla, monkeypatch, native):
+    """A tensor that a differentiable call saved and another call then writes in place: the backward refuses, as after torch's own."""
+    if not native:
+        monkeypatch.setattr(kla, "_native", kla._StepByStep)
+    d, _ = _inputs(torch.float32, False, False)
+    x, A, B, C, w, b = d["x"], d["A"], d["B"], d["C"], d["w"], d["b"]
+    xs, ws = x.detach().requires_grad_(True), w.detach().clone().requires_grad_(True)
+    heads = lambda t: t.unflatten(-1, (5, -1))  # noqa: E731
+
+    def conv(**kw):
+        return lambda t: kla.kla_conv(xs, w, b, t, **kw)[0]
+
+    def ssm(**kw):
+        return lambda t: kla.kla_ssm(xs, x, A, B, C, h0=t, **kw)[0]
+    like = lambda t: lambda: t.clone()  # noqa: E731
+    cases = {
+        "conv_step state": (like(d["st"]), conv(), lambda t: kla.kla_conv_step(x[:, 0], w, t, b)),
+        "conv_fwd state_out": (like(d["st"]), conv(), lambda t: kla.kla_conv_fwd(x, w, b, state_out=t)),
+        "conv_fwd out": (like(x), lambda t: kla.kla_conv(t, ws)[0],
+                         lambda t: kla.kla_conv_fwd(x, w, out=t)),
+        "conv_step out": (like(x[:, 0]), lambda t: kla.kla_conv(t[:, None], ws)[0],
+                          lambda t: kla.kla_conv_step(x[:, 0], w, d["st"].clone(), out=t)),
+        "ssm_step h": (like(d["h0"]), ssm(), lambda t: kla.kla_ssm_step(x[:, 0], x[:, 1], A, B[:, 0], C[:, 0], t)),
+        "ssm_fwd hT": (like(d["h0"]), ssm(save=False), lambda t: kla.kla_ssm_fwd(x, x, A, B, C, h0=t, hT=t)),
+        "ssm_fwd out": (like(x), lambda t: kla.kla_ssm(xs, t, A, B, C)[0], lambda t: kla.kla_ssm_fwd(x, x, A, B, C, out=t)),
+        "ssm_step out": (like(x[:, 0]), lambda t: kla.kla_ssm(xs[:, :1], t[:, None], A, B[:, :1], C[:, :1])[0],
+                         lambda t: kla.kla_ssm_step(x[:, 0], x[:, 1], A, B[:, 0], C[:, 0], d["h0"].clone(), out=t)),
+        "add_norm_fwd residual_out": (like(d["res"]), lambda t: kla.kla_add_norm(xs, b, t)[0], lambda t: kla.kla_add_norm_fwd(x, b, t, residual_out=t)),
+        "add_norm_fwd out": (like(x), lambda t: kla.kla_add_norm(t, b, xs)[0], lambda t: kla.kla_add_norm_fwd(x, b, out=t)),
+        "gated_norm_fwd out": (like(heads(x).contiguous()), lambda t: kla.kla_gated_norm(heads(xs), t, d["w5"]),
+                               lambda t: kla.kla_gated_norm_fwd(heads(x), heads(x), d["w5"], out=t)),
+    }
+    for name, (make, use, write) in cases.items():
+        t = make()
+        y = use(t)
+        y.sum().backward()                               # (nothing has changed yet)
+        y = use(t)
+        before = t._version
+        write(t)
+        assert t._version > before, name
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    # a tensor that counts nothing, and one that nobody saved, are written as before
+    with torch.inference_mode():
+        st, h = d["st"].clone(), d["h0"].clone()
+    kla.kla_conv_step(x[:, 0], w, st, b)
+    kla.kla_ssm_step(x[:, 0], x[:, 1], A, B[:, 0], C[:, 0], h)
+    with torch.inference_mode():
+        kla.kla_conv_step(x[:, 0], w, st, b)
+        kla.kla_conv_step(x[:, 0], w, d["st"], b)
