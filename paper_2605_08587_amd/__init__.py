@@ -304,6 +304,7 @@ def kla_chunk_fwd(q, k, v, log_alpha, eta, eps, h0=None, cu_seqlens=None, want_h
         if normalize_q or gdn_beta:
             raise ValueError("the single-stage hook takes no options")
         bits = KLA_TUNE_UNFUSED
+    given = out, hT
     if workspace is None:
         need = int(lib().kla_chunk_fwd_workspace_bytes_opts(N, T, H, dk, dv, chunk, dt, cu_hp, n_seq, bits & ~3))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
@@ -324,6 +325,7 @@ def kla_chunk_fwd(q, k, v, log_alpha, eta, eps, h0=None, cu_seqlens=None, want_h
         rc = lib().kla_chunk_fwd(*args)
     if rc != 0:
         raise KlaError(rc, "kla_chunk_fwd")
+    _written(*given)
     return out, hT
 
 
@@ -348,6 +350,7 @@ def kla_chunk_fwd_static(q, k, v, log_alpha, eta, eps, out, hT=None, h0=None, cu
                                     _ptr(hT), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, dk, dv, chunk, _dt(q), _stream())
     if rc != 0:
         raise KlaError(rc, "kla_chunk_fwd_static")
+    _written(out, hT)
     return out, hT
 
 
@@ -366,6 +369,7 @@ def kla_chunk_fwd_diag(q, k, v, log_alpha, eta, eps, h0=None, cu_seqlens=None, w
                                    hT=(hT, (n_states, q.shape[2], q.shape[3], v.shape[-1]), torch.float32))
     _dev(q, k, v, log_alpha, eta, h0, cu_seqlens, workspace, out, hT)
     dt = _dt(q)
+    given = out, hT
     need = int(lib().kla_chunk_fwd_diag_workspace_bytes(N, T, H, dk, dv, chunk, dt, cu_hp, n_seq))
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
@@ -380,6 +384,7 @@ def kla_chunk_fwd_diag(q, k, v, log_alpha, eta, eps, h0=None, cu_seqlens=None, w
     rc = lib().kla_chunk_fwd_diag_opts(*args, bits) if bits else lib().kla_chunk_fwd_diag(*args)
     if rc != 0:
         raise KlaError(rc, "kla_chunk_fwd_diag")
+    _written(*given)
     return out, hT
 
 
@@ -393,6 +398,7 @@ def kla_decode_step_diag(q, k, v, log_alpha, eta, eps, S, out=None, normalize_q=
         return r
     B, H, dk, dv = _check_decode(q, k, v, log_alpha, eta, S, out, la_shape=tuple(q.shape))
     _dev(q, k, v, log_alpha, eta, S, out)
+    given = out
     if out is None:
         out = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
     args = (_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(eta), float(eps), _ptr(S), _ptr(out), B, H, dk, dv, _dt(q),
@@ -400,6 +406,7 @@ def kla_decode_step_diag(q, k, v, log_alpha, eta, eps, S, out=None, normalize_q=
     rc = lib().kla_decode_step_diag_opts(*args, bits) if bits else lib().kla_decode_step_diag(*args)
     if rc != 0:
         raise KlaError(rc, "kla_decode_step_diag")
+    _written(S, given)
     return out
 
 
@@ -431,6 +438,7 @@ def kla_chunk_bwd(q, k, v, log_alpha, eta, eps, d_o, h0=None, d_hT=None, cu_seql
     cu_host, cu_hp, n_seq = _host_cu(cu_seqlens, cu_seqlens_host)
     n_states = n_seq if n_seq > 0 else q.shape[0]
     out = dict(out or {})
+    given = tuple(out.values())
     sq, sv, sg, ss = tuple(q.shape), tuple(q.shape[:3]) + (v.shape[-1],), tuple(q.shape[:3]), (n_states, q.shape[2], q.shape[3], v.shape[-1])
     N, T, H, dk, dv = _check_chunk(q, k, v, log_alpha, eta, h0, n_states, d_o=(d_o, sv, q.dtype), d_hT=(d_hT, ss, torch.float32),
                                    dq=(out.get("dq"), sq, q.dtype), dk=(out.get("dk"), sq, q.dtype),
@@ -465,6 +473,7 @@ def kla_chunk_bwd(q, k, v, log_alpha, eta, eps, d_o, h0=None, d_hT=None, cu_seql
         rc = lib().kla_chunk_bwd_opts(*args, _stream(), bits) if bits else lib().kla_chunk_bwd(*args, _stream())
     if rc != 0:
         raise KlaError(rc, "kla_chunk_bwd")
+    _written(*given)
     return out
 
 
@@ -485,6 +494,7 @@ def kla_decode_step(q, k, v, log_alpha, eta, eps, S, out=None, normalize_q=False
         return r
     B, H, dk, dv = _check_decode(q, k, v, log_alpha, eta, S, out)
     _dev(q, k, v, log_alpha, eta, S, out)
+    given = out
     if out is None:
         out = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
     args = (_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(eta), float(eps), _ptr(S), _ptr(out),
@@ -492,6 +502,7 @@ def kla_decode_step(q, k, v, log_alpha, eta, eps, S, out=None, normalize_q=False
     rc = lib().kla_decode_step_opts(*args, bits) if bits else lib().kla_decode_step(*args)
     if rc != 0:
         raise KlaError(rc, "kla_decode_step")
+    _written(S, given)
     return out
 
 
@@ -503,11 +514,13 @@ def kla_beta(k, eta, eps, out=None):
     _check("eta", eta, tuple(k.shape[:-1]), torch.float32)
     _check("out", out, tuple(k.shape[:-1]), torch.float32)
     _dev(k, eta, out)
+    given = out
     if out is None:
         out = torch.empty(k.shape[:-1], dtype=torch.float32, device=k.device)
     rc = lib().kla_beta(_ptr(k), _ptr(eta), float(eps), _ptr(out), n, dk, _dt(k), _stream())
     if rc != 0:
         raise KlaError(rc, "kla_beta")
+    _written(given)
     return out
 
 

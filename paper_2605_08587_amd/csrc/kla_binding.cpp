@@ -130,6 +130,7 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n)
                                                    (int)H, (int)dk, (int)dv, dt, stream(), (unsigned)opts);
     }
     if (rc != KLA_OK) return PyLong_FromLong(rc);
+    written({S, out});
     return THPVariable_Wrap(o);
     END_HANDLE_TH_ERRORS
 }
@@ -169,6 +170,7 @@ PyObject* chunk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
                                              c.dt, ws.data_ptr(), ws.nbytes(), stream(), (unsigned)opts);
     }
     if (rc != KLA_OK) return PyLong_FromLong(rc);
+    written({out_, hT_});
     PyObject* r = PyTuple_New(2);
     if (!r) return nullptr;
     PyTuple_SET_ITEM(r, 0, wrap(out));
