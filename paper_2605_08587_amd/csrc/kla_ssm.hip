@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void ssm_join_kernel(SsmArgs<T> a, int S)
     const Place p = sequence(a.seqs, blockIdx.y);
     const long base = first_slot(a, p);
     const long n = (p.end - p.first + a.Lseg - 1) / a.Lseg;
-    const float A2 = kLog2e * a.A[e];
+    const float A2 = rate(a.A[e]);
     const int c = (int)(e / S);
     float h = a.h0 ? a.h0[p.n * DS + e] : 0.f;
     constexpr int AHEAD = 8;                             // reads of so many segments at once
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmArgs<T> a, float* __re
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int n = q * K + k;
-        h[k] = fmaf(exp2_hw(delta * (kLog2e * a.A[(long)c * S + n])), h[k], du * to_float(a.B[b * a.ld_B + g * S + n]));
+        h[k] = fmaf(exp2_hw(delta * rate(a.A[(long)c * S + n])), h[k], du * to_float(a.B[b * a.ld_B + g * S + n]));
         s = fmaf(to_float(a.C[b * a.ld_C + g * S + n]), h[k], s);
         st[k] = h[k];
     }

@@ -288,7 +288,7 @@ __global__ __launch_bounds__(256) void ssm_join_bwd_kernel(SsmArgs<T> a, int S)
     const Place p = sequence(a.seqs, blockIdx.y);
     const long base = first_slot(a, p);
     const long n = (p.end - p.first + a.Lseg - 1) / a.Lseg;
-    const float A2 = kLog2e * a.A[e];
+    const float A2 = rate(a.A[e]);
     const int c = (int)(e / S);
     float g = a.d_hT ? a.d_hT[p.n * DS + e] : 0.f;
     constexpr int AHEAD = 8;                             // reads of so many segments at once

@@ -208,17 +208,19 @@ template <int K> __device__ __forceinline__ void load_states(float (&h)[K], cons
         }
     }
 }
-// log2(e) A of a lane's states.  A state that forgets at once (A = -inf) has the lowest number in its place: a token that is none, with a
+// log2(e) A of a state.  One that forgets at once (A = -inf) has the lowest number in its place: a token that is none, with a
 // step of 0, then leaves it as it is and does not make it 0 * inf.
-template <int K> __device__ __forceinline__ void load_rates(float (&A2)[K], const float* p)
+__device__ __forceinline__ float rate(float A)
 {
     constexpr float kMost = 3.402823466e38f;
+    const float A2 = kLog2e * A;
+    return fabsf(A2) > kMost ? copysignf(kMost, A2) : A2;                // (a NaN stays one)
+}
+template <int K> __device__ __forceinline__ void load_rates(float (&A2)[K], const float* p)
+{
     load_states<K>(A2, p);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        A2[k] *= kLog2e;
-        if (fabsf(A2[k]) > kMost) A2[k] = copysignf(kMost, A2[k]);       // (false for NaN)
-    }
+    for (int k = 0; k < K; ++k) A2[k] = rate(A2[k]);
 }
 template <int K> __device__ __forceinline__ void store_states(float* p, const float (&h)[K])
 {

@@ -267,3 +267,48 @@ def test_offsets_beyond_32_bits(kla):
     t = kla.kla_ssm_bwd(part[0], part[0], A, part[1], part[2], y[:, cut:].contiguous(), z=part[0], h0=mid)
     for k in ("du", "ddelta", "dz", "dB", "dC"):
         _close_runs(k, g[k][:, cut:], t[k])
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_steps_of_zero_where_states_forget_at_once(kla, packed):
+    """A = -inf in some places and steps of 0, in whole segments too: a step of 0 leaves every state as it is, in segments, in one piece and
+    token by token."""
+    D, S, T = 72, 16, 640
+    g, d, dev = _inputs(torch.float32, (1, T), 2 if packed else 1, D, 1, S, ("skip", "h0"), False, 79)
+    d["delta"] = d["delta"].abs()
+    d["delta"][:, 100:420] = 0                           # (segments of 64 tokens: the third to the sixth have no other step)
+    d["delta"][:, 500:] = 0
+    flat = {k: v if v is None or k in ("A", "skip", "h0") else v.flatten(0, 1) for k, v in d.items()}
+    flat["A"] = d["A"].clone()
+    flat["A"][::3, 5:] = -1e30                           # (the same in 64 bits, and with gradients that exist)
+    dev["A"] = flat["A"].clamp(min=-1e29).cuda()
+    dev["A"][dev["A"] < -1e28] = float("-inf")
+    dev["delta"] = d["delta"].cuda()
+    cu = offsets([300, 340]) if packed else None
+    kw = dict(softplus=False, **(dict(cu_seqlens=cu.cuda(), cu_seqlens_host=cu) if packed else {}))
+    seqs = lo.sequences(1, T, cu)
+    dy, dh = randn(g, 1, T, D), randn(g, len(seqs), D, S)
+    (y_ref, h_ref), g_ref = lo.gradients(lambda **k: lo.ssm(**k, softplus=False, seqs=seqs), flat, (dy[0], dh))
+    assert kla.lib().kla_ssm_fwd_workspace_bytes(1, T, D, 1, S, None if cu is None else cu.data_ptr(), 2 if packed else 0) > 0      # in segments
+    y, hT = kla.kla_ssm_fwd(**dev, **kw)
+    gr = kla.kla_ssm_bwd(**dev, d_y=dy.cuda(), d_hT=dh.cuda(), **kw)
+    close("y", y[0], y_ref, SCAN)
+    close("hT", hT, h_ref, SCAN)
+    for k in g_ref:
+        got, ref = gr["d" + k].reshape(g_ref[k].shape).cpu(), g_ref[k]
+        if k == "delta":                                 # exp(step A) has no derivative at a step of 0 where A = -inf
+            none = (d["delta"][0] == 0) & torch.isinf(dev["A"].cpu()).any(1)
+            got, ref = got.masked_fill(none, 0), ref.masked_fill(none, 0)
+        close("d" + k, got, ref, SCAN)
+    h = dev["h0"][:1].clone()
+    for t in (0, 1, 100, 101, 500):
+        if t == 100:                                     # (the states of the tokens between)
+            x = {k: v[:, 2:100].contiguous() if k in ("u", "delta", "B", "C") else v for k, v in dev.items()}
+            h = kla.kla_ssm_fwd(**dict(x, h0=h), softplus=False)[1]
+        if t == 500:
+            x = {k: v[:, 102:500].contiguous() if k in ("u", "delta", "B", "C") else v for k, v in dev.items()}
+            h = kla.kla_ssm_fwd(**dict(x, h0=h), softplus=False)[1]
+        x = {k: v[:, t] for k, v in dev.items() if k in ("u", "delta", "B", "C")}
+        ys = kla.kla_ssm_step(**x, A=dev["A"], skip=dev["skip"], h=h, softplus=False)
+        if t < 300 or not packed:
+            close("step %d" % t, ys[0], y_ref[t], SCAN)
