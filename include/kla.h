@@ -422,7 +422,8 @@ int kla_ssm_step(const void *u, long ld_u, const void *delta, long ld_delta, con
 
 /*
  * Before a block: the residual stream plus the scaled output of the block before, and its RMS norm.
- *     r' = residual + scale x,   y = weight r' / sqrt(mean(r'^2) + eps)        (0 for a row of zeros with eps = 0)
+ *     r' = residual + scale x,   y = weight r' / sqrt(mean(r'^2) + eps)        (0 for a row of zeros with eps = 0;
+ * the squares are fp32: elements below 2^-75 count as zeros there, and a row's sum of squares has to stay below 2^128)
  *   x           [M, D] dt, rows ld_x apart          in
  *   residual    [M, D] res_dt                       in   or NULL: r' = scale x
  *   scale       [D] or NULL for ones, weight [D]    in

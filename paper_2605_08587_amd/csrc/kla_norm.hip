@@ -31,11 +31,14 @@ template <int TPR> __device__ __forceinline__ float row_sum(float x, float* red)
         return s;
     }
 }
-// 1/sqrt(mean + eps); 0 for a row of zeros with eps = 0, whose norm is then zeros and not 0/0
+// 1/sqrt(mean + eps); 0 for a row of zeros with eps = 0, whose norm is then zeros and not 0/0.  The hardware's root takes a denormal for 0
+// and gives infinity: such a mean is brought into its range first.
 __device__ __forceinline__ float inv_rms(float sum, float inv_d, float eps)
 {
     const float m = fmaf(sum, inv_d, eps);
-    return m == 0.f ? 0.f : __builtin_amdgcn_rsqf(m);
+    const bool low = m < 0x1p-126f;
+    const float f = __builtin_amdgcn_rsqf(low ? m * 0x1p64f : m);
+    return m == 0.f ? 0.f : low ? f * 0x1p32f : f;
 }
 // the activated gate and its derivative
 __device__ __forceinline__ void gate_of(float t, bool plain_sigmoid, float* g, float* slope)

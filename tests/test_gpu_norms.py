@@ -192,3 +192,29 @@ def test_in_place_where_waves_share_columns(kla):
             assert rc == 0
             for k, t in (("dx", dx), ("dresidual", dr), ("dscale", ds), ("dweight", dw)):
                 assert torch.equal(bits(own[k]), bits(t)), k
+
+
+@pytest.mark.parametrize("D", [5, 64, 1000, 2048])
+def test_rows_whose_squares_are_denormal(kla, D):
+    """eps = 0 and rows so small that the mean of their squares has no leading 1 in fp32: normalised like any other.  Squares that fp32 cannot hold at all
+    make a row of zeros."""
+    g = torch.Generator().manual_seed(D)
+    x, w, gate = randn(g, 7, D), randn(g, D), randn(g, 7, D)
+    size = torch.tensor([1.0, 1e-18, 3e-20, 1e-20, 3e-21, 1e-21, 1e-26])[:, None]
+    x = (x.sign() * (0.5 + x.abs())) * size
+    print("norms", D, flush=True)
+    y, _ = kla.kla_add_norm_fwd(x.cuda(), w.cuda(), eps=0.0)
+    z = kla.kla_gated_norm_fwd(x[:, None].cuda(), gate[:, None].cuda(), w.cuda(), eps=0.0, activation="sigmoid")
+    ref = lo.add_norm(x.double(), w.double(), None, None, 0.0)[0]
+    ref_z = lo.gated_norm(x.double(), gate.double(), w.double(), 0.0, "sigmoid", False)
+    for i in range(6):
+        # an element's square rounds to a multiple of 2^-149, by half of one at most: against a mean square of at least size^2 / 4
+        b = SUMS + 0.5 * 2.0 ** -149 / (float(size[i]) ** 2 / 4)
+        close("y %d" % i, y[i], ref[i], b)
+        close("gated %d" % i, z[i, 0], ref_z[i], b)
+    assert not y[6].any() and not z[6].any()
+    dx = kla.kla_add_norm_bwd(x[:4].cuda(), w.cuda(), (gate[:4] * size[:4]).cuda(), eps=0.0)["dx"]
+    _, ref = lo.gradients(lambda x: lo.add_norm(x, w.double(), None, None, 0.0)[0], dict(x=x[:4]), ((gate * size)[:4],))
+    for i in range(4):
+        if D > 7:                                        # (narrow rows: what is left of terms that cancel)
+            close("dx %d" % i, dx[i], ref["x"][i], 4 * (SUMS + 0.5 * 2.0 ** -149 / (float(size[i]) ** 2 / 4)))
