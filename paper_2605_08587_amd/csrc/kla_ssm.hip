@@ -81,7 +81,9 @@ __global__ __launch_bounds__(THREADS, MODE == kSsmMaps && S == 64 ? 2 : 1) void 
     };
     auto tile = [&](auto which, int at) {
         constexpr int w = which.value;
+        const int left = tokens - at;
         bc.store(lds[w], in_bc[w]);
+        if (MODE != kSsmMaps && left < kTok) bc.clear(lds[w], left);     // (a segment that another follows has whole tiles)
         float u[NG], raw[NG], z[NG], y[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
@@ -96,7 +98,6 @@ __global__ __launch_bounds__(THREADS, MODE == kSsmMaps && S == 64 ? 2 : 1) void 
         }
         __syncthreads();
         load(which);
-        const int left = tokens - at;
         const float* row = lds[w] + o * 2 * K;
         // In steps, in this order: what eight tokens need from LDS is on its way while steps, gates and decays are formed, and the chain of
         // states finds everything at hand.  (Left to itself the compiler reads each row where it is used and waits.)

@@ -96,6 +96,7 @@ __global__ __launch_bounds__(kSsmBwdChannels * 8, S < 64 && sizeof(T) == 4 ? 2 :
         constexpr bool FULL = full.value != 0;
         const int w = tile & 1, left = FULL ? CK : min(tokens - tile * CK, CK);
         bc.store(lds[w], in_bc);
+        if (!FULL && left < CK) bc.clear(lds[w], left);
         float u[NG], raw[NG], z[NG], dy[NG], delta[NG], dc[NG], core[NG];
         float h[MAPS ? 1 : CK + 1][K];
 #pragma unroll
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(kSsmBwdChannels * 8, S < 64 && sizeof(T) == 4 ? 2 :
                         val[K + k] = uj * gk;
                         sb = fmaf(gk, m.b[k], sb);
                         sa = fmaf(e, A2[k], sa);
-                        dA[k] = fmaf(e, dj, dA[k]);
+                        if (FULL || n < left) dA[k] = fmaf(e, dj, dA[k]);    // (e may be infinite where dj is 0)
                     }
                     via_a[j] = sa;
                     via_b[j] = sb;
@@ -227,8 +228,8 @@ __global__ __launch_bounds__(kSsmBwdChannels * 8, S < 64 && sizeof(T) == 4 ? 2 :
                     const float s = sigmoid(z[i]);
                     out_z = rounded<T>(dy[i] * core[i] * (s * fmaf(z[i], 1.f - s, 1.f)));
                 }
-                d_skip = fmaf(dc[i], u[i], d_skip);      // (0 where there is no token or channel)
                 if (FULL || (8 * i + o < left && ch.mine)) {
+                    d_skip = fmaf(dc[i], u[i], d_skip);
                     d_bias += d_raw;
                     qu.store(i, out_u);
                     qd.store(i, out_d);

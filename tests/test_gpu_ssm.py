@@ -312,3 +312,39 @@ def test_steps_of_zero_where_states_forget_at_once(kla, packed):
         ys = kla.kla_ssm_step(**x, A=dev["A"], skip=dev["skip"], h=h, softplus=False)
         if t < 300 or not packed:
             close("step %d" % t, ys[0], y_ref[t], SCAN)
+
+
+@pytest.mark.parametrize("T", [21, 333])
+@pytest.mark.parametrize("what", ["B", "C", "u"])
+def test_infinities_in_the_last_token(kla, T, what):
+    """An infinity in the last token of a sequence that ends inside a tile is that token's: what is read in the place of the tokens that are not there makes
+    no NaN of it, in the states, the outputs or what its gradient does not reach."""
+    D, S, at = 40, 16, 3
+    g, d, dev = _inputs(torch.float32, (1, T), 1, D, 1, S, ALL, False, 80)
+    d["u"] = d["u"].abs() + 0.1
+    if what == "u":
+        d["u"][0, -1, at] = float("inf")
+        d["B"][0, -1, 0] = d["B"][0, -1, 0].abs() + 0.1
+        d["C"][0, -1, 0] = d["C"][0, -1, 0].abs() + 0.1
+    else:
+        d[what][0, -1, 0, at] = float("inf")
+    dev.update({k: d[k].cuda() for k in ("u", "B", "C")})
+    flat = {k: v if v is None or k in ("A", "skip", "delta_bias", "h0") else v.flatten(0, 1) for k, v in d.items()}
+    dy, dh = randn(g, 1, T, D), randn(g, 1, D, S)
+    (y_ref, h_ref), g_ref = lo.gradients(lambda **k: lo.ssm(**k, softplus=True, seqs=[(0, T)]), flat, (dy[0], dh))
+    y, hT = kla.kla_ssm_fwd(**dev)
+    gr = kla.kla_ssm_bwd(**dev, d_y=dy.cuda(), d_hT=dh.cuda())
+
+    def same(name, p, ref):
+        p, ref = p.cpu().reshape(ref.shape), ref
+        wild = ~torch.isfinite(ref)
+        assert torch.equal(p[wild].double().nan_to_num(7, 1, -1), ref[wild].nan_to_num(7, 1, -1)), name
+        close(name, p.masked_fill(wild, 0), ref.masked_fill(wild, 0), SCAN)
+    same("y", y, y_ref)
+    same("hT", hT, h_ref)
+    same("dskip", gr["dskip"], g_ref["skip"])
+    if what != "C":                                      # the infinity is not part of the states before it, nor of their gradients
+        same("dA", gr["dA"], g_ref["A"])
+        same("dh0", gr["dh0"], g_ref["h0"])
+    elif T < 100:                                        # (over more tokens the decays of such a state leave fp32's range: 0 times infinity)
+        same("dh0", gr["dh0"], g_ref["h0"])
