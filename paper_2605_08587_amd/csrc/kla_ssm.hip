@@ -110,7 +110,7 @@ __global__ __launch_bounds__(THREADS, MODE == kSsmMaps && S == 64 ? 2 : 1) void 
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const bool in = 8 * i + o < left;
-            const float soft = softplus(raw[i]);
+            const float soft = softplus<T>(raw[i]);
             delta[i] = where(in, a.softplus ? soft : raw[i]);
             du[i] = where(in, delta[i] * u[i]);
             if constexpr (HASZ) gate[i] = z[i] * sigmoid(z[i]);
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmArgs<T> a, float* __re
     for (int k = 0; k < K; ++k) h[k] = st[k];
     const float u = to_float(a.u[b * a.ld_u + c]);
     const float raw = to_float(a.delta[b * a.ld_delta + c]) + (a.delta_bias ? a.delta_bias[c] : 0.f);
-    const float delta = a.softplus ? softplus(raw) : raw, du = delta * u;
+    const float delta = a.softplus ? softplus<T>(raw) : raw, du = delta * u;
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {

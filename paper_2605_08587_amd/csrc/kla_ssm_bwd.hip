@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kSsmBwdChannels * 8, S < 64 && sizeof(T) == 4 ? 2 :
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const bool live = FULL || 8 * i + o < left, own = FULL || (live && ch.mine);
-            const float soft = softplus(raw[i]);
+            const float soft = softplus<T>(raw[i]);
             delta[i] = where(live, a.softplus ? soft : raw[i]);
             float gate = 1.f;
             if constexpr (HASZ) gate = z[i] * sigmoid(z[i]);

@@ -348,3 +348,24 @@ def test_infinities_in_the_last_token(kla, T, what):
         same("dh0", gr["dh0"], g_ref["h0"])
     elif T < 100:                                        # (over more tokens the decays of such a state leave fp32's range: 0 times infinity)
         same("dh0", gr["dh0"], g_ref["h0"])
+
+
+def test_steps_to_the_last_digits(kla):
+    """softplus of the steps in fp32, seen through one token with maps of ones (y is S times the step): relative to the step itself, from e^-85 to 100, and
+    at the values that are none.  Bar: units of 2^-23 of two hardware functions, eight roundings of 2^-24, and the fp32 constant of 2.8e-9 |x|."""
+    D, S = 4096, 8
+    raw = torch.linspace(-85, 100, D - 8)
+    raw = torch.cat([raw, torch.tensor([float("inf"), float("-inf"), float("nan"), 3.4e38, -3.4e38, 0.0, -0.0, 1e-30])])
+    one, A = torch.ones(1, 1, 1, S, device="cuda"), -torch.ones(D, S, device="cuda")
+    u, d = torch.ones(1, 1, D, device="cuda"), raw.cuda()[None, None]
+    y, _ = kla.kla_ssm_fwd(u, d, A, one, one)
+    z = kla.kla_ssm_step(u[0], d[0], A, one[0], one[0], torch.zeros(1, D, S, device="cuda"))
+    ref = torch.logaddexp(raw.double(), torch.zeros(D, dtype=torch.float64))
+    bar = 2 * 2.0 ** -23 + 8 * 2.0 ** -24 + 2.8e-9 * raw.double().abs()
+    for t in (y[0, 0], z[0]):
+        t = t.cpu().double() / S
+        ok = (S * ref < 3.4e38) & (ref > 0)              # (what y holds: 8 times 3.4e38 is infinite)
+        off = ((t - ref).abs() / ref)[ok]
+        worst = int((off / bar[ok]).argmax())
+        assert (off <= bar[ok]).all(), (float(raw[ok][worst]), float(off[worst]))
+        assert t[-8] == t[-5] == float("inf") and t[-7] == t[-4] == 0 and torch.isnan(t[-6])
