@@ -387,7 +387,8 @@ int kla_conv_step(const void *x, long ld_x, const float *weight, const float *bi
  *   y           [N, T, D] dt                                            out
  *   hT          [n_states, D, S] fp32                                   out  or NULL; may alias h0
  *   saved       kla_ssm_saved_bytes(...): the states at every 16th token (every 8th from S = 32 on), for the backward; or NULL
- * S in {8, 16, 32, 64}; D a multiple of G; D and the row strides at most 2^24; at most 65535 sequences and groups.
+ * S in {8, 16, 32, 64}; D a multiple of G; D and the row strides at most 2^24; at most 65535 sequences and groups (kla_ssm_step: any
+ * strides, number of sequences and groups).
  */
 size_t kla_ssm_fwd_workspace_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq);
 size_t kla_ssm_saved_bytes(int N, int T, int D, int G, int S, const int32_t *cu_seqlens_host, int n_seq);

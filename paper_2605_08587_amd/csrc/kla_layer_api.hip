@@ -78,7 +78,7 @@ template <typename T> kla::ConvArgs<T> conv_args(const void* x, long ld_x, const
 }
 
 // ---- selective scan ---------------------------------------------------------------------------------------------------------------
-// (a lane's offset from the first of 16 rows fits 32 bits)
+// (a lane's offset from the first of 16 rows fits 32 bits; a step has one row of a sequence and no such offsets)
 constexpr int kMaxSsmRow = 1 << 24;
 constexpr int kMaxSsmSeqs = 65535;                       // sequences, and groups: a launch's second dimension
 bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
@@ -150,12 +150,11 @@ SsmWork ssm_work(char* base, const kla::Seqs& s, const SsmPlan& p, long M, int D
     return w;
 }
 int ssm_check(const void* u, long ld_u, const void* delta, long ld_delta, const float* A, const void* B, long ld_B, const void* C, long ld_C, const void* z,
-              long ld_z, int D, int G, int S, int dt, unsigned opts)
+              long ld_z, int D, int G, int S, int dt, unsigned opts, long most)
 {
     if (!dt_ok(dt)) return KLA_ERR_DTYPE;
     if (!ssm_shape_ok(D, G, S) || ld_u < D || ld_delta < D || ld_B < (long)G * S || ld_C < (long)G * S || (z && ld_z < D) ||
-        ld_u > kMaxSsmRow || ld_delta > kMaxSsmRow || ld_B > kMaxSsmRow || ld_C > kMaxSsmRow || ld_z > kMaxSsmRow ||
-        (opts & ~(unsigned)KLA_LAYER_SOFTPLUS))
+        ld_u > most || ld_delta > most || ld_B > most || ld_C > most || (z && ld_z > most) || (opts & ~(unsigned)KLA_LAYER_SOFTPLUS))
         return KLA_ERR_SHAPE;
     if (!A) return KLA_ERR_NULL;
     (void)u; (void)delta; (void)B; (void)C;
@@ -312,7 +311,7 @@ int kla_ssm_fwd(const void* u, long ld_u, const void* delta, long ld_delta, cons
 {
     kla::Seqs s;
     long M;
-    if (const int e = ssm_check(u, ld_u, delta, ld_delta, A, B, ld_B, C, ld_C, z, ld_z, D, G, S, dt, opts)) return e;
+    if (const int e = ssm_check(u, ld_u, delta, ld_delta, A, B, ld_B, C, ld_C, z, ld_z, D, G, S, dt, opts, kMaxSsmRow)) return e;
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (M > 0 && (!u || !delta || !B || !C || !y)) return KLA_ERR_NULL;
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, y}) || !aligned(16, {A, h0, hT, saved}) || !aligned(4, {skip, delta_bias})) return KLA_ERR_ALIGN;
@@ -338,7 +337,7 @@ int kla_ssm_bwd(const void* u, long ld_u, const void* delta, long ld_delta, cons
 {
     kla::Seqs s;
     long M;
-    if (const int e = ssm_check(u, ld_u, delta, ld_delta, A, B, ld_B, C, ld_C, z, ld_z, D, G, S, dt, opts)) return e;
+    if (const int e = ssm_check(u, ld_u, delta, ld_delta, A, B, ld_B, C, ld_C, z, ld_z, D, G, S, dt, opts, kMaxSsmRow)) return e;
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (!dA || (M > 0 && (!u || !delta || !B || !C || !d_y || !du || !ddelta || !dB || !dC || (z && !dz)))) return KLA_ERR_NULL;
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, d_y, du, ddelta, dB, dC, dz}) || !aligned(16, {A, h0, d_hT, saved, dA, dh0}) ||
@@ -372,7 +371,7 @@ int kla_ssm_step(const void* u, long ld_u, const void* delta, long ld_delta, con
                  const float* skip, const void* z, long ld_z, const float* delta_bias, float* h, void* y, int N, int D, int G, int S, kla_dtype dt,
                  void* hip_stream, unsigned opts)
 {
-    if (const int e = ssm_check(u, ld_u, delta, ld_delta, A, B, ld_B, C, ld_C, z, ld_z, D, G, S, dt, opts)) return e;
+    if (const int e = ssm_check(u, ld_u, delta, ld_delta, A, B, ld_B, C, ld_C, z, ld_z, D, G, S, dt, opts, LONG_MAX)) return e;
     if (N < 0) return KLA_ERR_SHAPE;
     if (N > 0 && (!u || !delta || !B || !C || !h || !y)) return KLA_ERR_NULL;
     if (!aligned(elem_bytes(dt), {u, delta, B, C, z, y}) || !aligned(16, {A, h}) || !aligned(4, {skip, delta_bias})) return KLA_ERR_ALIGN;

@@ -369,3 +369,22 @@ def test_steps_to_the_last_digits(kla):
         worst = int((off / bar[ok]).argmax())
         assert (off <= bar[ok]).all(), (float(raw[ok][worst]), float(off[worst]))
         assert t[-8] == t[-5] == float("inf") and t[-7] == t[-4] == 0 and torch.isnan(t[-6])
+
+
+def test_step_of_rows_far_apart(kla):
+    """A token out of [N, T, D] whose rows are more than 2^24 elements apart: the bits of the same token by itself."""
+    N, D, G, S, row = 3, 72, 2, 16, 2 ** 24 + 72
+    g = torch.Generator(device="cuda").manual_seed(6)
+    whole = torch.empty(N, row, dtype=torch.bfloat16, device="cuda")
+    at, part = 0, {}
+    for k, w in (("u", D), ("delta", D), ("z", D), ("B", G * S), ("C", G * S)):
+        part[k] = whole[:, at:at + w]
+        part[k].copy_(torch.randn(N, w, generator=g, device="cuda"))
+        at += w
+    part["B"], part["C"] = part["B"].unflatten(-1, (G, S)), part["C"].unflatten(-1, (G, S))
+    A, h = -torch.rand(D, S, generator=g, device="cuda"), torch.randn(N, D, S, generator=g, device="cuda")
+    print("ssm step", row, flush=True)
+    h2 = h.clone()
+    y = kla.kla_ssm_step(**part, A=A, h=h)
+    y2 = kla.kla_ssm_step(**{k: v.contiguous() for k, v in part.items()}, A=A, h=h2)
+    assert torch.equal(bits(y), bits(y2)) and torch.equal(bits(h), bits(h2))

@@ -237,3 +237,13 @@ def test_row_strides(t, inner, ld):
 def test_rows_that_are_none(t, inner):
     with pytest.raises(ValueError):
         kla.layer._rows("x", t(), inner)
+
+
+def test_a_step_takes_rows_any_distance_apart():
+    """One token out of [N, T, D] with long T: its rows are T D apart.  (N = 0: nothing is launched.)"""
+    far = (1 << 24) + 1
+    for ld in ("ld_u", "ld_d", "ld_B", "ld_C", "ld_z"):
+        assert ssm_step(N=0, z=0x8000, **{"ld_z": 64, ld: far}) == OK, ld
+    for f in (ssm_fwd, ssm_bwd):
+        assert f(z=0x8000, ld_z=far, **({"dz": 0xf000} if f is ssm_bwd else {})) == E_SHAPE
+        assert f(ld_z=far, T=0, N=0, **(dict(dA=None) if f is ssm_bwd else dict(A=None))) == E_NULL      # (without a gate its stride means nothing)
