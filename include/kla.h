@@ -353,7 +353,7 @@ enum { KLA_LAYER_SILU = 1,        /* kla_conv_*: y = p sigmoid(p) instead of y =
  *   state       [n_states, W-1, D] dt or NULL       in   n_states, packed batches: as in kla_chunk_fwd
  *   y           [N, T, D] dt                        out
  *   state_out   [n_states, W-1, D] dt or NULL       out  the last W - 1 inputs; must not alias state (KLA_ERR_SHAPE)
- * W in 2..4, any D >= 1.
+ * W in 2..4, D in 1..2^30.
  */
 int kla_conv_fwd(const void *x, long ld_x, const float *weight, const float *bias, const void *state,
                  void *y, void *state_out,

@@ -60,10 +60,11 @@ int take_workspace(const void* ws, size_t have, size_t need)
 }
 
 // ---- short convolution ------------------------------------------------------------------------------------------------------------
+constexpr int kMaxConv = 1 << 30;                        // (a row rounded up to whole workgroups is an int)
 int conv_check(const void* x, long ld_x, const float* weight, int D, int W, int dt, unsigned opts)
 {
     if (!dt_ok(dt)) return KLA_ERR_DTYPE;
-    if (D <= 0 || W < 2 || W > 4 || ld_x < D || (opts & ~(unsigned)KLA_LAYER_SILU)) return KLA_ERR_SHAPE;
+    if (D <= 0 || D > kMaxConv || W < 2 || W > 4 || ld_x < D || (opts & ~(unsigned)KLA_LAYER_SILU)) return KLA_ERR_SHAPE;
     if (!weight) return KLA_ERR_NULL;
     (void)x;
     return KLA_OK;
@@ -238,7 +239,7 @@ int kla_conv_fwd(const void* x, long ld_x, const float* weight, const float* bia
 
 size_t kla_conv_bwd_workspace_bytes(int N, int T, int D, int W)
 {
-    if (N < 0 || T < 0 || D <= 0 || W < 2 || W > 4) return 0;
+    if (N < 0 || T < 0 || D <= 0 || D > kMaxConv || W < 2 || W > 4) return 0;
     return round256((size_t)kla::conv_bwd_plan((long)N * T, D).blocks_t * D * (W + 1) * sizeof(float));
 }
 

@@ -247,3 +247,12 @@ def test_a_step_takes_rows_any_distance_apart():
     for f in (ssm_fwd, ssm_bwd):
         assert f(z=0x8000, ld_z=far, **({"dz": 0xf000} if f is ssm_bwd else {})) == E_SHAPE
         assert f(ld_z=far, T=0, N=0, **(dict(dA=None) if f is ssm_bwd else dict(A=None))) == E_NULL      # (without a gate its stride means nothing)
+
+
+def test_widths_that_round_beyond_an_int():
+    """A row of nearly 2^31 channels, rounded up to whole vectors and workgroups, is no int any more: refused, not wrapped around."""
+    for D in ((1 << 30) + 1, (1 << 31) - 1):
+        for f in (conv_fwd, conv_bwd, conv_step):
+            assert f(D=D, ld=D, **({} if f is conv_step else dict(T=0))) == E_SHAPE
+        assert kla.lib().kla_conv_bwd_workspace_bytes(1, 1, D, 4) == 0
+    assert conv_step(D=1 << 30, ld=1 << 30, B=0) == OK
