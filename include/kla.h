@@ -334,7 +334,7 @@ int kla_beta(const void *k, const float *eta, float eps, float *beta,
  * layers, and the norms before and after a block.  The conventions above hold, except:
  *   - Inputs whose row stride ld_* (elements from one token to the next) is an argument may be column ranges of a wider
  *     tensor, e.g. of the output of one projection for several of them; a row itself is contiguous.  Everything else is
- *     contiguous, and so are all outputs.
+ *     contiguous, and so are all outputs.  An output must not overlap an input, except where it says so.
  *   - Data pointers have to be aligned to their element only (A, states and checkpoints: 16 bytes);
  *     rows may start at any element and have any width.
  *   - Parameters (weights, biases, scales) and their gradients are fp32.
@@ -351,8 +351,8 @@ enum { KLA_LAYER_SILU = 1,        /* kla_conv_*: y = p sigmoid(p) instead of y =
  *   x           [N, T, D] dt, rows ld_x apart       in
  *   weight      [D, W], bias [D] or NULL            in
  *   state       [n_states, W-1, D] dt or NULL       in   n_states, packed batches: as in kla_chunk_fwd
- *   y           [N, T, D] dt                        out
- *   state_out   [n_states, W-1, D] dt or NULL       out  the last W - 1 inputs; must not alias state (KLA_ERR_SHAPE)
+ *   y           [N, T, D] dt                        out  (y == x: KLA_ERR_SHAPE)
+ *   state_out   [n_states, W-1, D] dt or NULL       out  the last W - 1 inputs (state_out == state: KLA_ERR_SHAPE)
  * W in 2..4, D in 1..2^30.
  */
 int kla_conv_fwd(const void *x, long ld_x, const float *weight, const float *bias, const void *state,
@@ -361,7 +361,8 @@ int kla_conv_fwd(const void *x, long ld_x, const float *weight, const float *bia
                  int N, int T, int D, int W, kla_dtype dt, void *hip_stream, unsigned opts);
 
 /* Gradients of sum <d_y, y> + sum <d_state_out, state_out> (d_state_out NULL: zeros) from the inputs of the forward.
- * d_y, dx [N, T, D] contiguous; dbias, d_state NULL if unwanted; workspace 256-byte aligned. */
+ * d_y, dx [N, T, D] contiguous; dbias, d_state NULL if unwanted; workspace 256-byte aligned.  dx == x, dx == d_y, d_state == state,
+ * d_state == d_state_out: KLA_ERR_SHAPE. */
 size_t kla_conv_bwd_workspace_bytes(int N, int T, int D, int W);
 int kla_conv_bwd(const void *x, long ld_x, const float *weight, const float *bias, const void *state,
                  const void *d_y, const void *d_state_out,

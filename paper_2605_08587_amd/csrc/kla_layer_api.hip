@@ -224,7 +224,8 @@ int kla_conv_fwd(const void* x, long ld_x, const float* weight, const float* bia
     if (const int e = conv_check(x, ld_x, weight, D, W, dt, opts)) return e;
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (M > 0 && (!x || !y)) return KLA_ERR_NULL;
-    if (state_out && state_out == state) return KLA_ERR_SHAPE;       // one is written while the other is read
+    // written while others read it: a token's inputs are those of earlier tokens too
+    if ((state_out && state_out == state) || (M > 0 && y == x)) return KLA_ERR_SHAPE;
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, state, y, state_out}) || !aligned(4, {weight, bias})) return KLA_ERR_ALIGN;
     const bool silu = opts & KLA_LAYER_SILU;
@@ -252,6 +253,7 @@ int kla_conv_bwd(const void* x, long ld_x, const float* weight, const float* bia
     if (const int e = conv_check(x, ld_x, weight, D, W, dt, opts)) return e;
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (!dweight || (M > 0 && (!x || !d_y || !dx))) return KLA_ERR_NULL;
+    if ((M > 0 && (dx == x || dx == d_y)) || (d_state && (d_state == state || d_state == d_state_out))) return KLA_ERR_SHAPE;    // (as y and x)
     const size_t e = elem_bytes(dt);
     if (!aligned(e, {x, state, d_y, d_state_out, dx, d_state}) || !aligned(4, {weight, bias, dweight, dbias})) return KLA_ERR_ALIGN;
     if (const int r = take_workspace(workspace, workspace_bytes, kla_conv_bwd_workspace_bytes(N, T, D, W))) return r;

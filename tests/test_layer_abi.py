@@ -256,3 +256,10 @@ def test_widths_that_round_beyond_an_int():
             assert f(D=D, ld=D, **({} if f is conv_step else dict(T=0))) == E_SHAPE
         assert kla.lib().kla_conv_bwd_workspace_bytes(1, 1, D, 4) == 0
     assert conv_step(D=1 << 30, ld=1 << 30, B=0) == OK
+
+
+def test_convolution_in_place():
+    """A convolution cannot write where it reads: other threads still need what is there."""
+    assert conv_fwd(y=0x1000) == E_SHAPE
+    assert conv_bwd(dx=0x1000) == E_SHAPE and conv_bwd(dx=0x3000) == E_SHAPE
+    assert conv_bwd(st=0x6000, dst=0x6000) == E_SHAPE and conv_bwd(st=0x6000, dlast=0x7000, dst=0x7000) == E_SHAPE
