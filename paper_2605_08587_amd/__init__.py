@@ -163,6 +163,14 @@ def _written(*ts):
             torch.autograd.graph.increment_version(t)
 
 
+def _counting(cu_seqlens):
+    """Offsets whose changes can be told until the backward: an inference tensor counts none, and is copied to one that does."""
+    if cu_seqlens is None or not cu_seqlens.is_inference():
+        return cu_seqlens
+    with torch.inference_mode(False):
+        return cu_seqlens.clone()
+
+
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -606,10 +614,9 @@ class _KlaChunk(torch.autograd.Function):
     def forward(ctx, q, k, v, log_alpha, eta, h0, eps, cu_seqlens, cu_seqlens_host, normalize_q, gdn_beta, save):
         if cu_seqlens is not None:
             # the plan of the backward and what is left behind for it are for these offsets: a host copy of our own (the caller may
-            # fill its own anew), and the device's unchanged (an inference tensor does not count its changes)
+            # fill its own anew), and the device's unchanged
             cu_seqlens_host = _host_cu(cu_seqlens, cu_seqlens_host)[0].clone()
-            if cu_seqlens.is_inference():
-                cu_seqlens = cu_seqlens.clone()
+            cu_seqlens = _counting(cu_seqlens)
         if save and any(ctx.needs_input_grad[:6]):
             o, hT, saved = _fwd_save(q, k, v, log_alpha, eta, eps, h0, cu_seqlens, cu_seqlens_host, normalize_q, gdn_beta)
         else:

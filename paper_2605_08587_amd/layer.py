@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from . import KlaError, _binding, _check, _dev, _dt, _host_cu, _ptr, _stream, _written, _ws_bytes, lib
+from . import KlaError, _binding, _check, _counting, _dev, _dt, _host_cu, _ptr, _stream, _written, _ws_bytes, lib
 
 KLA_LAYER_SILU, KLA_LAYER_SOFTPLUS, KLA_LAYER_SIGMOID, KLA_LAYER_GATE_FIRST = 1, 2, 4, 8
 
@@ -126,7 +126,7 @@ class _Offsets:
         self.cu = self.host = None
         if cu is not None:
             self.host = _host_cu(cu, host)[0].clone()
-            self.cu = cu.clone() if cu.is_inference() else cu
+            self.cu = _counting(cu)
             self.version = self.cu._version
 
     def check(self):
