@@ -175,3 +175,41 @@ def test_widths_around_vectors(kla, D, dtype):
     assert torch.equal(last.cpu().double(), last_ref)
     for k, v in (("x", got["dx"][0]), ("weight", got["dweight"]), ("bias", got["dbias"]), ("state", got["dstate"])):
         close("d" + k, v, ref[k], SUMS)
+
+
+def _whole(x, weight, bias, state, seqs, silu):
+    """The definition a sequence and a tap at a time, for lengths at which token by token takes too long."""
+    ys, lasts, W = [], [], weight.shape[1]
+    for n, (lo_, hi) in enumerate(seqs):
+        line = torch.cat([x.new_zeros(W - 1, x.shape[1]) if state is None else state[n], x[lo_:hi]])
+        p = sum(line[j:j + hi - lo_] * weight[:, j] for j in range(W)) + bias
+        ys.append(p * torch.sigmoid(p) if silu else p)
+        lasts.append(line[hi - lo_:])
+    return torch.cat(ys), torch.stack(lasts)
+
+
+@pytest.mark.parametrize("dtype,W,silu,state,wide", [(torch.bfloat16, 4, True, True, "odd"), (torch.float32, 3, False, True, False),
+                                                     (torch.float32, 4, True, False, True), (torch.bfloat16, 2, False, True, False)])
+def test_long_strips_of_packed_batches(kla, dtype, W, silu, state, wide):
+    """As many tokens and channels as are taken in strips of 32 forward and 64 backward, whose sequences begin and end within them: every output and
+    gradient, those of the states from both sides among them."""
+    lens, D = [1, 0, 70, 5000, 63, 64, 65, 2, 9500, 3], 2051
+    print("conv strips", dtype, W, silu, state, wide, flush=True)
+    d, dev, dy, ds, cu = _inputs(dtype, 0, 0, D, W, lens, True, state, wide, 300 + W)
+    M = sum(lens)
+    assert M // 64 * ((D + 255) // 256) > 2048           # (the rule's side that the other tests are not on)
+    seqs = lo.sequences(0, 0, cu)
+    flat = dict(d, x=d["x"].reshape(-1, D))
+    (y_ref, last_ref), ref = lo.gradients(lambda **k: _whole(**k, seqs=seqs, silu=silu), flat, (dy.reshape(-1, D), ds))
+    short = {k: v if v is None else v[..., :5].double() if k in ("x", "state") else v[:5].double() for k, v in flat.items()}
+    short["x"], few = short["x"][:71], seqs[:3]          # (the same definition)
+    for p, q in zip(lo.conv(**short, seqs=few, silu=silu), _whole(**short, seqs=few, silu=silu)):
+        assert torch.allclose(p, q, rtol=0, atol=1e-12)
+    packed = dict(cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
+    y, last = kla.kla_conv_fwd(**dev, silu=silu, **packed)
+    got = kla.kla_conv_bwd(dev["x"], dev["weight"], dy.cuda(), dev["bias"], dev["state"], ds.cuda(), silu=silu, **packed)
+    close("y", y.reshape(-1, D), y_ref, SUMS)
+    assert torch.equal(last.cpu().double(), last_ref)
+    for k, v in (("x", got["dx"].reshape(-1, D)), ("weight", got["dweight"]), ("bias", got["dbias"]), ("state", got["dstate"])):
+        if v is not None:
+            close("d" + k, v, ref[k], SUMS)
