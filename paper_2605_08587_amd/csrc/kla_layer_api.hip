@@ -85,10 +85,13 @@ constexpr int kMaxSsmSeqs = 65535;                       // sequences, and group
 bool ssm_shape_ok(int D, int G, int S) { return D > 0 && D <= kMaxSsmRow && G > 0 && D % G == 0 && (S == 8 || S == 16 || S == 32 || S == 64); }
 // Tokens per segment.  A wave takes 8 channels of one segment and its tokens one after the other, about 70 ns each when it has its SIMD to
 // itself; segments cost a second pass over most of the tokens for their maps.  4096 waves run at twice the tokens per second of 1024, one
-// for each SIMD (kernels of forward and backward, 2048 tokens x 2048 channels: 168 us in segments, 443 us whole; two such sequences 297
-// and 447 us, three 435 and 462 us, four 551 and 490 us).  So batches of fewer than 768 waves are cut into segments until 4096 run; up to 255
-// tokens the additional launches cost more than they save.  Segments are whole pairs of tiles, and 64 tokens at least (in multiples of 64 one sequence
-// of 7000 tokens x 1024 channels took 82 us forward instead of 74).  In a packed batch the longest sequence decides: it would run on alone.
+// for each SIMD.  So batches of fewer than 768 waves are cut into segments until 4096 run; up to 255 tokens the additional launches cost more than they
+// save.  At 768 waves forward calls are about even: 2048 tokens and 16 states, whole and in segments, three sequences of 2048 channels 132 and 127 us, six
+// of 1024 126 and 128, twelve of 512 132 and 139; three of 512 tokens 36 and 42 us; 8, 32 and 64 states 98 and 110, 196 and 206, 314 and 356 us.  Both
+// directions together, cut alike, still gain there where sequences are long (447 and 393 us, of 8192 tokens 1751 and 1489) and lose where they are
+// short or have 64 states (300 tokens 92 and 107 us; 1258 and 1293).  Kernels of both: one sequence 443 and 168 us, two 447 and 297, four 490 and 551.
+// Segments are whole pairs of tiles, and 64 tokens at least (in multiples of 64 one sequence of 7000 tokens x 1024 channels took 82 us forward instead
+// of 74).  In a packed batch the longest sequence decides: it would run on alone.
 int ssm_segment(long M, int n_states, int D, long longest)
 {
     const int whole = INT_MAX / 32 * 32;
