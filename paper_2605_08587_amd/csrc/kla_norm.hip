@@ -65,7 +65,8 @@ template <int TPR, int V, int NV> struct Columns {
             if (v == NV - 1) twice = place - c[v];
         }
     }
-    // (the last vector is one of the threads' last: by_width)
+    // x, or 0 where the vector before has it too: of both factors of a product, as 0 times an infinity is none.  (The last vector is one of the
+    // threads' last: by_width.)
     __device__ __forceinline__ float once(int v, int i, float x) const { return v == NV - 1 && i < twice ? 0.f : x; }
     template <typename T> __device__ __forceinline__ Row<V, NV> load(const T* p, float fill = 0.f) const
     {
@@ -120,7 +121,10 @@ __global__ __launch_bounds__(block_threads(TPR)) void add_norm_fwd_kernel(AddNor
     }
     const Row<V, NV> w = at.load(a.weight);
     float sum = 0.f;
-    KLA_EACH(v, i) sum = fmaf(at.once(v, i, x.v[v][i]), x.v[v][i], sum);
+    KLA_EACH(v, i) {
+        const float o = at.once(v, i, x.v[v][i]);
+        sum = fmaf(o, o, sum);
+    }
     const float f = inv_rms(row_sum<TPR>(sum, red), 1.f / (float)a.D, a.eps);
     // Behind the sum's barrier: residual_out may be residual, and the row's last vector has columns of another wave's, which has to have read
     // them by then (up to TPR = 64 one wave has the row, and its loads stand ahead of its stores).
@@ -179,8 +183,8 @@ __global__ __launch_bounds__(block_threads(TPR)) void add_norm_bwd_kernel(AddNor
             const float t = fmaf(sc.v[v][i], x.v[v][i], n.v[v][i]);
             n.v[v][i] = t;
             const float o = at.once(v, i, t);
-            sq = fmaf(o, t, sq);
-            en = fmaf(dy.v[v][i] * w.v[v][i], o, en);
+            sq = fmaf(o, o, sq);
+            en = fmaf(at.once(v, i, dy.v[v][i] * w.v[v][i]), o, en);
         }
         sq = row_sum<TPR>(sq, red);
         en = row_sum<TPR>(en, red);
@@ -220,7 +224,8 @@ __global__ __launch_bounds__(block_threads(TPR)) void gated_norm_fwd_kernel(Gate
         float s;
         gate_of(g.v[v][i], plain, &g.v[v][i], &s);
         if (first) { x.v[v][i] *= g.v[v][i]; g.v[v][i] = 1.f; }
-        sum = fmaf(at.once(v, i, x.v[v][i]), x.v[v][i], sum);
+        const float o = at.once(v, i, x.v[v][i]);
+        sum = fmaf(o, o, sum);
     }
     const float f = inv_rms(row_sum<TPR>(sum, red), 1.f / (float)a.D, a.eps);
     KLA_EACH(v, i) x.v[v][i] *= f * w.v[v][i] * g.v[v][i];
@@ -252,8 +257,8 @@ __global__ __launch_bounds__(block_threads(TPR)) void gated_norm_bwd_kernel(Gate
             const float q = first ? x.v[v][i] * g : x.v[v][i];       // what is normalised
             const float e = (first ? dy.v[v][i] : dy.v[v][i] * g) * w.v[v][i];
             const float o = at.once(v, i, q);
-            sq = fmaf(o, q, sq);
-            en = fmaf(e, o, en);
+            sq = fmaf(o, o, sq);
+            en = fmaf(at.once(v, i, e), o, en);
         }
         sq = row_sum<TPR>(sq, red);
         en = row_sum<TPR>(en, red);

@@ -218,3 +218,34 @@ def test_rows_whose_squares_are_denormal(kla, D):
     for i in range(4):
         if D > 7:                                        # (narrow rows: what is left of terms that cancel)
             close("dx %d" % i, dx[i], ref["x"][i], 4 * (SUMS + 0.5 * 2.0 ** -149 / (float(size[i]) ** 2 / 4)))
+
+
+@pytest.mark.parametrize("D", [9, 100, 333, 1001, 2047, 8191])
+@pytest.mark.parametrize("dtype", [b16, f32])
+def test_infinities_where_vectors_overlap(kla, D, dtype):
+    """An infinity in a column that two vectors of a row share counts once: the row's other elements are 0 and its own a NaN, as by the definition, wherever it
+    stands; and so do infinities in the gradient."""
+    g = torch.Generator().manual_seed(D)
+    w = randn(g, D)
+    cols = sorted({0, 3, D - 1, D - 2, D - 3, D - 4, D - 5, D - 6, D - 7, D - 8, D - 9} & set(range(D)))
+    x, gate, dy = (randn(g, len(cols), D, dtype=dtype) for _ in range(3))
+    bad = x.clone()
+    bad[torch.arange(len(cols)), cols] = float("inf")
+    print("norms", D, dtype, flush=True)
+    y, _ = kla.kla_add_norm_fwd(bad.cuda(), w.cuda(), eps=EPS)
+    z = kla.kla_gated_norm_fwd(bad[:, None].cuda(), gate[:, None].cuda(), w.cuda(), eps=EPS)[:, 0]
+    for t in (y, z):
+        t = t.cpu()
+        for r, c in enumerate(cols):
+            assert torch.isnan(t[r, c]) and not t[r, :c].any() and not t[r, c + 1:].any(), (r, c)
+    # an infinite gradient at one element: the definition's infinities everywhere, with their signs
+    wild = dy.clone()
+    wild[torch.arange(len(cols)), cols] = float("inf")
+    for f, at in ((lambda t: kla.kla_add_norm_bwd(x.cuda(), w.cuda(), t.cuda(), eps=EPS)["dx"], None),
+                  (lambda t: kla.kla_gated_norm_bwd(x[:, None].cuda(), gate[:, None].cuda(), w.cuda(), t[:, None].cuda(), eps=EPS)["dx"][:, 0], gate)):
+        dx = f(wild).cpu().double()
+        e = wild.double() * w.double() * (1 if at is None else at.double() * torch.sigmoid(at.double()))
+        n = lo._normed(x.double(), EPS)
+        ref = e - n * (e * n).mean(-1, keepdim=True)
+        assert torch.equal(torch.isnan(dx), torch.isnan(ref))
+        assert torch.equal(dx[~torch.isnan(ref)], ref[~torch.isnan(ref)])
