@@ -5,6 +5,8 @@
 // Before a sequence's first token stands its state, the last W - 1 inputs of earlier tokens (or zeros); nothing of another
 // sequence is ever multiplied, not even by zero.  Two passes over the elements forward, three backward: bound by memory.  bf16, 2048 channels,
 // 8 x 4096 tokens: forward 54 us (268 MB, 5.0 TB/s), backward 93 us (403 MB, 4.3 TB/s) and 5 us for the sums; a large copy 4.8 TB/s.
+#include <algorithm>
+
 #include "kla_layer.hpp"
 
 namespace kla {
@@ -337,7 +339,7 @@ template <typename T, int W, int V, bool SILU> static hipError_t conv_fwd(const 
     const long strips = (a.M + L - 1) / L, n_main = (strips + ty - 1) / ty * blocks_c;
     const long n_state = a.state_out ? (a.seqs.n_seq + (long)ty - 1) / ty * blocks_c : 0;
     if (n_main + n_state == 0) return hipSuccess;
-    if (n_main + n_state > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (n_main + n_state > most_blocks(256)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)(n_main + n_state)), block(256);
     if (tx == 64) hipLaunchKernelGGL((conv_fwd_kernel<T, W, V, SILU, true>), grid, block, 0, st, a, tx, L, blocks_c, (unsigned)n_main);
     else          hipLaunchKernelGGL((conv_fwd_kernel<T, W, V, SILU, false>), grid, block, 0, st, a, tx, L, blocks_c, (unsigned)n_main);
@@ -348,7 +350,7 @@ template <typename T, int W, int V, bool SILU> static hipError_t conv_bwd(const 
     const ConvBwdPlan p = conv_bwd_plan(a.M, a.D);
     const int blocks_c = (a.D + p.tx * V - 1) / (p.tx * V);
     const long n_main = p.blocks_t * blocks_c, n_state = a.d_state ? (a.seqs.n_seq + (long)p.ty - 1) / p.ty * blocks_c : 0;
-    if (n_main + n_state > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (n_main + n_state > most_blocks(256)) return hipErrorInvalidConfiguration;
     if (n_main + n_state > 0) {
         const dim3 grid((unsigned)(n_main + n_state)), block(256);
         if (p.tx == 64) hipLaunchKernelGGL((conv_bwd_kernel<T, W, V, SILU, true>), grid, block, 0, st, a, p.tx, p.L, blocks_c, (unsigned)n_main);
@@ -384,16 +386,22 @@ template <typename T> hipError_t launch_conv_step(const T* x, long ld_x, const f
                                                   bool silu, hipStream_t st)
 {
     const int blocks_c = (D + 255) / 256;
-    const long blocks = (long)blocks_c * B;
-    if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks), block(256);
-    switch (W) {
-        case 2:  hipLaunchKernelGGL((conv_step_kernel<T, 2>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
-        case 3:  hipLaunchKernelGGL((conv_step_kernel<T, 3>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
-        default: hipLaunchKernelGGL((conv_step_kernel<T, 4>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+    const dim3 block(256);
+    const int piece = (int)std::min<long>(most_blocks(256) / blocks_c, B);           // sequences of a launch
+    for (int done = 0, n; done < B; done += n) {
+        n = std::min(piece, B - done);
+        const dim3 grid((unsigned)((long)blocks_c * n));
+        switch (W) {
+            case 2:  hipLaunchKernelGGL((conv_step_kernel<T, 2>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+            case 3:  hipLaunchKernelGGL((conv_step_kernel<T, 3>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+            default: hipLaunchKernelGGL((conv_step_kernel<T, 4>), grid, block, 0, st, x, ld_x, weight, bias, state, y, D, blocks_c, silu); break;
+        }
+        if (const hipError_t e = hipGetLastError()) return e;
+        x += n * ld_x;
+        state += (long)n * (W - 1) * D;
+        y += (long)n * D;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 #define KLA_CONV(T)                                                                                                                       \

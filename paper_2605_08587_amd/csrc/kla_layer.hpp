@@ -95,6 +95,9 @@ __device__ __forceinline__ Place sequence_of(const Seqs& s, long t)
     return sequence(s, lo);
 }
 
+// A launch's threads are counted in 32 bits: one of more runs what is left of the number, without an error.
+inline long most_blocks(int threads) { return 0xffffffffL / threads; }
+
 // ---- launchers ------------------------------------------------------------------------------------------------------------------
 // Sums over the rows of partial[P][n0 + n1 + n2] in a fixed order, the columns to up to three outputs (each may be NULL).
 struct ColumnSums { long n[3]; float* out[3]; };
@@ -146,6 +149,7 @@ template <typename T> struct SsmArgs {
     float* saved;                                        // states at every checkpoint, or NULL
     float* seg_state; float* seg_delta;                  // per slot: [D][S] and [D]; NULL: one segment per sequence
     Seqs seqs; long M; int D, G, Lseg; long slots;
+    long slot0;                                          // of a launch that takes not all of them
     bool softplus;
     int channels;                                        // of a workgroup of the forward: 32 or 64
     // backward
@@ -161,6 +165,6 @@ constexpr int kSsmBwdChannels = 32;
 constexpr int ssm_checkpoint(int S) { return S > 16 ? 8 : 16; }     // tokens between checkpoints
 template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool outputs, hipStream_t st);
 template <typename T> hipError_t launch_ssm_bwd(const SsmArgs<T>& a, int S, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st);
-template <typename T> hipError_t launch_ssm_step(const SsmArgs<T>& a, float* h, int B, int S, hipStream_t st);
+template <typename T> hipError_t launch_ssm_step(SsmArgs<T> a, float* h, int B, int S, hipStream_t st);
 
 }  // namespace kla

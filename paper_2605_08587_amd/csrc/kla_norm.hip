@@ -7,6 +7,8 @@
 // once; nothing but the inputs is kept for the backward, which forms f again.  Bound by memory: bf16, 32768 rows of 1024 with an fp32 stream
 // forward 74 us (403 MB, 5.4 TB/s), backward 120 us (604 MB, 5.0 TB/s); 262144 heads of 256 with their gates forward 77 us (403 MB, 5.2 TB/s),
 // backward 129 us (671 MB, 5.2 TB/s); a large copy 4.8 TB/s.
+#include <algorithm>
+
 #include "kla_layer.hpp"
 
 namespace kla {
@@ -321,13 +323,19 @@ template <typename T, typename F> static hipError_t for_rows(int D, F&& f)
 }
 template <typename T, typename R> hipError_t launch_add_norm_fwd(const AddNormArgs<T, R>& a, hipStream_t st)
 {
-    if (a.M == 0) return hipSuccess;
     return for_rows<T>(a.D, [&](auto tpr, auto v, auto nv) {
-        constexpr int rows = block_threads(tpr.value) / tpr.value;
-        const long blocks = (a.M + rows - 1) / rows;
-        if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
-        hipLaunchKernelGGL((add_norm_fwd_kernel<T, R, tpr.value, v.value, nv.value>), dim3((unsigned)blocks), dim3(block_threads(tpr.value)), 0, st, a);
-        return hipGetLastError();
+        constexpr int threads = block_threads(tpr.value), rows = threads / tpr.value;
+        AddNormArgs<T, R> b = a;
+        for (long done = 0; done < a.M; done += b.M) {
+            b.M = std::min(a.M - done, most_blocks(threads) * rows);
+            b.x = a.x + done * a.ld_x;
+            b.y = a.y + done * a.D;
+            if (a.residual) b.residual = a.residual + done * a.D;
+            if (a.residual_out) b.residual_out = a.residual_out + done * a.D;
+            hipLaunchKernelGGL((add_norm_fwd_kernel<T, R, tpr.value, v.value, nv.value>), dim3((unsigned)((b.M + rows - 1) / rows)), dim3(threads), 0, st, b);
+            if (const hipError_t e = hipGetLastError()) return e;
+        }
+        return hipSuccess;
     });
 }
 template <typename T, typename R> hipError_t launch_add_norm_bwd(const AddNormArgs<T, R>& a, float* dweight, float* dscale, hipStream_t st)
@@ -344,13 +352,21 @@ template <typename T, typename R> hipError_t launch_add_norm_bwd(const AddNormAr
 }
 template <typename T> hipError_t launch_gated_norm_fwd(const GatedNormArgs<T>& a, hipStream_t st)
 {
-    if (a.M == 0) return hipSuccess;
     return for_rows<T>(a.D, [&](auto tpr, auto v, auto nv) {
-        constexpr int rows = block_threads(tpr.value) / tpr.value;
-        const long blocks = (a.M * a.H + rows - 1) / rows;
-        if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
-        hipLaunchKernelGGL((gated_norm_fwd_kernel<T, tpr.value, v.value, nv.value>), dim3((unsigned)blocks), dim3(block_threads(tpr.value)), 0, st, a);
-        return hipGetLastError();
+        constexpr int threads = block_threads(tpr.value), rows = threads / tpr.value;
+        const long piece = most_blocks(threads) * rows / a.H;            // tokens of a launch
+        if (piece == 0) return hipErrorInvalidConfiguration;
+        GatedNormArgs<T> b = a;
+        for (long done = 0; done < a.M; done += b.M) {
+            b.M = std::min(a.M - done, piece);
+            b.x = a.x + done * a.ld_x;
+            b.gate = a.gate + done * a.ld_gate;
+            b.y = a.y + done * a.H * a.D;
+            hipLaunchKernelGGL((gated_norm_fwd_kernel<T, tpr.value, v.value, nv.value>), dim3((unsigned)((b.M * a.H + rows - 1) / rows)), dim3(threads), 0,
+                               st, b);
+            if (const hipError_t e = hipGetLastError()) return e;
+        }
+        return hipSuccess;
     });
 }
 template <typename T> hipError_t launch_gated_norm_bwd(const GatedNormArgs<T>& a, float* dweight, hipStream_t st)

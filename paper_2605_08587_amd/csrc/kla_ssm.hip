@@ -7,6 +7,8 @@
 // sixteen lanes have twice the scalar work per state (one sequence of 65536 tokens x 1024 channels x 16 states 773 us, eight 551 us).
 // That sequence: maps and outputs take 13 and 19 vector instructions per token and wave (8 channels) and keep the ALU busy for 96 and 93 %.
 // 4 x 2048 tokens x 2048 channels, training: 142 us, one wave per SIMD (69 ns a token), the ALU busy for 59 %; 8 x 2048: 224 us, 76 %.
+#include <algorithm>
+
 #include "kla_ssm_ops.hpp"
 
 namespace kla {
@@ -24,7 +26,7 @@ __global__ __launch_bounds__(THREADS, MODE == kSsmMaps && S == 64 ? 2 : 1) void 
     __shared__ __align__(16) float lds[2][2 * kTok * S];
     const int o = threadIdx.x & 7;
     const int block = blockIdx.x % blocks_c;
-    const long slot = blockIdx.x / blocks_c;
+    const long slot = a.slot0 + blockIdx.x / blocks_c;
     Segment g;
     if (!segment_of(a, slot, &g)) return;
     if (MODE == kSsmMaps && g.last) return;              // nothing follows it
@@ -247,23 +249,26 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmArgs<T> a, float* __re
     }
 }
 
-template <typename T, int S, int THREADS> static hipError_t ssm_fwd_by(const SsmArgs<T>& a, bool outputs, hipStream_t st)
+template <typename T, int S, SsmMode MODE, bool HASZ, int THREADS> static hipError_t ssm_fwd_mode(SsmArgs<T> a, hipStream_t st)
 {
     const int blocks_c = ssm_channel_blocks(a.D, a.G, THREADS / 8);
-    const long blocks = blocks_c * a.slots;
-    if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks), block(THREADS);
-    if (a.seg_state) {
-        hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmMaps, false, THREADS>), grid, block, 0, st, a, blocks_c);
+    for (long n; a.slot0 < a.slots; a.slot0 += n) {
+        n = std::min(a.slots - a.slot0, most_blocks(THREADS) / blocks_c);
+        hipLaunchKernelGGL((ssm_fwd_kernel<T, S, MODE, HASZ, THREADS>), dim3((unsigned)(blocks_c * n)), dim3(THREADS), 0, st, a, blocks_c);
         if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+template <typename T, int S, int THREADS> static hipError_t ssm_fwd_by(const SsmArgs<T>& a, bool outputs, hipStream_t st)
+{
+    if (a.slots == 0) return hipSuccess;
+    if (a.seg_state) {
+        if (const hipError_t e = ssm_fwd_mode<T, S, kSsmMaps, false, THREADS>(a, st)) return e;
         hipLaunchKernelGGL((ssm_join_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    if (!outputs) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmStates, false, THREADS>), grid, block, 0, st, a, blocks_c);
-    else if (a.z) hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, true, THREADS>), grid, block, 0, st, a, blocks_c);
-    else          hipLaunchKernelGGL((ssm_fwd_kernel<T, S, kSsmOutputs, false, THREADS>), grid, block, 0, st, a, blocks_c);
-    return hipGetLastError();
+    if (!outputs) return ssm_fwd_mode<T, S, kSsmStates, false, THREADS>(a, st);
+    return a.z ? ssm_fwd_mode<T, S, kSsmOutputs, true, THREADS>(a, st) : ssm_fwd_mode<T, S, kSsmOutputs, false, THREADS>(a, st);
 }
 template <typename T, int S> static hipError_t ssm_fwd(const SsmArgs<T>& a, bool outputs, hipStream_t st)
 {
@@ -281,25 +286,35 @@ template <typename T> hipError_t launch_ssm_fwd(const SsmArgs<T>& a, int S, bool
         default: return ssm_fwd<T, 64>(a, outputs, st);
     }
 }
-template <typename T> hipError_t launch_ssm_step(const SsmArgs<T>& a, float* h, int B, int S, hipStream_t st)
+template <typename T> hipError_t launch_ssm_step(SsmArgs<T> a, float* h, int B, int S, hipStream_t st)
 {
     const int blocks_c = (a.D + 63) / 64;
-    const long blocks = (long)blocks_c * B;
-    if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks), block(256);
-    switch (S) {
-        case 8:  hipLaunchKernelGGL((ssm_step_kernel<T, 8>), grid, block, 0, st, a, h, blocks_c); break;
-        case 16: hipLaunchKernelGGL((ssm_step_kernel<T, 16>), grid, block, 0, st, a, h, blocks_c); break;
-        case 32: hipLaunchKernelGGL((ssm_step_kernel<T, 32>), grid, block, 0, st, a, h, blocks_c); break;
-        default: hipLaunchKernelGGL((ssm_step_kernel<T, 64>), grid, block, 0, st, a, h, blocks_c); break;
+    const dim3 block(256);
+    const int piece = (int)std::min<long>(most_blocks(256) / blocks_c, B);           // sequences of a launch
+    for (int done = 0, n; done < B; done += n) {
+        n = std::min(piece, B - done);
+        const dim3 grid((unsigned)((long)blocks_c * n));
+        switch (S) {
+            case 8:  hipLaunchKernelGGL((ssm_step_kernel<T, 8>), grid, block, 0, st, a, h, blocks_c); break;
+            case 16: hipLaunchKernelGGL((ssm_step_kernel<T, 16>), grid, block, 0, st, a, h, blocks_c); break;
+            case 32: hipLaunchKernelGGL((ssm_step_kernel<T, 32>), grid, block, 0, st, a, h, blocks_c); break;
+            default: hipLaunchKernelGGL((ssm_step_kernel<T, 64>), grid, block, 0, st, a, h, blocks_c); break;
+        }
+        if (const hipError_t e = hipGetLastError()) return e;
+        a.u += n * a.ld_u;
+        a.delta += n * a.ld_delta;
+        a.B += n * a.ld_B;
+        a.C += n * a.ld_C;
+        if (a.z) a.z += n * a.ld_z;
+        a.y += (long)n * a.D;
+        h += (long)n * a.D * S;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 #define KLA_SSM(T)                                                                                       \
     template hipError_t launch_ssm_fwd<T>(const SsmArgs<T>&, int, bool, hipStream_t);                    \
-    template hipError_t launch_ssm_step<T>(const SsmArgs<T>&, float*, int, int, hipStream_t);
+    template hipError_t launch_ssm_step<T>(SsmArgs<T>, float*, int, int, hipStream_t);
 KLA_SSM(float)
 KLA_SSM(bf16_t)
 

@@ -10,6 +10,8 @@
 // at every step, then over the four waves through LDS, then over the workgroups in a kernel of their own: no atomics.
 // The vector ALU bounds it: 55 instructions per token and wave of 8 channels x 16 states (26 of them the formulas').  bf16, 2048 channels, 16 states:
 // 8 x 2048 tokens 522 us with the ALU busy for 92 %, 4 x 2048 tokens 330 us, one wave per SIMD, 72 %; the sums over the workgroups 23 and 13 us.
+#include <algorithm>
+
 #include "kla_ssm_ops.hpp"
 
 namespace kla {
@@ -42,7 +44,7 @@ __global__ __launch_bounds__(kSsmBwdChannels * 8, S < 64 && sizeof(T) == 4 ? 2 :
     __shared__ float red[MAPS ? 1 : WAVES][MAPS ? 1 : CK][2 * S];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, o = lane & 7;
     const int block = blockIdx.x % blocks_c;
-    const long slot = blockIdx.x / blocks_c;
+    const long slot = a.slot0 + blockIdx.x / blocks_c;
     Segment g;
     if (!segment_of(a, slot, &g)) return;
     if (MAPS && g.t0 == g.seq.first) return;             // nothing stands before it
@@ -323,9 +325,10 @@ __global__ __launch_bounds__(256) void ssm_clear_kernel(SsmArgs<T> a, long row)
 
 // Gradients of B and C: the sums over the workgroups of a group's channels.  A stream: 134 MB in 23 us, 5.8 TB/s.
 template <typename T, int S>
-__global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const float* __restrict__ part, T* __restrict__ dB, T* __restrict__ dC, long M, int G, int blocks)
+__global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const float* __restrict__ part, T* __restrict__ dB, T* __restrict__ dC, long M, int G, int blocks,
+                                                         long first)
 {
-    const long e = (long)blockIdx.x * 256 + threadIdx.x;     // (token, 2 S)
+    const long e = first + (long)blockIdx.x * 256 + threadIdx.x;     // (token, 2 S)
     const int g = blockIdx.y;
     if (e >= M * 2 * S) return;
     float s = 0.f;
@@ -337,17 +340,23 @@ __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const float* __restrict
     else       dB[(tok * G + g) * S + n - S] = rounded<T>(s);
 }
 
+template <typename T, int S, bool MAPS, bool HASZ> static hipError_t ssm_bwd_pass(SsmArgs<T> a, int blocks_c, hipStream_t st)
+{
+    constexpr int THREADS = kSsmBwdChannels * 8;
+    for (long n; a.slot0 < a.slots; a.slot0 += n) {
+        n = std::min(a.slots - a.slot0, most_blocks(THREADS) / blocks_c);
+        hipLaunchKernelGGL((ssm_bwd_kernel<T, S, MAPS, HASZ>), dim3((unsigned)(blocks_c * n)), dim3(THREADS), 0, st, a, blocks_c);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
 template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, float* dA, T* dB, T* dC, float* dskip, float* ddelta_bias, hipStream_t st)
 {
     const int blocks_c = ssm_channel_blocks(a.D, a.G, kSsmBwdChannels);
-    const long blocks = blocks_c * a.slots, row = (long)a.D * (S + 2);
-    if (blocks > 0x7fffffffL || (a.M * 2 * S + 255) / 256 > 0x7fffffffL) return hipErrorInvalidConfiguration;
-    if (blocks > 0) {
-        const dim3 grid((unsigned)blocks), block(kSsmBwdChannels * 8);
+    const long row = (long)a.D * (S + 2);
+    if (a.slots > 0) {
         if (a.seg_state) {
-            if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, true>), grid, block, 0, st, a, blocks_c);
-            else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, true, false>), grid, block, 0, st, a, blocks_c);
-            if (const hipError_t e = hipGetLastError()) return e;
+            if (const hipError_t e = a.z ? ssm_bwd_pass<T, S, true, true>(a, blocks_c, st) : ssm_bwd_pass<T, S, true, false>(a, blocks_c, st)) return e;
             hipLaunchKernelGGL((ssm_join_bwd_kernel<T>), dim3((unsigned)(((long)a.D * S + 255) / 256), a.seqs.n_seq), dim3(256), 0, st, a, S);
             if (const hipError_t e = hipGetLastError()) return e;
         }
@@ -355,13 +364,11 @@ template <typename T, int S> static hipError_t ssm_bwd(const SsmArgs<T>& a, floa
             hipLaunchKernelGGL((ssm_clear_kernel<T>), dim3((unsigned)a.slots), dim3(256), 0, st, a, row);
             if (const hipError_t e = hipGetLastError()) return e;
         }
-        if (a.z) hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, true>), grid, block, 0, st, a, blocks_c);
-        else     hipLaunchKernelGGL((ssm_bwd_kernel<T, S, false, false>), grid, block, 0, st, a, blocks_c);
-        if (const hipError_t e = hipGetLastError()) return e;
+        if (const hipError_t e = a.z ? ssm_bwd_pass<T, S, false, true>(a, blocks_c, st) : ssm_bwd_pass<T, S, false, false>(a, blocks_c, st)) return e;
     }
-    if (a.M > 0) {
-        hipLaunchKernelGGL((ssm_sum_bc_kernel<T, S>), dim3((unsigned)((a.M * 2 * S + 255) / 256), a.G), dim3(256), 0, st, a.part_bc, dB, dC, a.M, a.G,
-                           blocks_c / a.G);
+    for (long first = 0; first < a.M * 2 * S; first += most_blocks(256) * 256) {
+        const long blocks = std::min((a.M * 2 * S - first + 255) / 256, most_blocks(256));
+        hipLaunchKernelGGL((ssm_sum_bc_kernel<T, S>), dim3((unsigned)blocks, a.G), dim3(256), 0, st, a.part_bc, dB, dC, a.M, a.G, blocks_c / a.G, first);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     return launch_column_sums(a.part_p, a.slots, {{(long)a.D * S, a.D, a.D}, {dA, dskip, ddelta_bias}}, st);
