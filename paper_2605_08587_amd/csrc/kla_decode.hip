@@ -204,13 +204,17 @@ __global__ __launch_bounds__(256) void beta_kernel(const T* __restrict__ k, cons
 template <typename T>
 hipError_t launch_beta(const T* k, const float* eta, float eps, float* beta, long n_rows, int dk, hipStream_t st)
 {
-    if (n_rows == 0) return hipSuccess;
     const int lpr = dk / 8;
-    const long rows_per_block = 256 / lpr;
-    const unsigned blocks = (unsigned)((n_rows + rows_per_block - 1) / rows_per_block);
-    if (dk == 64) hipLaunchKernelGGL((beta_kernel<T, 64>), dim3(blocks), dim3(256), 0, st, k, eta, eps, beta, n_rows);
-    else          hipLaunchKernelGGL((beta_kernel<T, 128>), dim3(blocks), dim3(256), 0, st, k, eta, eps, beta, n_rows);
-    return hipGetLastError();
+    const long rows_per_block = 256 / lpr, most = 0xffffffffL / 256 * rows_per_block;     // rows of a launch, whose threads are counted in 32 bits
+    for (long done = 0, n; done < n_rows; done += n) {
+        n = n_rows - done < most ? n_rows - done : most;
+        const unsigned blocks = (unsigned)((n + rows_per_block - 1) / rows_per_block);
+        const T* kp = k + done * dk;
+        if (dk == 64) hipLaunchKernelGGL((beta_kernel<T, 64>), dim3(blocks), dim3(256), 0, st, kp, eta + done, eps, beta + done, n);
+        else          hipLaunchKernelGGL((beta_kernel<T, 128>), dim3(blocks), dim3(256), 0, st, kp, eta + done, eps, beta + done, n);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 template hipError_t launch_beta<float>(const float*, const float*, float, float*, long, int, hipStream_t);
 template hipError_t launch_beta<bf16_t>(const bf16_t*, const float*, float, float*, long, int, hipStream_t);

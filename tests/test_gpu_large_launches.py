@@ -117,3 +117,14 @@ def test_scan_of_many_tokens(kla):
         for k in ("dB", "dC"):
             # (cut into other segments: two orders of the same sums, each rounded once)
             close(k, g[k][p], q[k], 2 * SCAN + 2.0 ** -8)
+
+
+def test_beta(kla):
+    """The recurrence's write coefficients of more than 2^29 tokens and heads."""
+    n, dk = 32 * MOST + 9, 64
+    print("beta", n, flush=True)
+    k, eta = torch.empty(n, dk, dtype=b16, device="cuda").fill_(0.5), torch.rand(n, device="cuda")
+    k[-9:] = _randn(9, dk)
+    beta = kla.kla_beta(k, eta, 1e-6)
+    for p in (slice(0, 7), slice(n - 40, n)):
+        assert torch.equal(bits(beta[p]), bits(kla.kla_beta(k[p], eta[p].clone(), 1e-6)))
