@@ -18,7 +18,7 @@ SOURCES = ["kla_api.hip", "kla_decode.hip", "kla_chunk_intra.hip", "kla_chunk_in
            "kla_layer_api.hip", "kla_layer_sums.hip", "kla_conv.hip", "kla_norm.hip", "kla_ssm.hip", "kla_ssm_bwd.hip"]
 BINDING_SOURCES = ["kla_binding.cpp", "kla_layer_binding.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-         # hipcc -O3 must not form packed-fp32 instructions on the test machines
+         # hipcc -O3 must not form packed-fp32 instructions: some of their forms have given wrong results
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # keep MFMA accumulators in ordinary VGPRs: the kernels scale and convert them between products,
          # and the AGPR form costs a register move per element each way

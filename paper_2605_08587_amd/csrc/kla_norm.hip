@@ -5,8 +5,8 @@
 //   f (e - n mean(e n)),  and  d_w = sum over the rows of dy n.
 // A row stays in the registers of its TPR threads between the sum and its use, so that every element is read once and written
 // once; nothing but the inputs is kept for the backward, which forms f again.  Bound by memory: bf16, 32768 rows of 1024 with an fp32 stream
-// forward 74 us (403 MB, 5.4 TB/s), backward 120 us (604 MB, 5.0 TB/s); 262144 heads of 256 with their gates forward 77 us (403 MB, 5.2 TB/s),
-// backward 129 us (671 MB, 5.2 TB/s); a large copy 4.8 TB/s.
+// forward 74 us (403 MB, 5.4 TB/s), backward 119 us (604 MB, 5.1 TB/s); 262144 heads of 256 with their gates forward 78 us (403 MB, 5.2 TB/s),
+// backward 135 us (671 MB, 5.0 TB/s); a large copy 4.8 TB/s.
 #include <algorithm>
 
 #include "kla_layer.hpp"

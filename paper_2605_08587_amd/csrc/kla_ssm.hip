@@ -4,9 +4,9 @@
 // with B, C shared by the channels of a group.  Everything is fp32 in registers.  Per token, channel and state: an exponential, two
 // products, two products with sums, that is six slots of the vector ALU (the exponential takes two), which bounds it and not memory.  Eight
 // lanes per channel and not one: the scalars of a token (steps, gates) are formed once per channel, and a channel's chain is its own wave's;
-// sixteen lanes have twice the scalar work per state (one sequence of 65536 tokens x 1024 channels x 16 states 773 us, eight 551 us).
-// That sequence: maps and outputs take 13 and 19 vector instructions per token and wave (8 channels) and keep the ALU busy for 96 and 93 %.
-// 4 x 2048 tokens x 2048 channels, training: 142 us, one wave per SIMD (69 ns a token), the ALU busy for 59 %; 8 x 2048: 224 us, 76 %.
+// sixteen lanes have twice the scalar work per state (one sequence of 65536 tokens x 1024 channels x 16 states 773 us against 576, both of one early
+// form; 548 now).  That sequence: maps and outputs take 13 and 18 vector instructions per token and wave (8 channels) and keep the ALU busy for 96 and
+// 93 %.  4 x 2048 tokens x 2048 channels, training: 146 us, one wave per SIMD (71 ns a token), the ALU busy for 56 %; 8 x 2048: 220 us, 76 %.
 #include <algorithm>
 
 #include "kla_ssm_ops.hpp"

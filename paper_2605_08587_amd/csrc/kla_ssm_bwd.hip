@@ -9,7 +9,7 @@
 // stay in registers for the way back.  Sums over channels go through the wave by lane swaps that halve what is left
 // at every step, then over the four waves through LDS, then over the workgroups in a kernel of their own: no atomics.
 // The vector ALU bounds it: 55 instructions per token and wave of 8 channels x 16 states (26 of them the formulas').  bf16, 2048 channels, 16 states:
-// 8 x 2048 tokens 522 us with the ALU busy for 92 %, 4 x 2048 tokens 330 us, one wave per SIMD, 72 %; the sums over the workgroups 23 and 13 us.
+// 8 x 2048 tokens 520 us with the ALU busy for 92 %, 4 x 2048 tokens 325 us, one wave per SIMD, 72 %; the sums over the workgroups 23 and 13 us.
 #include <algorithm>
 
 #include "kla_ssm_ops.hpp"
