@@ -460,6 +460,56 @@ int kla_gated_norm_bwd(const void *x, long ld_x, const void *gate, long ld_gate,
                        const void *d_y, void *dx, void *d_gate, float *dweight, long M, int H, int D, kla_dtype dt,
                        void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Softmax attention, the other mixing layer of hybrid stacks: over whole sequences (forward and backward), and for new
+ * tokens over a paged cache of earlier ones.  Query i of a sequence sees keys j of the same sequence:
+ *     s_ij = scale q_i . k_j,   p_ij = exp(s_ij) / sum_j exp(s_ij),   o_i = sum_j p_ij v_j,   lse_i = log sum_j exp(s_ij)
+ * with KLA_ATTN_CAUSAL j <= i only, and with window > 0 (causal only) j > i - window only.  H query heads share Hk key heads,
+ * H a multiple of Hk: query head h reads key head h / (H / Hk).
+ *   - q [N, T, H, D], k, v [N, T, Hk, D] dt: tokens ld_q, ld_k, ld_v elements apart (column ranges of a wider tensor), the heads of a
+ *     token contiguous.  D is 64 or 128.  Rows start at multiples of 16 bytes: pointers and strides are (else KLA_ERR_ALIGN).
+ *   - T H / Hk at most 2^30, H D and strides at most 2^28 elements, scale positive and finite.
+ *   - Scores, softmax and sums are fp32; weights are rounded to dt where they are multiplied with values, outputs once.
+ *     Results are deterministic (no atomics).  A key that a query does not see has no part in its row, also where it holds a NaN.  A
+ *     row whose scores are all -inf, or one of whose scores is +inf or NaN, is NaN.
+ *   - An output must not overlap an input.
+ * ------------------------------------------------------------------------------------------------------------------ */
+enum { KLA_ATTN_CAUSAL = 1 };
+
+/*   o           [N, T, H, D] dt                     out
+ *   lse         [N, T, H] fp32                      out  or NULL if unwanted; what the backward takes */
+int kla_attn_fwd(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
+                 void *o, float *lse, float scale, int window,
+                 const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                 int N, int T, int H, int Hk, int D, kla_dtype dt, void *hip_stream, unsigned opts);
+
+/* New tokens of n_seq (packed) or N sequences behind `cached` earlier ones each: token t of sequence s stands at position cached[s] + t
+ * and sees the sequence's cached tokens and the new ones up to itself (and in its window).  The keys and values of the new tokens are
+ * stored in the cache too; `cached` stays as it is, for the other layers of a step.
+ *   k_cache, v_cache [n_pages, Hk, page, D] dt      in/out  page a power of two, 16 to 1024
+ *   page_table  [sequences, max_pages] int32        in   device; rows ld_table apart: entry p holds the page of positions p page ..
+ *   cached      [sequences] int32                   in   device; taken as at least 0 and at most max_pages page
+ *   o           [N, T, H, D] dt, lse [N, T, H] fp32 or NULL    out
+ *   max_len     a bound of cached + new tokens for how the work is cut: results beyond it are right, but slower
+ * Only entries of positions in some query's window that lie below `cached` are read, and those of new tokens.  An entry that is no page (below 0 or
+ * from n_pages on) reads as the nearest page that is one, and nothing is stored through it; nor are new tokens at positions from
+ * max_pages page on.  A page that new tokens go to must not be read or written through another entry in the same call.
+ * max_pages page at most 2^30.  workspace 256-byte aligned. */
+size_t kla_attn_extend_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t *cu_seqlens_host, int n_seq,
+                                       int max_len, kla_dtype dt);
+int kla_attn_extend(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
+                    void *k_cache, void *v_cache, const int32_t *page_table, long ld_table, const int32_t *cached,
+                    void *o, float *lse, float scale, int window,
+                    const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                    int N, int T, int H, int Hk, int D, int n_pages, int page, int max_pages, int max_len,
+                    kla_dtype dt, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* One new token for B sequences: q, o [B, H, D], k, v [B, Hk, D]; workspace as for kla_attn_extend with N = B, T = 1. */
+int kla_attn_step(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
+                  void *k_cache, void *v_cache, const int32_t *page_table, long ld_table, const int32_t *cached,
+                  void *o, float scale, int window, int B, int H, int Hk, int D, int n_pages, int page, int max_pages,
+                  int max_len, kla_dtype dt, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /*
  * Test hook: the per-chunk objects the first stage of kla_chunk_fwd leaves in its workspace,
  * unpacked to plain row-major fp32 so that they can be compared one by one with eqs. (6)-(7).

@@ -125,7 +125,7 @@ def lib():
                 raise RuntimeError("libkla.so is not built: run `python -m paper_2605_08587_amd.build` "
                                    "(there is no CPU fallback)")
             l = ctypes.CDLL(LIB_PATH)
-            for name, (res, args) in {**_SIGNATURES, **layer.SIGNATURES}.items():
+            for name, (res, args) in {**_SIGNATURES, **layer.SIGNATURES, **attention.SIGNATURES}.items():
                 fn = getattr(l, name)
                 fn.restype, fn.argtypes = res, args
             _native, _lib = _load_native(l), l
@@ -670,3 +670,5 @@ from . import layer  # noqa: E402  (needs the names above)
 from .layer import (KLA_LAYER_GATE_FIRST, KLA_LAYER_SIGMOID, KLA_LAYER_SILU, KLA_LAYER_SOFTPLUS,  # noqa: E402, F401
                     kla_add_norm, kla_add_norm_bwd, kla_add_norm_fwd, kla_conv, kla_conv_bwd, kla_conv_fwd, kla_conv_step, kla_gated_norm,
                     kla_gated_norm_bwd, kla_gated_norm_fwd, kla_ssm, kla_ssm_bwd, kla_ssm_fwd, kla_ssm_step)
+from . import attention  # noqa: E402
+from .attention import KLA_ATTN_CAUSAL, kla_attn_extend, kla_attn_fwd, kla_attn_step  # noqa: E402, F401

@@ -1,0 +1,141 @@
+"""Softmax attention beside the recurrences of a hybrid stack (include/kla.h): over whole sequences, and for new tokens over a paged cache.
+Argument marshalling only, as in the package itself: every step runs in the HIP kernels.
+
+kla_attn_fwd / kla_attn_bwd are the two directions and kla_attn the differentiable call; kla_attn_extend takes new tokens of several sequences over
+their cached ones, kla_attn_step one token of each.  q [..., H, D] and k, v [..., Hk, D] may be column ranges of a wider tensor: the heads
+of a token are contiguous, the tokens evenly spaced, and a row starts at a multiple of 16 bytes.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import _binding, _check, _dev, _dt, _ptr, _stream, _written, _ws_bytes, lib
+from .layer import _batch, _call, _host, _native, _on_gpu, _rows, _sizes, _workspace
+
+KLA_ATTN_CAUSAL = 1
+
+_vp, _i, _l, _f, _z, _u = ctypes.c_void_p, ctypes.c_int, ctypes.c_long, ctypes.c_float, ctypes.c_size_t, ctypes.c_uint
+_SEQS = [_vp, _vp, _i]
+_IN = [_vp, _l] * 3
+_CACHE = [_vp, _vp, _vp, _l, _vp]
+SIGNATURES = {
+    "kla_attn_fwd": (_i, [*_IN, _vp, _vp, _f, _i, *_SEQS, *[_i] * 6, _vp, _u]),
+    "kla_attn_extend_workspace_bytes": (_z, [*[_i] * 5, _vp, *[_i] * 3]),
+    "kla_attn_extend": (_i, [*_IN, *_CACHE, _vp, _vp, _f, _i, *_SEQS, *[_i] * 10, _vp, _z, _vp]),
+    "kla_attn_step": (_i, [*_IN, *_CACHE, _vp, _f, _i, *[_i] * 9, _vp, _z, _vp]),
+}
+
+
+def _scale(scale, D):
+    return D ** -0.5 if scale is None else float(scale)
+
+
+def _heads(q, k, v, lead):
+    """lead: number of leading dimensions; returns H, Hk, D, the type and the token strides of q, k, v."""
+    if q.dim() != lead + 2 or k.dim() != lead + 2:
+        raise ValueError("q must be [%s, H, D] and k, v [%s, Hk, D]" % (("N, T",) * 2 if lead == 2 else ("B",) * 2))
+    at, (H, D), Hk = tuple(q.shape[:lead]), q.shape[-2:], k.shape[-2]
+    dt = _dt(q)
+    _sizes(*q.shape, Hk)
+    _check("k", k, (*at, Hk, D), q.dtype)
+    _check("v", v, (*at, Hk, D), q.dtype)
+    if Hk == 0 or H % Hk:
+        raise ValueError("%d query heads cannot share %d key heads evenly" % (H, Hk))
+    _on_gpu(q, k, v)
+    return H, Hk, D, dt, (_rows("q", q, 2), _rows("k", k, 2), _rows("v", v, 2))
+
+
+def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, want_lse=True, out=None, lse=None):
+    """Softmax attention of q [N,T,H,D] over k, v [N,T,Hk,D] of the same sequence (D 64 or 128, H a multiple of Hk): returns (o, lse), lse [N,T,H]
+    fp32 the logarithms of the rows' sums (None unless want_lse).  causal: a token sees those up to itself, and with window > 0 only the last
+    `window` of them; scale: of the scores, D ** -0.5 by default.  Packed batches by cu_seqlens as in kla_chunk_fwd."""
+    host = _host(cu_seqlens, cu_seqlens_host)
+    H, Hk, D, dt, ld = _heads(q, k, v, 2)
+    N, T = q.shape[:2]
+    _, cu_hp, n_seq, _n = _batch(q, cu_seqlens, host)
+    _sizes(window)
+    _check("out", out, (N, T, H, D), q.dtype)
+    _check("lse", lse, (N, T, H), torch.float32)
+    _on_gpu(cu_seqlens, out, lse)
+    _dev(cu_seqlens, out, lse)
+    given = out, lse
+    if out is None:
+        out = torch.empty((N, T, H, D), dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((N, T, H), dtype=torch.float32, device=q.device)
+    _call("kla_attn_fwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(out), _ptr(lse), _scale(scale, D), int(window), _ptr(cu_seqlens), cu_hp,
+          n_seq, N, T, H, Hk, D, dt, _stream(), KLA_ATTN_CAUSAL if causal else 0)
+    _written(*given)
+    return out, lse
+
+
+def _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, n):
+    if k_cache.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k_cache, v_cache must be [pages, Hk, page, D] and page_table [sequences, max_pages]")
+    n_pages, page, max_pages = k_cache.shape[0], k_cache.shape[2], page_table.shape[1]
+    _check("k_cache", k_cache, (n_pages, Hk, page, D), q.dtype)
+    _check("v_cache", v_cache, (n_pages, Hk, page, D), q.dtype)
+    _check("page_table", page_table, (n, max_pages), torch.int32)
+    _check("cached", cached, (n,), torch.int32)
+    _sizes(n_pages, page, max_pages, max_pages * page)
+    _on_gpu(k_cache, v_cache, page_table, cached)
+    _dev(k_cache, v_cache, cached)
+    return n_pages, page, max_pages, _rows("page_table", page_table)
+
+
+def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, window=0, cu_seqlens=None, cu_seqlens_host=None, max_len=None,
+                    want_lse=False, out=None, lse=None, workspace=None):
+    """New tokens of several sequences over a paged cache: q [N,T,H,D], k, v [N,T,Hk,D] (packed batches by cu_seqlens) stand behind cached [sequences]
+    (int32) earlier tokens each and see those and the new ones up to themselves (the last `window` of them, if it is not 0).  The keys and
+    values of position p of sequence s stand in k_cache, v_cache [pages,Hk,page,D] at [page_table[s, p // page], :, p % page] (page_table
+    int32, page a power of two from 16 to 1024); those of the new tokens are stored there.  cached is not advanced.  Returns o, with want_lse
+    (o, lse).  max_len: a bound of cached + new tokens, if the caller knows a closer one than the table's width (only how the work
+    is cut depends on it)."""
+    host = _host(cu_seqlens, cu_seqlens_host)
+    H, Hk, D, dt, ld = _heads(q, k, v, 2)
+    N, T = q.shape[:2]
+    _, cu_hp, n_seq, n = _batch(q, cu_seqlens, host)
+    _sizes(window)
+    n_pages, page, max_pages, ld_table = _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, n)
+    _check("out", out, (N, T, H, D), q.dtype)
+    _check("lse", lse, (N, T, H), torch.float32)
+    _on_gpu(cu_seqlens, out, lse, workspace)
+    _dev(cu_seqlens, out, lse, workspace)
+    max_len = max_pages * page if max_len is None else int(max_len)
+    _sizes(max_len)
+    if workspace is None:
+        workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, max_len, dt)), q)
+    given = out, lse
+    if out is None:
+        out = torch.empty((N, T, H, D), dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((N, T, H), dtype=torch.float32, device=q.device)
+    _call("kla_attn_extend", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(k_cache), _ptr(v_cache), _ptr(page_table), ld_table, _ptr(cached),
+          _ptr(out), _ptr(lse), _scale(scale, D), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, n_pages, page, max_pages, max_len, dt,
+          _ptr(workspace), _ws_bytes(workspace), _stream())
+    _written(k_cache, v_cache, *given)
+    return (out, lse) if lse is not None else out
+
+
+def kla_attn_step(q, k, v, k_cache, v_cache, page_table, cached, scale=None, window=0, max_len=None, out=None, workspace=None):
+    """One new token of B sequences: q [B,H,D], k, v [B,Hk,D]; otherwise as kla_attn_extend.  Returns o [B,H,D]."""
+    H, Hk, D, dt, ld = _heads(q, k, v, 1)
+    B = q.shape[0]
+    _sizes(window)
+    n_pages, page, max_pages, ld_table = _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, B)
+    _check("out", out, (B, H, D), q.dtype)
+    _on_gpu(out, workspace)
+    _dev(out, workspace)
+    max_len = max_pages * page if max_len is None else int(max_len)
+    _sizes(max_len)
+    if workspace is None:
+        workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(B, 1, H, Hk, D, None, 0, max_len, dt)), q)
+    given = out
+    if out is None:
+        out = torch.empty((B, H, D), dtype=q.dtype, device=q.device)
+    _call("kla_attn_step", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(k_cache), _ptr(v_cache), _ptr(page_table), ld_table, _ptr(cached),
+          _ptr(out), _scale(scale, D), int(window), B, H, Hk, D, n_pages, page, max_pages, max_len, dt, _ptr(workspace), _ws_bytes(workspace), _stream())
+    _written(k_cache, v_cache, given)
+    return out

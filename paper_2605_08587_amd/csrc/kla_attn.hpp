@@ -1,0 +1,222 @@
+// What the attention kernels share: 32x32 matrix products on 16-byte operands, swizzled tiles of rows in LDS, where a tile of query rows
+// lies in its batch, and the launchers' arguments.
+//
+// All products are 32x32 tiles accumulated in fp32.  A lane is (n, h) = (lane % 32, lane / 32).
+//
+//   accumulator     : lane (n, h) holds rows 8 (e / 4) + 4 h + e % 4 of column n, e = 0..15
+//   "slot" (16 B)   : of operand row n (A) or operand column n (B), contraction indices
+//                       rows of memory : the 16-byte piece 2 c + h of row n, c = 0, 1, ..
+//                       from registers : of an accumulator whose row index is the next contraction index, registers 8 c .. 8 c + 7 rounded
+//                                        to bf16, or 4 c .. 4 c + 3 in fp32: rows 16 c + 4 h + {0..3, 8..11}, or 8 c + 4 h + {0..3}
+//
+// The hardware pairs element i of an A slot with element i of a B slot, half by half, so any order of the contraction index serves as long as both
+// use the same.  Scores are formed transposed, S^T = K Q^T: a lane then has one query, its softmax needs one exchange between the halves
+// of a wave, and exp(S^T) is the B operand of O^T += V^T P^T as it lies.
+#pragma once
+#include "kla_bf16_ops.hpp"
+#include "kla_layer.hpp"
+
+namespace kla {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+constexpr unsigned kAttnCausal = 1u;                     // (the value of KLA_ATTN_CAUSAL in include/kla.h)
+
+// ---- products ---------------------------------------------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ void mma32x32(floatx16& acc, u32x4 a, u32x4 b)
+{
+    if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    } else {
+        const floatx4 x = __builtin_bit_cast(floatx4, a), y = __builtin_bit_cast(floatx4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc, 0, 0, 0);
+    }
+}
+// Rows of an accumulator that one slot holds per half: an accumulator gives 16 / kSlot<T> slots of kSlot<T> registers
+template <typename T> constexpr int kSlot = 16 / (int)sizeof(T);
+template <typename T, int C> __device__ __forceinline__ u32x4 slot_of(const floatx16& s)
+{
+    if constexpr (sizeof(T) == 2) {
+        const u32x4 r = {pack_bf16x2(s[8 * C], s[8 * C + 1]), pack_bf16x2(s[8 * C + 2], s[8 * C + 3]), pack_bf16x2(s[8 * C + 4], s[8 * C + 5]),
+                         pack_bf16x2(s[8 * C + 6], s[8 * C + 7])};
+        return r;
+    } else {
+        const floatx4 r = {s[4 * C], s[4 * C + 1], s[4 * C + 2], s[4 * C + 3]};
+        return __builtin_bit_cast(u32x4, r);
+    }
+}
+// the accumulator row of register e is acc_row(e) + 4 h
+__host__ __device__ constexpr int acc_row(int e) { return 8 * (e >> 2) + (e & 3); }
+
+// Where an operand's row that a mask hides holds an infinity or a NaN, its zero weight does not: 0 x inf.  Kernels that find their result not finite
+// compute it again with products that keep such rows apart: a_fin has zeros for the elements of a that are not finite, a_sgn has +-1 for infinities
+// and 0 elsewhere, a_bad 1 for whatever is not finite.  With b's signs and the mask's ones, two more products count what a column takes in.
+template <typename T> struct Apart { u32x4 fin, sgn, bad; };
+template <typename T> __device__ __forceinline__ Apart<T> apart(u32x4 a)
+{
+    Apart<T> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            uint32_t fin = 0, sgn = 0, bad = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t x = (a[i] >> (16 * j)) & 0xffffu;
+                const bool b = (x & 0x7f80u) == 0x7f80u, inf = (x & 0x7fffu) == 0x7f80u;
+                fin |= (b ? 0u : x) << (16 * j);
+                sgn |= (inf ? 0x3f80u | (x & 0x8000u) : 0u) << (16 * j);
+                bad |= (b ? 0x3f80u : 0u) << (16 * j);
+            }
+            r.fin[i] = fin; r.sgn[i] = sgn; r.bad[i] = bad;
+        } else {
+            const uint32_t x = a[i];
+            const bool b = (x & 0x7f800000u) == 0x7f800000u, inf = (x & 0x7fffffffu) == 0x7f800000u;
+            r.fin[i] = b ? 0u : x;
+            r.sgn[i] = inf ? 0x3f800000u | (x & 0x80000000u) : 0u;
+            r.bad[i] = b ? 0x3f800000u : 0u;
+        }
+    }
+    return r;
+}
+// +-1 for values that are not zero (0 for NaN: what they meet becomes one)
+__device__ __forceinline__ float sign_of(float x) { return x > 0.f ? 1.f : x < 0.f ? -1.f : 0.f; }
+// what a column takes in: `signs` the sum of the signs of its infinite terms, `count` how many terms are not finite
+__device__ __forceinline__ float not_finite(float signs, float count)
+{
+    return count == 0.f ? 0.f : signs == count ? __builtin_inff() : signs == -count ? -__builtin_inff() : __builtin_nanf("");
+}
+__device__ __forceinline__ bool finite(const floatx16& x)
+{
+    float t = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t = fmaf(x[e], 0.f, t);
+    return t == 0.f;
+}
+
+// ---- tiles of rows in LDS ---------------------------------------------------------------------------------------------------------
+// Rows of D elements stand as pieces of 16 bytes; piece p of a row is at position p ^ row_swz(row).  Slot reads of 32 rows (16 lanes a cycle:
+// rows {0-3, 12-15, 20-27} or the others) and transposing reads (32 lanes a cycle: four rows of 64 bytes) both then spread over the banks.
+template <int PIECES> __host__ __device__ constexpr int row_swz(int row)
+{
+    if (PIECES == 8) return ((row >> 1 & 1) << 2) | (row >> 2 & 3);
+    return ((row & 3) << 2) | (row >> 2 & 3);
+}
+// 16 bytes per lane from the lane's address to LDS at lds_wave_base + 16 lane (as dma16, with an address of 64 bits)
+__device__ __forceinline__ void dma16_from(const char* lane_address, char* lds_wave_base)
+{
+    const uint32_t m = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) char*)lds_wave_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(lane_address), "s"(m) : "memory");
+}
+// A tile of rows of D elements of T
+template <typename T, int D> struct RowTile {
+    static constexpr int RB = D * (int)sizeof(T);        // bytes of a row
+    static constexpr int PIECES = RB / 16;
+    static constexpr int NC = RB / 32;                   // slots of a row per half
+    static constexpr int RPI = 1024 / RB;                // rows of one copy instruction
+    // Row slots: offset of row n, piece 2 c + h (rows 32 i + n: + 32 i RB)
+    static __device__ __forceinline__ int row_offset(int n, int h) { return n * RB + ((h ^ row_swz<PIECES>(n)) * 16); }
+    static __device__ __forceinline__ u32x4 row_slot(const char* tile, int row_off, int c) { return ld16(tile + (row_off ^ (32 * c))); }
+    // Column slots, the contraction along rows: column 32 dt + n, rows as an accumulator's registers give them
+    static __device__ __forceinline__ int col_offset(int lane)
+    {
+        const int n = lane & 31, h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // source lane (a, c) of sixteen: row 4 h + a, columns 4 c .. 4 c + 3 of sixteen
+            const int a = lane >> 2 & 3, c = lane & 3, s = lane >> 4 & 1, row = 4 * h + a;
+            return row * RB + (((2 * s + (c >> 1)) ^ row_swz<PIECES>(row)) * 16) + (c & 1) * 8;
+        } else {
+            return 4 * h * RB + (((n >> 2) ^ h) * 16) + (n & 3) * 4;
+        }
+    }
+    // slot C of the 32 rows from `tile` on
+    template <int C, int DT> static __device__ __forceinline__ u32x4 col_slot(const char* tile, int col_off)
+    {
+        if constexpr (sizeof(T) == 2) {
+            const u32x2 lo = lds_read_tr(tile + (col_off ^ (64 * DT)) + 16 * C * RB), hi = lds_read_tr(tile + (col_off ^ (64 * DT) ^ 32) + (16 * C + 8) * RB);
+            return u32x4{lo.x, lo.y, hi.x, hi.y};
+        } else {
+            u32x4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                r[i] = *reinterpret_cast<const uint32_t*>(tile + (col_off ^ (64 * i) ^ (32 * (C & 1)) ^ (128 * DT)) + (8 * C + i) * RB);
+            return r;
+        }
+    }
+};
+static_assert(row_swz<16>(8) == 2 && row_swz<8>(8) == 2 && row_swz<16>(16) == 0 && row_swz<8>(16) == 0, "col_slot's constants");
+
+// All of this wave's copies have landed, and its LDS reads are done; then every wave's.
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_copies_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// max and sum over the two halves of a wave, in every lane
+__device__ __forceinline__ float halves_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// ---- rows of a batch --------------------------------------------------------------------------------------------------------------
+// The query heads of one key head are rows of their own: row r of (sequence, key head) is token r / G, head hk G + r % G.  A key head's tiles of
+// `rows` rows (packed batches: tile `idx` counted over the sequences in order); false: there is none.
+struct RowPlace { int n; int tile; int len; long tok0; };
+__device__ __forceinline__ bool find_rows(const Seqs& s, int G, int rows, long per, long idx, RowPlace* p)
+{
+    if (!s.cu) {                                         // tiles of one number of all sequences beside each other
+        p->n = (int)(idx % s.n_seq);
+        p->tile = (int)(idx / s.n_seq);
+        p->len = s.T;
+        p->tok0 = (long)p->n * s.T;
+        return p->tile < per;
+    }
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < s.n_seq; base += 64) {
+        const int n = min(base + lane, s.n_seq - 1);
+        const int c0 = s.cu[n], len = base + lane < s.n_seq ? s.cu[n + 1] - c0 : 0;
+        const int mine = (int)(((long)len * G + rows - 1) / rows);
+        int sum = mine;                                  // inclusive prefix sum over the lanes
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += o;
+        }
+        const unsigned long long here = __ballot(idx < sum);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            p->n = base + l;
+            p->tile = (int)idx - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(mine, l));
+            p->len = __builtin_amdgcn_readlane(len, l);
+            p->tok0 = __builtin_amdgcn_readlane(c0, l);
+            return true;
+        }
+        idx -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+// ---- launchers --------------------------------------------------------------------------------------------------------------------
+template <typename T> struct AttnArgs {
+    const T* q; long ld_q; const T* k; long ld_k; const T* v; long ld_v;                  // rows of new tokens
+    T* o; float* lse;                                    // lse: or NULL
+    Seqs seqs; int H, Hk, G;
+    float scale; int window; bool causal;
+    // the cache of earlier tokens: pages [n_pages][Hk][1 << page_shift][D]; table [n_seq][max_pages], rows ld_table apart
+    T* k_cache; T* v_cache; const int* table; long ld_table; const int* cached; int n_pages, page_shift, max_pages;
+    // keys in `splits` parts: part_o [splits][tokens H][D] and part_lse [splits][tokens H] (base 2)
+    int splits; float* part_o; float* part_lse; long M;
+    long tiles, per;                                     // tiles of query rows of a key head: in all; of one sequence (fixed lengths)
+    long unit0;                                          // first workgroup of this launch
+};
+// How the forward's work is cut: rows of a tile (128: four waves of 32 rows that share tiles of keys; 32: four waves that share the rows and divide the
+// keys) and parts of the keys.
+struct AttnPlan { int rows; int splits; };
+template <typename T> hipError_t launch_attn_fwd(const AttnArgs<T>& a, int D, const AttnPlan& p, bool paged, hipStream_t st);
+template <typename T> hipError_t launch_attn_join(const AttnArgs<T>& a, int D, hipStream_t st);
+
+}  // namespace kla

@@ -1,0 +1,175 @@
+// C ABI of softmax attention (declared in include/kla.h): argument validation, how the work is cut, workspace carving and launch sequencing.  No
+// allocation, no state, nothing read from the environment; everything is enqueued on the caller's stream.
+#include <limits.h>
+#include <math.h>
+
+#include "kla_args.hpp"
+#include "kla_attn.hpp"
+
+namespace {
+
+using kla::bf16_t;
+
+static_assert(KLA_ATTN_CAUSAL == (int)kla::kAttnCausal, "option bits");
+
+constexpr int kMaxAttnRows = 1 << 30;                    // tokens times query heads of a key head, and positions (32-bit numbers)
+constexpr long kMaxAttnStride = 1L << 28;                // elements from one token to the next
+
+struct AttnSizes { int N, T, H, Hk, D; };
+int attn_sizes(const AttnSizes& z, int dt)
+{
+    if (!dt_ok(dt)) return KLA_ERR_DTYPE;
+    if (z.N < 0 || z.T < 0 || z.H <= 0 || z.Hk <= 0 || z.H % z.Hk || (z.D != 64 && z.D != 128) || (long)z.H * z.D > kMaxAttnStride ||
+        (long)z.T * (z.H / z.Hk) > kMaxAttnRows)
+        return KLA_ERR_SHAPE;
+    return KLA_OK;
+}
+int attn_check(const AttnSizes& z, long ld_q, long ld_k, long ld_v, float scale, int window, int dt)
+{
+    if (const int e = attn_sizes(z, dt)) return e;
+    if (ld_q < (long)z.H * z.D || ld_k < (long)z.Hk * z.D || ld_v < (long)z.Hk * z.D || ld_q > kMaxAttnStride || ld_k > kMaxAttnStride || ld_v > kMaxAttnStride ||
+        !(scale > 0.f) || isinf(scale) || window < 0)
+        return KLA_ERR_SHAPE;
+    const long vec = 16 / (long)elem_bytes(dt);
+    return ld_q % vec || ld_k % vec || ld_v % vec ? KLA_ERR_ALIGN : KLA_OK;
+}
+// Tiles of `rows` query rows of one key head
+long attn_tiles(const kla::Seqs& s, const int32_t* cu_host, int G, int rows, long* per)
+{
+    *per = ((long)s.T * G + rows - 1) / rows;
+    if (!s.cu) return *per * s.n_seq;
+    long tiles = 0;
+    for (int i = 0; i < s.n_seq; ++i) tiles += ((long)(cu_host[i + 1] - cu_host[i]) * G + rows - 1) / rows;
+    return tiles;
+}
+int longest(const kla::Seqs& s, const int32_t* cu_host)
+{
+    if (!s.cu) return s.n_seq ? s.T : 0;
+    int most = 0;
+    for (int i = 0; i < s.n_seq; ++i) most = cu_host[i + 1] - cu_host[i] > most ? cu_host[i + 1] - cu_host[i] : most;
+    return most;
+}
+// The forward over whole sequences: four waves of 32 rows each to a workgroup, which share every tile of keys, unless that gives too few workgroups
+// for the CUs; then four waves share 32 rows and divide the keys.
+kla::AttnPlan attn_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
+{
+    long per;
+    return {attn_tiles(s, cu_host, G, 128, &per) * Hk >= 256 ? 128 : 32, 1};
+}
+// New tokens over a cache of up to max_len tokens.
+kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk, int max_len)
+{
+    kla::AttnPlan p;
+    p.rows = (long)longest(s, cu_host) * G <= 32 ? 32 : 128;
+    long per;
+    const long units = attn_tiles(s, cu_host, G, p.rows, &per) * Hk;
+    if (units == 0) { p.splits = 1; return p; }
+    const long want = p.rows == 32 ? (1024 + units - 1) / units : (512 + units - 1) / units;
+    const long most = p.rows == 32 ? ((long)max_len + 127) / 128 : ((long)max_len + 255) / 256;
+    p.splits = (int)(want < most ? want : most);
+    if (p.splits < 1) p.splits = 1;
+    if (p.splits > 64) p.splits = 64;
+    return p;
+}
+template <typename T>
+kla::AttnArgs<T> attn_args(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* o, float* lse, const kla::Seqs& s, long M,
+                           const AttnSizes& z, float scale, int window, unsigned opts)
+{
+    kla::AttnArgs<T> a = {};
+    a.q = static_cast<const T*>(q); a.ld_q = ld_q; a.k = static_cast<const T*>(k); a.ld_k = ld_k; a.v = static_cast<const T*>(v); a.ld_v = ld_v;
+    a.o = static_cast<T*>(o); a.lse = lse; a.seqs = s; a.H = z.H; a.Hk = z.Hk; a.G = z.H / z.Hk;
+    a.scale = scale; a.window = window; a.causal = opts & KLA_ATTN_CAUSAL; a.splits = 1; a.M = M;
+    return a;
+}
+struct ExtendWork { float *part_o, *part_lse; size_t bytes; };
+ExtendWork extend_work(char* base, const kla::AttnPlan& p, long M, int H, int D)
+{
+    Carve c{base};
+    ExtendWork w = {};
+    if (p.splits > 1) {
+        w.part_o = c.take<float>((size_t)p.splits * M * H * D);
+        w.part_lse = c.take<float>((size_t)p.splits * M * H);
+    }
+    w.bytes = c.used;
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* o, float* lse, float scale, int window,
+                 const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int n_seq, int N, int T, int H, int Hk, int D, kla_dtype dt, void* hip_stream,
+                 unsigned opts)
+{
+    kla::Seqs s;
+    long M;
+    const AttnSizes z = {N, T, H, Hk, D};
+    if (const int e = attn_check(z, ld_q, ld_k, ld_v, scale, window, dt)) return e;
+    if ((opts & ~(unsigned)KLA_ATTN_CAUSAL) || (window && !(opts & KLA_ATTN_CAUSAL))) return KLA_ERR_SHAPE;
+    if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
+    if (M > 0 && (!q || !k || !v || !o)) return KLA_ERR_NULL;
+    if (M > 0 && (o == q || o == k || o == v)) return KLA_ERR_SHAPE;                   // (other workgroups still read them)
+    if (!aligned(16, {q, k, v, o}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
+    const kla::AttnPlan p = attn_plan(s, cu_seqlens_host, H / Hk, Hk);
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    auto run = [&](auto a) {
+        a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);
+        return status(kla::launch_attn_fwd(a, D, p, false, st));
+    };
+    return dt == KLA_BF16 ? run(attn_args<bf16_t>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, opts))
+                          : run(attn_args<float>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, opts));
+}
+
+size_t kla_attn_extend_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t* cu_seqlens_host, int n_seq, int max_len, kla_dtype dt)
+{
+    kla::Seqs s;
+    long M;
+    if (attn_sizes({N, T, H, Hk, D}, dt) || max_len < 0 || take_seqs(n_seq > 0 ? cu_seqlens_host : nullptr, cu_seqlens_host, n_seq, N, T, &s, &M)) return 0;
+    return extend_work(nullptr, extend_plan(s, cu_seqlens_host, H / Hk, Hk, max_len), M, H, D).bytes;
+}
+
+int kla_attn_extend(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* k_cache, void* v_cache, const int32_t* page_table,
+                    long ld_table, const int32_t* cached, void* o, float* lse, float scale, int window, const int32_t* cu_seqlens_dev,
+                    const int32_t* cu_seqlens_host, int n_seq, int N, int T, int H, int Hk, int D, int n_pages, int page, int max_pages, int max_len,
+                    kla_dtype dt, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    kla::Seqs s;
+    long M;
+    const AttnSizes z = {N, T, H, Hk, D};
+    if (const int e = attn_check(z, ld_q, ld_k, ld_v, scale, window, dt)) return e;
+    int shift = 4;
+    while (shift < 10 && (1 << shift) < page) ++shift;
+    if (page != 1 << shift || n_pages <= 0 || max_pages <= 0 || ((long)max_pages << shift) > kMaxAttnRows || ld_table < max_pages || max_len < 0)
+        return KLA_ERR_SHAPE;
+    if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
+    if (M > 0 && (!q || !k || !v || !o || !k_cache || !v_cache || !page_table || !cached)) return KLA_ERR_NULL;
+    if (M > 0 && (o == q || o == k || o == v || k_cache == v_cache || k_cache == q || k_cache == k || k_cache == v || k_cache == o || v_cache == q ||
+                  v_cache == k || v_cache == v || v_cache == o))
+        return KLA_ERR_SHAPE;
+    if (!aligned(16, {q, k, v, o, k_cache, v_cache}) || !aligned(4, {lse, page_table, cached})) return KLA_ERR_ALIGN;
+    const kla::AttnPlan p = extend_plan(s, cu_seqlens_host, H / Hk, Hk, max_len);
+    const ExtendWork w = extend_work(static_cast<char*>(workspace), p, M, H, D);
+    if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    auto run = [&](auto a) {
+        a.k_cache = static_cast<decltype(a.k_cache)>(k_cache); a.v_cache = static_cast<decltype(a.v_cache)>(v_cache);
+        a.table = page_table; a.ld_table = ld_table; a.cached = cached; a.n_pages = n_pages; a.page_shift = shift; a.max_pages = max_pages;
+        a.splits = p.splits; a.part_o = w.part_o; a.part_lse = w.part_lse;
+        a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);
+        if (const hipError_t e = kla::launch_attn_fwd(a, D, p, true, st)) return status(e);
+        return p.splits > 1 ? status(kla::launch_attn_join(a, D, st)) : (int)KLA_OK;
+    };
+    return dt == KLA_BF16 ? run(attn_args<bf16_t>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, KLA_ATTN_CAUSAL))
+                          : run(attn_args<float>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, KLA_ATTN_CAUSAL));
+}
+
+int kla_attn_step(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* k_cache, void* v_cache, const int32_t* page_table,
+                  long ld_table, const int32_t* cached, void* o, float scale, int window, int B, int H, int Hk, int D, int n_pages, int page, int max_pages,
+                  int max_len, kla_dtype dt, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    return kla_attn_extend(q, ld_q, k, ld_k, v, ld_v, k_cache, v_cache, page_table, ld_table, cached, o, nullptr, scale, window, nullptr, nullptr, 0, B, 1, H,
+                           Hk, D, n_pages, page, max_pages, max_len, dt, workspace, workspace_bytes, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,426 @@
+// Softmax attention, forward: whole sequences, and new tokens over a paged cache.
+//
+//     s_ij = scale q_i . k_j over the keys j that query i sees,  m_i >= max_j s_ij - 8 / log2(e),  p_ij = exp(s_ij - m_i)
+//     l_i = sum_j p_ij,  o_i = (sum_j p_ij v_j) / l_i,  lse_i = m_i + log l_i
+//
+// One pass over the keys: a wave has 32 query rows, and for every tile of keys forms S^T = K Q^T, p, and O^T += V^T p^T on the matrix pipe, with
+// the running reference m, the sum l and O^T in registers.  O^T is scaled anew only where some row's maximum has grown by more than
+// 2^8 over m (p then stays below 2^8, far from any overflow, and the quotient does not depend on m).  Scores, p, l and O are fp32; p is
+// rounded to the inputs' type where it enters the product with V (bf16: 2^-9 of each weight, as much as the rounding of the output itself).
+#include "kla_attn.hpp"
+
+namespace kla {
+
+namespace {
+
+// a scalar load (the index is the same in all lanes)
+__device__ __forceinline__ int uniform_load(const int* p, long i)
+{
+    return ((const __attribute__((address_space(4))) int*)(uintptr_t)p)[i];
+}
+
+// RW waves of 32 rows each that share tiles of keys (KW = 1), or KW waves that divide the keys of 32 rows (RW = 1).
+template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
+    static_assert(RW == 1 || KW == 1, "one way to share the work");
+    using Tile = RowTile<T, D>;
+    static constexpr int W = RW * KW;
+    static constexpr int BN = sizeof(T) == 4 || KW > 1 ? 32 : 64;         // keys of a tile
+    static constexpr int KT = BN / 32;
+    static constexpr int TILE = BN * Tile::RB;
+    static constexpr int STAGE = 2 * TILE;
+    static constexpr int LDS = KW * 2 * STAGE;
+    static constexpr int NDT = D / 32;
+    static constexpr int NS = 16 / kSlot<T>;             // slots of an accumulator
+    static_assert(KW == 1 || KW * (D + 2) * 32 * 4 <= LDS, "room for the waves' results");
+
+    struct Keys { int n; int cached; int total; long tok0; int hk; };
+
+    // Copies of the K and V rows of keys j0 .. j0 + BN - 1 (those beyond `last` repeat it) by the waves of a team
+    static __device__ __forceinline__ void copy(const AttnArgs<T>& a, const Keys& k, int j0, int last, char* stage, int wave, int lane)
+    {
+        constexpr int RPI = Tile::RPI, ROWS = BN / RW, NI = ROWS / RPI;
+        static_assert(ROWS % RPI == 0 && 16 % RPI == 0, "whole copy instructions");
+        const long ldk = a.ld_k * (long)sizeof(T), ldv = a.ld_v * (long)sizeof(T);
+        const char* kn = reinterpret_cast<const char*>(a.k) + k.tok0 * ldk + (long)k.hk * Tile::RB;
+        const char* vn = reinterpret_cast<const char*>(a.v) + k.tok0 * ldv + (long)k.hk * Tile::RB;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES;
+            const int j = min(j0 + row, last);
+            const int piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16;
+            const char *ks, *vs;
+            if constexpr (PAGED) {
+                ks = kn + (long)max(j - k.cached, 0) * ldk;
+                vs = vn + (long)max(j - k.cached, 0) * ldv;
+                // (the rows of an instruction are of one page: pages begin at multiples of 16 keys)
+                const int jb = min(j0 + first, last);
+                if (jb < k.cached) {
+                    const int id = uniform_load(a.table, k.n * a.ld_table + (jb >> a.page_shift));
+                    const long page = min(max(id, 0), a.n_pages - 1);
+                    const long at = ((((page * a.Hk + k.hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * Tile::RB);
+                    const bool old = j < k.cached;
+                    ks = old ? reinterpret_cast<const char*>(a.k_cache) + at : ks;
+                    vs = old ? reinterpret_cast<const char*>(a.v_cache) + at : vs;
+                }
+            } else {
+                ks = kn + (long)j * ldk;
+                vs = vn + (long)j * ldv;
+            }
+            dma16_from(ks + piece, stage + first * Tile::RB);
+            dma16_from(vs + piece, stage + TILE + first * Tile::RB);
+        }
+    }
+
+    // The new tokens whose first row lies in this tile go into their pages.
+    static __device__ __forceinline__ void store_new(const AttnArgs<T>& a, const Keys& k, int t0, int t1)
+    {
+        constexpr int P = Tile::PIECES;
+        for (int i = threadIdx.x; i < (t1 - t0) * P; i += 64 * W) {
+            const int t = t0 + i / P, pos = k.cached + t;
+            const long page = (long)pos >> a.page_shift;
+            if (page >= a.max_pages) continue;
+            const int id = a.table[k.n * a.ld_table + page];
+            if (id < 0 || id >= a.n_pages) continue;
+            const long at = (((((long)id * a.Hk + k.hk) << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * Tile::RB) + (i % P) * 16;
+            const long from = (long)k.hk * Tile::RB + (i % P) * 16;
+            st16(reinterpret_cast<char*>(a.k_cache) + at, ld16(reinterpret_cast<const char*>(a.k) + (k.tok0 + t) * a.ld_k * (long)sizeof(T) + from));
+            st16(reinterpret_cast<char*>(a.v_cache) + at, ld16(reinterpret_cast<const char*>(a.v) + (k.tok0 + t) * a.ld_v * (long)sizeof(T) + from));
+        }
+    }
+
+    struct Rows {                                        // a wave's 32 query rows, lane = row
+        u32x4 q[Tile::NC];
+        int lo, hi;                                      // first and last key that this lane's row sees
+        int lo_most, hi_least;                           // the largest and smallest of the wave's
+        int lo_least, hi_most;
+        float c;                                         // scores in units of log 2
+    };
+    struct State { floatx16 o[NDT]; float m, mc, l; };
+
+    template <bool CAREFUL>
+    static __device__ __forceinline__ void tile(const Rows& r, State& s, const char* stage, int j0, int last, int row_off, int col_off, int h)
+    {
+        floatx16 st[KT];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) st[kt][e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(st[kt], Tile::row_slot(stage + 32 * kt * Tile::RB, row_off, c), r.q[c]);
+        }
+        const bool masked = j0 + BN - 1 > min(r.hi_least, last) || j0 < r.lo_most;
+        if (masked) {
+            const int hi = min(r.hi, last) - j0 - 4 * h, lo = r.lo - j0 - 4 * h;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int j = 32 * kt + acc_row(e);
+                    st[kt][e] = j <= hi && j >= lo ? st[kt][e] : -__builtin_inff();
+                }
+        }
+        float top = st[0][0];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, st[kt][e]);
+        top = halves_max(top);
+        // (nothing seen so far: m is -inf and any score above it makes a reference)
+        if (__any(top * r.c > s.m * r.c + 8.f)) {
+            const float m = fmaxf(s.m, top), mc = m == -__builtin_inff() ? 0.f : m * r.c;
+            const float f = exp2_hw(s.m * r.c - mc);     // (0 from -inf)
+            s.m = m; s.mc = mc;
+            s.l *= f;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s.o[dt][e] *= f;
+        }
+        float l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                st[kt][e] = exp2_hw(fmaf(st[kt][e], r.c, -s.mc));
+                l[e & 1] += st[kt][e];
+            }
+        s.l += l[0] + l[1];
+        if constexpr (CAREFUL) {
+            if (masked) {
+                const int hi = min(r.hi, last) - j0 - 4 * h, lo = r.lo - j0 - 4 * h;
+                static_for<NDT>([&](auto dt) {
+                    floatx16 signs, count;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) signs[e] = count[e] = 0.f;
+                    static_for<KT>([&](auto kt) {
+                        floatx16 sgn, seen;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int j = 32 * kt + acc_row(e);
+                            seen[e] = j <= hi && j >= lo ? 1.f : 0.f;
+                            sgn[e] = sign_of(st[kt][e]);
+                        }
+                        static_for<NS>([&](auto c) {
+                            const Apart<T> x = apart<T>(Tile::template col_slot<c, dt>(stage + TILE + 32 * kt * Tile::RB, col_off));
+                            mma32x32<T>(s.o[dt], x.fin, slot_of<T, c>(st[kt]));
+                            mma32x32<T>(signs, x.sgn, slot_of<T, c>(sgn));
+                            mma32x32<T>(count, x.bad, slot_of<T, c>(seen));
+                        });
+                    });
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s.o[dt][e] += not_finite(signs[e], count[e]);
+                });
+                return;
+            }
+        }
+        static_for<KT>([&](auto kt) {
+            static_for<NS>([&](auto c) {
+                const u32x4 p = slot_of<T, c>(st[kt]);
+                static_for<NDT>([&](auto dt) { mma32x32<T>(s.o[dt], Tile::template col_slot<c, dt>(stage + TILE + 32 * kt * Tile::RB, col_off), p); });
+            });
+        });
+    }
+
+    // Tiles tb .. te - 1 of keys, from j_first on, for one wave's rows
+    template <bool CAREFUL>
+    static __device__ __forceinline__ void pass(const AttnArgs<T>& a, const Keys& k, const Rows& r, State& s, int j_first, int tb, int te, int last, char* ring,
+                                                int wave, int lane)
+    {
+        const int h = lane >> 5, row_off = Tile::row_offset(lane & 31, h), col_off = Tile::col_offset(lane);
+        s.m = -__builtin_inff();
+        s.mc = s.l = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s.o[dt][e] = 0.f;
+        if (tb < te) copy(a, k, j_first + tb * BN, last, ring, KW > 1 ? 0 : wave, lane);
+        for (int t = tb; t < te; ++t) {
+            // the copies of this tile have landed, and the other stage is no longer read
+            if constexpr (RW > 1) wait_copies_and_barrier();
+            else wait_copies();
+            const int j0 = j_first + t * BN;
+            char* stage = ring + ((t - tb) & 1) * STAGE;
+            if (t + 1 < te) copy(a, k, j0 + BN, last, ring + ((t - tb + 1) & 1) * STAGE, KW > 1 ? 0 : wave, lane);
+            if (j0 > r.hi_most || j0 + BN - 1 < r.lo_least) continue;
+            tile<CAREFUL>(r, s, stage, j0, last, row_off, col_off, h);
+        }
+        s.l = halves_sum(s.l);
+    }
+
+    static __device__ __forceinline__ bool all_finite(const State& s)
+    {
+        bool f = true;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) f = f && finite(s.o[dt]);
+        return f;
+    }
+
+    // 4 consecutive features of one row
+    static __device__ __forceinline__ void store4(const AttnArgs<T>& a, int split, long row, int d, float x0, float x1, float x2, float x3)
+    {
+        const Floats<4> x = {{x0, x1, x2, x3}};
+        if (a.splits > 1) store_vec<float, 4>(a.part_o + ((long)split * a.M * a.H + row) * D + d, x);
+        else store_vec<T, 4>(a.o + row * D + d, x);
+    }
+    // l = 0: no keys here (a split's part), or scores that are all -inf (the quotient is a NaN)
+    static __device__ __forceinline__ float inverse(const AttnArgs<T>& a, float l) { return a.splits > 1 && l == 0.f ? 0.f : 1.f / l; }
+    static __device__ __forceinline__ void store_lse(const AttnArgs<T>& a, int split, long row, float m, float l)
+    {
+        const float lse = m + __log2f(l);                // base 2
+        if (a.splits > 1) a.part_lse[(long)split * a.M * a.H + row] = lse;
+        else if (a.lse) a.lse[row] = lse * kLn2;
+    }
+
+    static __device__ __forceinline__ void run(const AttnArgs<T>& a, char* lds)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int n = lane & 31, h = lane >> 5;
+        // heaviest tiles (the last ones of their sequences) first; the parts of a tile and the key heads beside each other
+        const long unit = a.unit0 + blockIdx.x;
+        const int split = (int)(unit % a.splits);
+        Keys k;
+        k.hk = (int)(unit / a.splits % a.Hk);
+        RowPlace at;
+        if (!find_rows(a.seqs, a.G, 32 * RW, a.per, a.tiles - 1 - unit / a.splits / a.Hk, &at)) return;
+        k.n = at.n; k.tok0 = at.tok0;
+        k.cached = 0;
+        if constexpr (PAGED) k.cached = (int)min((long)max(uniform_load(a.cached, at.n), 0), (long)a.max_pages << a.page_shift);
+        k.total = k.cached + at.len;
+        const int rows = at.len * a.G, row0 = at.tile * 32 * RW;
+        const int t_first = row0 / a.G, t_last = min(row0 + 32 * RW - 1, rows - 1) / a.G;
+        // keys of the tile's rows, and this part of them
+        const int k_first = a.window ? max(0, k.cached + t_first - a.window + 1) : 0, k_last = a.causal ? k.cached + t_last : k.total - 1;
+        const int j_first = k_first / BN * BN, nt = (k_last - j_first) / BN + 1;
+        const int s0 = (int)((long)nt * split / a.splits), s1 = (int)((long)nt * (split + 1) / a.splits);
+        int tb = s0, te = s1;
+        if constexpr (KW > 1) {
+            tb = s0 + (int)((long)(s1 - s0) * wave / KW);
+            te = s0 + (int)((long)(s1 - s0) * (wave + 1) / KW);
+        }
+        // this wave's rows
+        const int w0 = row0 + (KW > 1 ? 0 : 32 * wave), row = min(w0 + n, rows - 1);
+        const int t = row / a.G, head = k.hk * a.G + (row - t * a.G);
+        Rows r;
+        r.c = a.scale * kLog2e;
+        {
+            const char* q = reinterpret_cast<const char*>(a.q + (k.tok0 + t) * a.ld_q + (long)head * D);
+#pragma unroll
+            for (int c = 0; c < Tile::NC; ++c) r.q[c] = ld16(q + (2 * c + h) * 16);
+        }
+        const int tw0 = min(w0, rows - 1) / a.G, tw1 = min(w0 + 31, rows - 1) / a.G;
+        r.lo = a.window ? max(0, k.cached + t - a.window + 1) : 0;
+        r.lo_least = a.window ? max(0, k.cached + tw0 - a.window + 1) : 0;
+        r.lo_most = a.window ? max(0, k.cached + tw1 - a.window + 1) : 0;
+        r.hi = a.causal ? k.cached + t : k.total - 1;
+        r.hi_least = a.causal ? k.cached + tw0 : k.total - 1;
+        r.hi_most = w0 >= rows ? -1 : a.causal ? k.cached + tw1 : k.total - 1;       // (no rows of its own: every tile is passed over)
+        if constexpr (PAGED) {
+            if (split == 0) {                            // tokens whose first row lies in this tile
+                const int u0 = (row0 + a.G - 1) / a.G, u1 = min(at.len, (row0 + 32 * RW + a.G - 1) / a.G);
+                store_new(a, k, u0, u1);
+            }
+        }
+        State s;
+        char* ring = lds + (KW > 1 ? wave * 2 * STAGE : 0);
+        pass<false>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
+        const bool again = !all_finite(s);
+        if constexpr (RW > 1) {
+            if (__syncthreads_or(again)) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
+        } else {
+            if (__any(again)) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
+        }
+        const long out0 = k.tok0 * a.H + (long)k.hk * a.G;
+        auto out_row = [&](int rr) { const int tt = rr / a.G; return out0 + (long)tt * a.H + (rr - tt * a.G); };
+        const float mc = s.m == -__builtin_inff() ? s.m : s.mc;
+        if constexpr (KW == 1) {
+            if (w0 + n < rows) {
+                const long to = out_row(row);
+                const float f = inverse(a, s.l);
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        store4(a, split, to, 32 * dt + 8 * i + 4 * h, s.o[dt][4 * i] * f, s.o[dt][4 * i + 1] * f, s.o[dt][4 * i + 2] * f, s.o[dt][4 * i + 3] * f);
+                if (h == 0) store_lse(a, split, to, mc, s.l);
+            }
+        } else {
+            // the waves' parts, [wave][D + 2][32]: O^T, reference, sum
+            __syncthreads();
+            float* part = reinterpret_cast<float*>(lds);
+            constexpr int PW = (D + 2) * 32;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) part[wave * PW + (32 * dt + acc_row(e) + 4 * h) * 32 + n] = s.o[dt][e];
+            if (h == 0) {
+                part[wave * PW + D * 32 + n] = mc;
+                part[wave * PW + (D + 1) * 32 + n] = s.l;
+            }
+            __syncthreads();
+            const int rr = row0 + n, d0 = (threadIdx.x >> 5) * (D / (2 * KW));
+            if (rr < rows) {
+                float m = -__builtin_inff(), l = 0.f, w[KW];
+#pragma unroll
+                for (int i = 0; i < KW; ++i) m = fmaxf(m, part[i * PW + D * 32 + n]);
+#pragma unroll
+                for (int i = 0; i < KW; ++i) {
+                    w[i] = m == -__builtin_inff() ? 0.f : exp2_hw(part[i * PW + D * 32 + n] - m);
+                    l = fmaf(w[i], part[i * PW + (D + 1) * 32 + n], l);
+                }
+                const long to = out_row(rr);
+                const float f = inverse(a, l);
+#pragma unroll
+                for (int d = 0; d < D / (2 * KW); d += 4) {
+                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < KW; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = fmaf(w[i], part[i * PW + (d0 + d + e) * 32 + n], x[e]);
+                    store4(a, split, to, d0 + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+                }
+                if (threadIdx.x < 32) store_lse(a, split, to, m, l);
+            }
+        }
+    }
+};
+
+template <typename T, int D, int RW, int KW, bool PAGED>
+__global__ __launch_bounds__(64 * RW * KW, KW > 1 ? 1 : 2) void attn_fwd_kernel(const AttnArgs<T> a)
+{
+    extern __shared__ char lds[];
+    Fwd<T, D, RW, KW, PAGED>::run(a, lds);
+}
+
+template <typename T, int D, int RW, int KW, bool PAGED> hipError_t launch(AttnArgs<T> a, hipStream_t st)
+{
+    using F = Fwd<T, D, RW, KW, PAGED>;
+    const auto kernel = attn_fwd_kernel<T, D, RW, KW, PAGED>;
+    if (F::LDS > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, F::LDS);
+        if (e != hipSuccess) return e;
+    }
+    const long units = a.tiles * a.Hk * a.splits, most = most_blocks(64 * F::W);
+    for (a.unit0 = 0; a.unit0 < units; a.unit0 += most) {
+        kernel<<<dim3((unsigned)(units - a.unit0 < most ? units - a.unit0 : most)), dim3(64 * F::W), F::LDS, st>>>(a);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+
+// The parts of a row joined: sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A workgroup has 256 / (D / 4) rows, a thread four features.
+template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs<T> a, long row0)
+{
+    constexpr int TPR = D / 4;
+    const long rows = a.M * a.H, row = row0 + (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    if (row >= rows) return;
+    const int d = (threadIdx.x % TPR) * 4;
+    float m = -__builtin_inff();
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * rows + row]);
+    float l = 0.f;
+    Floats<4> x = {{0.f, 0.f, 0.f, 0.f}};
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = m == -__builtin_inff() ? 0.f : exp2_hw(a.part_lse[s * rows + row] - m);
+        const Floats<4> o = load_vec<float, 4>(a.part_o + (s * rows + row) * D + d);
+        l += w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.v[i] = fmaf(w, o.v[i], x.v[i]);
+    }
+    const float f = 1.f / l;                             // (no key in any part: a NaN, as scores that are all -inf)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[i] *= f;
+    store_vec<T, 4>(a.o + row * D + d, x);
+    if (a.lse && d == 0) a.lse[row] = (m + __log2f(l)) * kLn2;
+}
+
+template <typename T, int D> hipError_t join(const AttnArgs<T>& a, hipStream_t st)
+{
+    const long per = 256 / (D / 4), blocks = (a.M * a.H + per - 1) / per, most = most_blocks(256);
+    for (long b = 0; b < blocks; b += most) {
+        attn_join_kernel<T, D><<<dim3((unsigned)(blocks - b < most ? blocks - b : most)), dim3(256), 0, st>>>(a, b * per);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T, int D> hipError_t pick(const AttnArgs<T>& a, const AttnPlan& p, bool paged, hipStream_t st)
+{
+    constexpr int KW = sizeof(T) == 4 && D == 128 ? 2 : 4;
+    if (p.rows == 32) return paged ? launch<T, D, 1, KW, true>(a, st) : launch<T, D, 1, KW, false>(a, st);
+    return paged ? launch<T, D, 4, 1, true>(a, st) : launch<T, D, 4, 1, false>(a, st);
+}
+
+}  // namespace
+
+template <typename T> hipError_t launch_attn_fwd(const AttnArgs<T>& a, int D, const AttnPlan& p, bool paged, hipStream_t st)
+{
+    if (a.tiles == 0) return hipSuccess;
+    return D == 64 ? pick<T, 64>(a, p, paged, st) : pick<T, 128>(a, p, paged, st);
+}
+template <typename T> hipError_t launch_attn_join(const AttnArgs<T>& a, int D, hipStream_t st) { return D == 64 ? join<T, 64>(a, st) : join<T, 128>(a, st); }
+
+template hipError_t launch_attn_fwd<float>(const AttnArgs<float>&, int, const AttnPlan&, bool, hipStream_t);
+template hipError_t launch_attn_fwd<bf16_t>(const AttnArgs<bf16_t>&, int, const AttnPlan&, bool, hipStream_t);
+template hipError_t launch_attn_join<float>(const AttnArgs<float>&, int, hipStream_t);
+template hipError_t launch_attn_join<bf16_t>(const AttnArgs<bf16_t>&, int, hipStream_t);
+
+}  // namespace kla
