@@ -483,6 +483,17 @@ int kla_attn_fwd(const void *q, long ld_q, const void *k, long ld_k, const void 
                  const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
                  int N, int T, int H, int Hk, int D, kla_dtype dt, void *hip_stream, unsigned opts);
 
+/* Gradients of sum <d_o, o> from the inputs and outputs of the forward (o, lse).
+ *   o, d_o [N, T, H, D] dt, lse [N, T, H] fp32      in   contiguous
+ *   dq [N, T, H, D], dk, dv [N, T, Hk, D] dt        out  contiguous
+ * workspace 256-byte aligned. */
+size_t kla_attn_bwd_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t *cu_seqlens_host, int n_seq, kla_dtype dt);
+int kla_attn_bwd(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
+                 const void *o, const float *lse, const void *d_o, void *dq, void *dk, void *dv, float scale, int window,
+                 const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
+                 int N, int T, int H, int Hk, int D, kla_dtype dt,
+                 void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);
+
 /* New tokens of n_seq (packed) or N sequences behind `cached` earlier ones each: token t of sequence s stands at position cached[s] + t
  * and sees the sequence's cached tokens and the new ones up to itself (and in its window).  The keys and values of the new tokens are
  * stored in the cache too; `cached` stays as it is, for the other layers of a step.

@@ -671,4 +671,4 @@ from .layer import (KLA_LAYER_GATE_FIRST, KLA_LAYER_SIGMOID, KLA_LAYER_SILU, KLA
                     kla_add_norm, kla_add_norm_bwd, kla_add_norm_fwd, kla_conv, kla_conv_bwd, kla_conv_fwd, kla_conv_step, kla_gated_norm,
                     kla_gated_norm_bwd, kla_gated_norm_fwd, kla_ssm, kla_ssm_bwd, kla_ssm_fwd, kla_ssm_step)
 from . import attention  # noqa: E402
-from .attention import KLA_ATTN_CAUSAL, kla_attn_extend, kla_attn_fwd, kla_attn_step  # noqa: E402, F401
+from .attention import KLA_ATTN_CAUSAL, kla_attn, kla_attn_bwd, kla_attn_extend, kla_attn_fwd, kla_attn_step  # noqa: E402, F401

@@ -11,8 +11,8 @@ import ctypes
 
 import torch
 
-from . import _binding, _check, _dev, _dt, _ptr, _stream, _written, _ws_bytes, lib
-from .layer import _batch, _call, _host, _native, _on_gpu, _rows, _sizes, _workspace
+from . import _check, _dev, _dt, _ptr, _stream, _written, _ws_bytes, lib
+from .layer import _Offsets, _batch, _call, _host, _no_second, _on_gpu, _rows, _sizes, _workspace
 
 KLA_ATTN_CAUSAL = 1
 
@@ -22,6 +22,8 @@ _IN = [_vp, _l] * 3
 _CACHE = [_vp, _vp, _vp, _l, _vp]
 SIGNATURES = {
     "kla_attn_fwd": (_i, [*_IN, _vp, _vp, _f, _i, *_SEQS, *[_i] * 6, _vp, _u]),
+    "kla_attn_bwd_workspace_bytes": (_z, [*[_i] * 5, _vp, _i, _i]),
+    "kla_attn_bwd": (_i, [*_IN, *[_vp] * 6, _f, _i, *_SEQS, *[_i] * 6, _vp, _z, _vp, _u]),
     "kla_attn_extend_workspace_bytes": (_z, [*[_i] * 5, _vp, *[_i] * 3]),
     "kla_attn_extend": (_i, [*_IN, *_CACHE, _vp, _vp, _f, _i, *_SEQS, *[_i] * 10, _vp, _z, _vp]),
     "kla_attn_step": (_i, [*_IN, *_CACHE, _vp, _f, _i, *[_i] * 9, _vp, _z, _vp]),
@@ -69,6 +71,51 @@ def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu
           n_seq, N, T, H, Hk, D, dt, _stream(), KLA_ATTN_CAUSAL if causal else 0)
     _written(*given)
     return out, lse
+
+
+def kla_attn_bwd(q, k, v, o, lse, d_o, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, workspace=None):
+    """Backward of kla_attn_fwd, from what it returned: a dict of dq, dk, dv."""
+    for name, t in (("o", o), ("lse", lse), ("d_o", d_o)):
+        if t is None:
+            raise ValueError("%s is required" % name)
+    H, Hk, D, dt, ld = _heads(q, k, v, 2)
+    N, T = q.shape[:2]
+    _, cu_hp, n_seq, _n = _batch(q, cu_seqlens, cu_seqlens_host)
+    _sizes(window)
+    _check("o", o, (N, T, H, D), q.dtype)
+    _check("d_o", d_o, (N, T, H, D), q.dtype)
+    _check("lse", lse, (N, T, H), torch.float32)
+    _on_gpu(o, lse, d_o, cu_seqlens, workspace)
+    _dev(o, lse, d_o, cu_seqlens, workspace)
+    if workspace is None:
+        workspace = _workspace(int(lib().kla_attn_bwd_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, dt)), q)
+    g = {name: torch.empty(t.shape, dtype=t.dtype, device=t.device) for name, t in (("dq", q), ("dk", k), ("dv", v))}
+    _call("kla_attn_bwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(o), _ptr(lse), _ptr(d_o), *(_ptr(t) for t in g.values()),
+          _scale(scale, D), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, dt, _ptr(workspace), _ws_bytes(workspace), _stream(),
+          KLA_ATTN_CAUSAL if causal else 0)
+    return g
+
+
+class _Attn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, scale, causal, window, cu_seqlens, cu_seqlens_host):
+        ctx.offsets = _Offsets(cu_seqlens, cu_seqlens_host)
+        wanted = any(ctx.needs_input_grad)
+        o, lse = kla_attn_fwd(q, k, v, scale, causal, window, cu_seqlens, cu_seqlens_host, want_lse=wanted)
+        ctx.save_for_backward(q, k, v, o, lse)
+        ctx.misc = (scale, causal, window)
+        return o
+
+    @staticmethod
+    def backward(ctx, d_o):
+        _no_second("kla_attn")
+        g = kla_attn_bwd(*ctx.saved_tensors, d_o.contiguous(), *ctx.misc, **ctx.offsets.check())
+        return (*g.values(), None, None, None, None, None)
+
+
+def kla_attn(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None):
+    """Differentiable kla_attn_fwd: o, gradients with respect to q, k and v.  The graph holds q, k, v, o and the rows' lse."""
+    return _Attn.apply(q, k, v, scale, bool(causal), int(window), cu_seqlens, _host(cu_seqlens, cu_seqlens_host))
 
 
 def _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, n):

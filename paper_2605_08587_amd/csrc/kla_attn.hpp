@@ -49,9 +49,9 @@ template <typename T, int C> __device__ __forceinline__ u32x4 slot_of(const floa
 // the accumulator row of register e is acc_row(e) + 4 h
 __host__ __device__ constexpr int acc_row(int e) { return 8 * (e >> 2) + (e & 3); }
 
-// Where an operand's row that a mask hides holds an infinity or a NaN, its zero weight does not: 0 x inf.  Kernels that find their result not finite
-// compute it again with products that keep such rows apart: a_fin has zeros for the elements of a that are not finite, a_sgn has +-1 for infinities
-// and 0 elsewhere, a_bad 1 for whatever is not finite.  With b's signs and the mask's ones, two more products count what a column takes in.
+// Where an operand's row that a mask hides holds an infinity or a NaN, its zero weight does not hide it: 0 x inf.  Kernels that find their result not
+// finite compute it again with products that keep such rows apart: the elements of a that are not finite are zeros in `fin`, and two more products count
+// what a column takes in, into one accumulator: `sgn` (4096 times the sign of an infinity) times the signs of b plus `bad` (1) times the mask's ones.
 template <typename T> struct Apart { u32x4 fin, sgn, bad; };
 template <typename T> __device__ __forceinline__ Apart<T> apart(u32x4 a)
 {
@@ -65,7 +65,7 @@ template <typename T> __device__ __forceinline__ Apart<T> apart(u32x4 a)
                 const uint32_t x = (a[i] >> (16 * j)) & 0xffffu;
                 const bool b = (x & 0x7f80u) == 0x7f80u, inf = (x & 0x7fffu) == 0x7f80u;
                 fin |= (b ? 0u : x) << (16 * j);
-                sgn |= (inf ? 0x3f80u | (x & 0x8000u) : 0u) << (16 * j);
+                sgn |= (inf ? 0x4580u | (x & 0x8000u) : 0u) << (16 * j);
                 bad |= (b ? 0x3f80u : 0u) << (16 * j);
             }
             r.fin[i] = fin; r.sgn[i] = sgn; r.bad[i] = bad;
@@ -73,7 +73,7 @@ template <typename T> __device__ __forceinline__ Apart<T> apart(u32x4 a)
             const uint32_t x = a[i];
             const bool b = (x & 0x7f800000u) == 0x7f800000u, inf = (x & 0x7fffffffu) == 0x7f800000u;
             r.fin[i] = b ? 0u : x;
-            r.sgn[i] = inf ? 0x3f800000u | (x & 0x80000000u) : 0u;
+            r.sgn[i] = inf ? 0x45800000u | (x & 0x80000000u) : 0u;
             r.bad[i] = b ? 0x3f800000u : 0u;
         }
     }
@@ -81,9 +81,10 @@ template <typename T> __device__ __forceinline__ Apart<T> apart(u32x4 a)
 }
 // +-1 for values that are not zero (0 for NaN: what they meet becomes one)
 __device__ __forceinline__ float sign_of(float x) { return x > 0.f ? 1.f : x < 0.f ? -1.f : 0.f; }
-// what a column takes in: `signs` the sum of the signs of its infinite terms, `count` how many terms are not finite
-__device__ __forceinline__ float not_finite(float signs, float count)
+// what a column takes in, of an accumulator of the two products: all of its infinities of one sign and no NaN, or a NaN
+__device__ __forceinline__ float not_finite(float x)
 {
+    const float signs = rintf(x * (1.f / 4096.f)), count = fmaf(signs, -4096.f, x);      // (at most 64 terms)
     return count == 0.f ? 0.f : signs == count ? __builtin_inff() : signs == -count ? -__builtin_inff() : __builtin_nanf("");
 }
 __device__ __forceinline__ bool finite(const floatx16& x)
@@ -107,6 +108,12 @@ __device__ __forceinline__ void dma16_from(const char* lane_address, char* lds_w
 {
     const uint32_t m = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) char*)lds_wave_base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(lane_address), "s"(m) : "memory");
+}
+// 4 bytes per lane, to lds_wave_base + 4 lane
+__device__ __forceinline__ void dma4_from(const void* lane_address, char* lds_wave_base)
+{
+    const uint32_t m = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) char*)lds_wave_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(lane_address), "s"(m) : "memory");
 }
 // A tile of rows of D elements of T
 template <typename T, int D> struct RowTile {
@@ -145,6 +152,40 @@ template <typename T, int D> struct RowTile {
     }
 };
 static_assert(row_swz<16>(8) == 2 && row_swz<8>(8) == 2 && row_swz<16>(16) == 0 && row_swz<8>(16) == 0, "col_slot's constants");
+
+// acc += (32 rows of a tile)^T b, b an accumulator of weights.  Where the block is masked, rows that are not finite count for what `seen(e)` (e: of b)
+// says sees them.
+template <bool CAREFUL, typename T, int D, int NDT, typename Seen>
+__device__ __forceinline__ void add_product(floatx16 (&acc)[NDT], const char* tile, int col_off, const floatx16& b, bool masked, Seen&& seen)
+{
+    using Tile = RowTile<T, D>;
+    constexpr int NS = 16 / kSlot<T>;
+    if constexpr (CAREFUL) {
+        if (masked) {
+            floatx16 sgn, ones;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) { sgn[e] = sign_of(b[e]); ones[e] = seen(e) ? 1.f : 0.f; }
+            static_for<NDT>([&](auto dt) {
+                floatx16 x;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = 0.f;
+                static_for<NS>([&](auto c) {
+                    const Apart<T> a = apart<T>(Tile::template col_slot<c, dt>(tile, col_off));
+                    mma32x32<T>(acc[dt], a.fin, slot_of<T, c>(b));
+                    mma32x32<T>(x, a.sgn, slot_of<T, c>(sgn));
+                    mma32x32<T>(x, a.bad, slot_of<T, c>(ones));
+                });
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[dt][e] += not_finite(x[e]);
+            });
+            return;
+        }
+    }
+    static_for<NS>([&](auto c) {
+        const u32x4 s = slot_of<T, c>(b);
+        static_for<NDT>([&](auto dt) { mma32x32<T>(acc[dt], Tile::template col_slot<c, dt>(tile, col_off), s); });
+    });
+}
 
 // All of this wave's copies have landed, and its LDS reads are done; then every wave's.
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
@@ -213,6 +254,17 @@ template <typename T> struct AttnArgs {
     long tiles, per;                                     // tiles of query rows of a key head: in all; of one sequence (fixed lengths)
     long unit0;                                          // first workgroup of this launch
 };
+// Backward: d_o, dq like o, dk, dv [tokens][Hk][D]; row_lse, row_delta [tokens][H]: the rows' lse (base 2) and <d_o, o>; part_dk, part_dv
+// [parts][tokens][Hk][D] where the query rows of a tile of keys are taken in `parts` parts.
+template <typename T> struct AttnBwdArgs {
+    AttnArgs<T> f;                                       // (o, lse: the forward's; tiles, per, unit0: of a launch)
+    const T* d_o; T* dq; T* dk; T* dv;
+    float* row_lse; float* row_delta;
+    int parts; float* part_dk; float* part_dv;
+    long key_tiles, key_per;                             // tiles of 128 keys: in all; of one sequence (fixed lengths)
+};
+template <typename T> hipError_t launch_attn_bwd(const AttnBwdArgs<T>& a, int D, hipStream_t st);
+
 // How the forward's work is cut: rows of a tile (128: four waves of 32 rows that share tiles of keys; 32: four waves that share the rows and divide the
 // keys) and parts of the keys.
 struct AttnPlan { int rows; int splits; };

@@ -2,6 +2,7 @@
 // allocation, no state, nothing read from the environment; everything is enqueued on the caller's stream.
 #include <limits.h>
 #include <math.h>
+#include <type_traits>
 
 #include "kla_args.hpp"
 #include "kla_attn.hpp"
@@ -81,6 +82,30 @@ kla::AttnArgs<T> attn_args(const void* q, long ld_q, const void* k, long ld_k, c
     a.scale = scale; a.window = window; a.causal = opts & KLA_ATTN_CAUSAL; a.splits = 1; a.M = M;
     return a;
 }
+// Backward: the query rows that see a tile of 128 keys are taken in parts where there are fewer than two such tiles for each CU.
+int attn_bwd_parts(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
+{
+    long per;
+    const long units = attn_tiles(s, cu_host, 1, 128, &per) * Hk;
+    if (units == 0 || units >= 512) return 1;
+    const long want = (512 + units - 1) / units, most = ((long)longest(s, cu_host) * G + 255) / 256;
+    const long parts = want < most ? want : most;
+    return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+}
+struct BwdWork { float *row_lse, *row_delta, *part_dk, *part_dv; size_t bytes; };
+BwdWork bwd_work(char* base, int parts, long M, const AttnSizes& z)
+{
+    Carve c{base};
+    BwdWork w = {};
+    w.row_lse = c.take<float>((size_t)M * z.H);
+    w.row_delta = c.take<float>((size_t)M * z.H);
+    if (parts > 1) {
+        w.part_dk = c.take<float>((size_t)parts * M * z.Hk * z.D);
+        w.part_dv = c.take<float>((size_t)parts * M * z.Hk * z.D);
+    }
+    w.bytes = c.used;
+    return w;
+}
 struct ExtendWork { float *part_o, *part_lse; size_t bytes; };
 ExtendWork extend_work(char* base, const kla::AttnPlan& p, long M, int H, int D)
 {
@@ -119,6 +144,52 @@ int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void*
     };
     return dt == KLA_BF16 ? run(attn_args<bf16_t>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, opts))
                           : run(attn_args<float>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, opts));
+}
+
+size_t kla_attn_bwd_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t* cu_seqlens_host, int n_seq, kla_dtype dt)
+{
+    kla::Seqs s;
+    long M;
+    const AttnSizes z = {N, T, H, Hk, D};
+    if (attn_sizes(z, dt) || take_seqs(n_seq > 0 ? cu_seqlens_host : nullptr, cu_seqlens_host, n_seq, N, T, &s, &M)) return 0;
+    return bwd_work(nullptr, attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk), M, z).bytes;
+}
+
+int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, const void* o, const float* lse, const void* d_o, void* dq,
+                 void* dk, void* dv, float scale, int window, const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int n_seq, int N, int T, int H,
+                 int Hk, int D, kla_dtype dt, void* workspace, size_t workspace_bytes, void* hip_stream, unsigned opts)
+{
+    kla::Seqs s;
+    long M;
+    const AttnSizes z = {N, T, H, Hk, D};
+    if (const int e = attn_check(z, ld_q, ld_k, ld_v, scale, window, dt)) return e;
+    if ((opts & ~(unsigned)KLA_ATTN_CAUSAL) || (window && !(opts & KLA_ATTN_CAUSAL))) return KLA_ERR_SHAPE;
+    if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
+    if (M > 0 && (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv)) return KLA_ERR_NULL;
+    if (M > 0)
+        for (const void* out : {dq, dk, dv})
+            for (const void* in : {q, k, v, o, d_o}) if (out == in) return KLA_ERR_SHAPE;
+    if (M > 0 && (dq == dk || dq == dv || dk == dv)) return KLA_ERR_SHAPE;
+    if (!aligned(16, {q, k, v, o, d_o, dq, dk, dv}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
+    const int parts = attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk);
+    const BwdWork w = bwd_work(static_cast<char*>(workspace), parts, M, z);
+    if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    auto run = [&](auto a) {
+        using Q = decltype(a.o);
+        using E = std::remove_pointer_t<Q>;
+        kla::AttnBwdArgs<E> b = {};
+        b.f = a;
+        b.d_o = static_cast<const E*>(d_o); b.dq = static_cast<Q>(dq); b.dk = static_cast<Q>(dk); b.dv = static_cast<Q>(dv);
+        b.row_lse = w.row_lse; b.row_delta = w.row_delta; b.parts = parts; b.part_dk = w.part_dk; b.part_dv = w.part_dv;
+        b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 128, &b.f.per);
+        b.key_tiles = attn_tiles(s, cu_seqlens_host, 1, 128, &b.key_per);
+        return status(kla::launch_attn_bwd(b, D, st));
+    };
+    void* out = const_cast<void*>(o);
+    float* l = const_cast<float*>(lse);
+    return dt == KLA_BF16 ? run(attn_args<bf16_t>(q, ld_q, k, ld_k, v, ld_v, out, l, s, M, z, scale, window, opts))
+                          : run(attn_args<float>(q, ld_q, k, ld_k, v, ld_v, out, l, s, M, z, scale, window, opts));
 }
 
 size_t kla_attn_extend_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t* cu_seqlens_host, int n_seq, int max_len, kla_dtype dt)

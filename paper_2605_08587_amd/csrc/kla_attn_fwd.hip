@@ -30,7 +30,6 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     static constexpr int STAGE = 2 * TILE;
     static constexpr int LDS = KW * 2 * STAGE;
     static constexpr int NDT = D / 32;
-    static constexpr int NS = 16 / kSlot<T>;             // slots of an accumulator
     static_assert(KW == 1 || KW * (D + 2) * 32 * 4 <= LDS, "room for the waves' results");
 
     struct Keys { int n; int cached; int total; long tok0; int hk; };
@@ -109,8 +108,8 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
             for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(st[kt], Tile::row_slot(stage + 32 * kt * Tile::RB, row_off, c), r.q[c]);
         }
         const bool masked = j0 + BN - 1 > min(r.hi_least, last) || j0 < r.lo_most;
+        const int hi = min(r.hi, last) - j0 - 4 * h, lo = r.lo - j0 - 4 * h;
         if (masked) {
-            const int hi = min(r.hi, last) - j0 - 4 * h, lo = r.lo - j0 - 4 * h;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -145,39 +144,9 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                 l[e & 1] += st[kt][e];
             }
         s.l += l[0] + l[1];
-        if constexpr (CAREFUL) {
-            if (masked) {
-                const int hi = min(r.hi, last) - j0 - 4 * h, lo = r.lo - j0 - 4 * h;
-                static_for<NDT>([&](auto dt) {
-                    floatx16 signs, count;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) signs[e] = count[e] = 0.f;
-                    static_for<KT>([&](auto kt) {
-                        floatx16 sgn, seen;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int j = 32 * kt + acc_row(e);
-                            seen[e] = j <= hi && j >= lo ? 1.f : 0.f;
-                            sgn[e] = sign_of(st[kt][e]);
-                        }
-                        static_for<NS>([&](auto c) {
-                            const Apart<T> x = apart<T>(Tile::template col_slot<c, dt>(stage + TILE + 32 * kt * Tile::RB, col_off));
-                            mma32x32<T>(s.o[dt], x.fin, slot_of<T, c>(st[kt]));
-                            mma32x32<T>(signs, x.sgn, slot_of<T, c>(sgn));
-                            mma32x32<T>(count, x.bad, slot_of<T, c>(seen));
-                        });
-                    });
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s.o[dt][e] += not_finite(signs[e], count[e]);
-                });
-                return;
-            }
-        }
         static_for<KT>([&](auto kt) {
-            static_for<NS>([&](auto c) {
-                const u32x4 p = slot_of<T, c>(st[kt]);
-                static_for<NDT>([&](auto dt) { mma32x32<T>(s.o[dt], Tile::template col_slot<c, dt>(stage + TILE + 32 * kt * Tile::RB, col_off), p); });
-            });
+            add_product<CAREFUL, T, D>(s.o, stage + TILE + 32 * kt * Tile::RB, col_off, st[kt], masked,
+                                       [&](int e) { return 32 * kt + acc_row(e) <= hi && 32 * kt + acc_row(e) >= lo; });
         });
     }
 
