@@ -12,7 +12,7 @@ import ctypes
 import torch
 
 from . import _check, _dev, _dt, _ptr, _stream, _written, _ws_bytes, lib
-from .layer import _Offsets, _batch, _call, _host, _no_second, _on_gpu, _rows, _sizes, _workspace
+from .layer import _Offsets, _batch, _call, _eager, _host, _native, _no_second, _on_gpu, _rows, _sizes, _workspace
 
 KLA_ATTN_CAUSAL = 1
 
@@ -28,10 +28,12 @@ SIGNATURES = {
     "kla_attn_extend": (_i, [*_IN, *_CACHE, _vp, _vp, _f, _i, *_SEQS, *[_i] * 10, _vp, _z, _vp]),
     "kla_attn_step": (_i, [*_IN, *_CACHE, _vp, _f, _i, *[_i] * 9, _vp, _z, _vp]),
 }
+# what kla_binding.so calls, in the order of its bind_attn
+NATIVE = ("kla_attn_fwd", "kla_attn_bwd_workspace_bytes", "kla_attn_bwd", "kla_attn_extend_workspace_bytes", "kla_attn_extend", "kla_attn_step")
 
 
-def _scale(scale, D):
-    return D ** -0.5 if scale is None else float(scale)
+def _scale(scale, q):
+    return q.shape[-1] ** -0.5 if scale is None and q.dim() and q.shape[-1] else float(scale or 0.0)
 
 
 def _heads(q, k, v, lead):
@@ -45,7 +47,6 @@ def _heads(q, k, v, lead):
     _check("v", v, (*at, Hk, D), q.dtype)
     if Hk == 0 or H % Hk:
         raise ValueError("%d query heads cannot share %d key heads evenly" % (H, Hk))
-    _on_gpu(q, k, v)
     return H, Hk, D, dt, (_rows("q", q, 2), _rows("k", k, 2), _rows("v", v, 2))
 
 
@@ -54,20 +55,23 @@ def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu
     fp32 the logarithms of the rows' sums (None unless want_lse).  causal: a token sees those up to itself, and with window > 0 only the last
     `window` of them; scale: of the scores, D ** -0.5 by default.  Packed batches by cu_seqlens as in kla_chunk_fwd."""
     host = _host(cu_seqlens, cu_seqlens_host)
+    r = _native("attn_fwd", "kla_attn_fwd", q, k, v, _scale(scale, q), bool(causal), window, cu_seqlens, host, bool(want_lse), out, lse)
+    if r is not None:
+        return r
     H, Hk, D, dt, ld = _heads(q, k, v, 2)
     N, T = q.shape[:2]
     _, cu_hp, n_seq, _n = _batch(q, cu_seqlens, host)
     _sizes(window)
     _check("out", out, (N, T, H, D), q.dtype)
     _check("lse", lse, (N, T, H), torch.float32)
-    _on_gpu(cu_seqlens, out, lse)
+    _on_gpu(q, k, v, cu_seqlens, out, lse)
     _dev(cu_seqlens, out, lse)
     given = out, lse
     if out is None:
         out = torch.empty((N, T, H, D), dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
         lse = torch.empty((N, T, H), dtype=torch.float32, device=q.device)
-    _call("kla_attn_fwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(out), _ptr(lse), _scale(scale, D), int(window), _ptr(cu_seqlens), cu_hp,
+    _call("kla_attn_fwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(out), _ptr(lse), _scale(scale, q), int(window), _ptr(cu_seqlens), cu_hp,
           n_seq, N, T, H, Hk, D, dt, _stream(), KLA_ATTN_CAUSAL if causal else 0)
     _written(*given)
     return out, lse
@@ -85,13 +89,13 @@ def kla_attn_bwd(q, k, v, o, lse, d_o, scale=None, causal=True, window=0, cu_seq
     _check("o", o, (N, T, H, D), q.dtype)
     _check("d_o", d_o, (N, T, H, D), q.dtype)
     _check("lse", lse, (N, T, H), torch.float32)
-    _on_gpu(o, lse, d_o, cu_seqlens, workspace)
+    _on_gpu(q, k, v, o, lse, d_o, cu_seqlens, workspace)
     _dev(o, lse, d_o, cu_seqlens, workspace)
     if workspace is None:
         workspace = _workspace(int(lib().kla_attn_bwd_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, dt)), q)
     g = {name: torch.empty(t.shape, dtype=t.dtype, device=t.device) for name, t in (("dq", q), ("dk", k), ("dv", v))}
     _call("kla_attn_bwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(o), _ptr(lse), _ptr(d_o), *(_ptr(t) for t in g.values()),
-          _scale(scale, D), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, dt, _ptr(workspace), _ws_bytes(workspace), _stream(),
+          _scale(scale, q), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, dt, _ptr(workspace), _ws_bytes(workspace), _stream(),
           KLA_ATTN_CAUSAL if causal else 0)
     return g
 
@@ -115,7 +119,12 @@ class _Attn(torch.autograd.Function):
 
 def kla_attn(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None):
     """Differentiable kla_attn_fwd: o, gradients with respect to q, k and v.  The graph holds q, k, v, o and the rows' lse."""
-    return _Attn.apply(q, k, v, scale, bool(causal), int(window), cu_seqlens, _host(cu_seqlens, cu_seqlens_host))
+    host = _host(cu_seqlens, cu_seqlens_host)
+    if _eager():
+        r = _native("attn_train", "kla_attn_fwd", q, k, v, _scale(scale, q), bool(causal), window, cu_seqlens, host)
+        if r is not None:
+            return r
+    return _Attn.apply(q, k, v, scale, bool(causal), int(window), cu_seqlens, host)
 
 
 def _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, n):
@@ -127,8 +136,6 @@ def _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, n):
     _check("page_table", page_table, (n, max_pages), torch.int32)
     _check("cached", cached, (n,), torch.int32)
     _sizes(n_pages, page, max_pages, max_pages * page)
-    _on_gpu(k_cache, v_cache, page_table, cached)
-    _dev(k_cache, v_cache, cached)
     return n_pages, page, max_pages, _rows("page_table", page_table)
 
 
@@ -141,17 +148,22 @@ def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, w
     (o, lse).  max_len: a bound of cached + new tokens, if the caller knows a closer one than the table's width (only how the work
     is cut depends on it)."""
     host = _host(cu_seqlens, cu_seqlens_host)
+    if workspace is None:
+        r = _native("attn_extend", "kla_attn_extend", q, k, v, k_cache, v_cache, page_table, cached, _scale(scale, q), window, cu_seqlens, host, max_len,
+                    bool(want_lse), out, lse)
+        if r is not None:
+            return r if r[1] is not None else r[0]
     H, Hk, D, dt, ld = _heads(q, k, v, 2)
     N, T = q.shape[:2]
     _, cu_hp, n_seq, n = _batch(q, cu_seqlens, host)
     _sizes(window)
     n_pages, page, max_pages, ld_table = _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, n)
-    _check("out", out, (N, T, H, D), q.dtype)
-    _check("lse", lse, (N, T, H), torch.float32)
-    _on_gpu(cu_seqlens, out, lse, workspace)
-    _dev(cu_seqlens, out, lse, workspace)
     max_len = max_pages * page if max_len is None else int(max_len)
     _sizes(max_len)
+    _check("out", out, (N, T, H, D), q.dtype)
+    _check("lse", lse, (N, T, H), torch.float32)
+    _on_gpu(q, k, v, k_cache, v_cache, page_table, cached, cu_seqlens, out, lse, workspace)
+    _dev(k_cache, v_cache, cached, cu_seqlens, out, lse, workspace)
     if workspace is None:
         workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, max_len, dt)), q)
     given = out, lse
@@ -160,7 +172,7 @@ def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, w
     if lse is None and want_lse:
         lse = torch.empty((N, T, H), dtype=torch.float32, device=q.device)
     _call("kla_attn_extend", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(k_cache), _ptr(v_cache), _ptr(page_table), ld_table, _ptr(cached),
-          _ptr(out), _ptr(lse), _scale(scale, D), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, n_pages, page, max_pages, max_len, dt,
+          _ptr(out), _ptr(lse), _scale(scale, q), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, n_pages, page, max_pages, max_len, dt,
           _ptr(workspace), _ws_bytes(workspace), _stream())
     _written(k_cache, v_cache, *given)
     return (out, lse) if lse is not None else out
@@ -168,21 +180,25 @@ def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, w
 
 def kla_attn_step(q, k, v, k_cache, v_cache, page_table, cached, scale=None, window=0, max_len=None, out=None, workspace=None):
     """One new token of B sequences: q [B,H,D], k, v [B,Hk,D]; otherwise as kla_attn_extend.  Returns o [B,H,D]."""
+    if workspace is None:
+        r = _native("attn_step", "kla_attn_step", q, k, v, k_cache, v_cache, page_table, cached, _scale(scale, q), window, max_len, out)
+        if r is not None:
+            return r
     H, Hk, D, dt, ld = _heads(q, k, v, 1)
     B = q.shape[0]
     _sizes(window)
     n_pages, page, max_pages, ld_table = _cache_check(q, k_cache, v_cache, page_table, cached, Hk, D, B)
-    _check("out", out, (B, H, D), q.dtype)
-    _on_gpu(out, workspace)
-    _dev(out, workspace)
     max_len = max_pages * page if max_len is None else int(max_len)
     _sizes(max_len)
+    _check("out", out, (B, H, D), q.dtype)
+    _on_gpu(q, k, v, k_cache, v_cache, page_table, cached, out, workspace)
+    _dev(k_cache, v_cache, cached, out, workspace)
     if workspace is None:
         workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(B, 1, H, Hk, D, None, 0, max_len, dt)), q)
     given = out
     if out is None:
         out = torch.empty((B, H, D), dtype=q.dtype, device=q.device)
     _call("kla_attn_step", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(k_cache), _ptr(v_cache), _ptr(page_table), ld_table, _ptr(cached),
-          _ptr(out), _scale(scale, D), int(window), B, H, Hk, D, n_pages, page, max_pages, max_len, dt, _ptr(workspace), _ws_bytes(workspace), _stream())
+          _ptr(out), _scale(scale, q), int(window), B, H, Hk, D, n_pages, page, max_pages, max_len, dt, _ptr(workspace), _ws_bytes(workspace), _stream())
     _written(k_cache, v_cache, given)
     return out

@@ -17,7 +17,7 @@ SOURCES = ["kla_api.hip", "kla_decode.hip", "kla_chunk_intra.hip", "kla_chunk_in
            "kla_chunk_scan_bf16.hip", "kla_chunk_rows_bf16.hip", "kla_chunk_segments.hip", "kla_chunk_bwd.hip", "kla_chunk_bwd_bf16.hip", "kla_chunk_rev_bf16.hip", "kla_probe.hip",
            "kla_layer_api.hip", "kla_layer_sums.hip", "kla_conv.hip", "kla_norm.hip", "kla_ssm.hip", "kla_ssm_bwd.hip",
            "kla_attn_api.hip", "kla_attn_fwd.hip", "kla_attn_bwd.hip"]
-BINDING_SOURCES = ["kla_binding.cpp", "kla_layer_binding.cpp"]
+BINDING_SOURCES = ["kla_binding.cpp", "kla_layer_binding.cpp", "kla_attn_binding.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # hipcc -O3 must not form packed-fp32 instructions: some of their forms have given wrong results
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -53,7 +53,7 @@ def build_lib(verbose: bool = False, extra=(), jobs: int = 8) -> str:
 
 
 def build_binding(verbose: bool = False) -> str:
-    """Compiles csrc/kla_binding.cpp and csrc/kla_layer_binding.cpp (host code only) against the installed PyTorch."""
+    """Compiles csrc/kla_*binding.cpp (host code only) against the installed PyTorch."""
     import sysconfig
     import tempfile
     from concurrent.futures import ThreadPoolExecutor

@@ -370,7 +370,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "kla_binding", nullptr, -1, methods
 PyMODINIT_FUNC PyInit_kla_binding()
 {
     PyObject* m = PyModule_Create(&module);
-    if (m && PyModule_AddFunctions(m, layer_methods) < 0) Py_CLEAR(m);
+    if (m && (PyModule_AddFunctions(m, layer_methods) < 0 || PyModule_AddFunctions(m, attn_methods) < 0)) Py_CLEAR(m);
     if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);   // whose tensors it can read
     return m;
 }

@@ -118,5 +118,7 @@ inline PyObject* wrap(const std::optional<at::Tensor>& t)
 
 // The entry points of the operators around the recurrence (kla_layer_binding.cpp), ended by an entry without a name
 extern PyMethodDef layer_methods[];
+// and those of attention (kla_attn_binding.cpp)
+extern PyMethodDef attn_methods[];
 
 }  // namespace kla_binding
