@@ -507,7 +507,7 @@ int kla_attn_bwd(const void *q, long ld_q, const void *k, long ld_k, const void 
  * max_pages page on.  A page that new tokens go to must not be read or written through another entry in the same call.
  * max_pages page at most 2^30.  workspace 256-byte aligned. */
 size_t kla_attn_extend_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t *cu_seqlens_host, int n_seq,
-                                       int max_len, kla_dtype dt);
+                                       int window, int max_len, kla_dtype dt);
 int kla_attn_extend(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
                     void *k_cache, void *v_cache, const int32_t *page_table, long ld_table, const int32_t *cached,
                     void *o, float *lse, float scale, int window,
@@ -515,7 +515,7 @@ int kla_attn_extend(const void *q, long ld_q, const void *k, long ld_k, const vo
                     int N, int T, int H, int Hk, int D, int n_pages, int page, int max_pages, int max_len,
                     kla_dtype dt, void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* One new token for B sequences: q, o [B, H, D], k, v [B, Hk, D]; workspace as for kla_attn_extend with N = B, T = 1. */
+/* One new token for B sequences: q, o [B, H, D], k, v [B, Hk, D]; workspace as for kla_attn_extend, N = B and T = 1. */
 int kla_attn_step(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
                   void *k_cache, void *v_cache, const int32_t *page_table, long ld_table, const int32_t *cached,
                   void *o, float scale, int window, int B, int H, int Hk, int D, int n_pages, int page, int max_pages,

@@ -24,7 +24,7 @@ SIGNATURES = {
     "kla_attn_fwd": (_i, [*_IN, _vp, _vp, _f, _i, *_SEQS, *[_i] * 6, _vp, _u]),
     "kla_attn_bwd_workspace_bytes": (_z, [*[_i] * 5, _vp, _i, _i]),
     "kla_attn_bwd": (_i, [*_IN, *[_vp] * 6, _f, _i, *_SEQS, *[_i] * 6, _vp, _z, _vp, _u]),
-    "kla_attn_extend_workspace_bytes": (_z, [*[_i] * 5, _vp, *[_i] * 3]),
+    "kla_attn_extend_workspace_bytes": (_z, [*[_i] * 5, _vp, *[_i] * 4]),
     "kla_attn_extend": (_i, [*_IN, *_CACHE, _vp, _vp, _f, _i, *_SEQS, *[_i] * 10, _vp, _z, _vp]),
     "kla_attn_step": (_i, [*_IN, *_CACHE, _vp, _f, _i, *[_i] * 9, _vp, _z, _vp]),
 }
@@ -165,7 +165,7 @@ def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, w
     _on_gpu(q, k, v, k_cache, v_cache, page_table, cached, cu_seqlens, out, lse, workspace)
     _dev(k_cache, v_cache, cached, cu_seqlens, out, lse, workspace)
     if workspace is None:
-        workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, max_len, dt)), q)
+        workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, int(window), max_len, dt)), q)
     given = out, lse
     if out is None:
         out = torch.empty((N, T, H, D), dtype=q.dtype, device=q.device)
@@ -194,7 +194,7 @@ def kla_attn_step(q, k, v, k_cache, v_cache, page_table, cached, scale=None, win
     _on_gpu(q, k, v, k_cache, v_cache, page_table, cached, out, workspace)
     _dev(k_cache, v_cache, cached, out, workspace)
     if workspace is None:
-        workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(B, 1, H, Hk, D, None, 0, max_len, dt)), q)
+        workspace = _workspace(int(lib().kla_attn_extend_workspace_bytes(B, 1, H, Hk, D, None, 0, int(window), max_len, dt)), q)
     given = out
     if out is None:
         out = torch.empty((B, H, D), dtype=q.dtype, device=q.device)

@@ -249,8 +249,9 @@ template <typename T> struct AttnArgs {
     float scale; int window; bool causal;
     // the cache of earlier tokens: pages [n_pages][Hk][1 << page_shift][D]; table [n_seq][max_pages], rows ld_table apart
     T* k_cache; T* v_cache; const int* table; long ld_table; const int* cached; int n_pages, page_shift, max_pages;
-    // keys in `splits` parts: part_o [splits][tokens H][D] and part_lse [splits][tokens H] (base 2)
-    int splits; float* part_o; float* part_lse; long M;
+    // keys in up to `splits` (at most 64) parts of at least `chunk` each (a multiple of 128): part_o [splits][tokens H][D] and part_lse [splits][tokens H] (base 2), where there are
+    // several; part_count [tokens H]: how many there are
+    int splits, chunk; float* part_o; float* part_lse; int* part_count; long M;
     long tiles, per;                                     // tiles of query rows of a key head: in all; of one sequence (fixed lengths)
     long unit0;                                          // first workgroup of this launch
 };
@@ -266,8 +267,8 @@ template <typename T> struct AttnBwdArgs {
 template <typename T> hipError_t launch_attn_bwd(const AttnBwdArgs<T>& a, int D, hipStream_t st);
 
 // How the forward's work is cut: rows of a tile (128: four waves of 32 rows that share tiles of keys; 32: four waves that share the rows and divide the
-// keys) and parts of the keys.
-struct AttnPlan { int rows; int splits; };
+// keys), parts of the keys and their least length.
+struct AttnPlan { int rows; int splits; int chunk; };
 template <typename T> hipError_t launch_attn_fwd(const AttnArgs<T>& a, int D, const AttnPlan& p, bool paged, hipStream_t st);
 template <typename T> hipError_t launch_attn_join(const AttnArgs<T>& a, int D, hipStream_t st);
 

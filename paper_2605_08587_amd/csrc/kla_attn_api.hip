@@ -55,21 +55,35 @@ int longest(const kla::Seqs& s, const int32_t* cu_host)
 kla::AttnPlan attn_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
 {
     long per;
-    return {attn_tiles(s, cu_host, G, 128, &per) * Hk >= 256 ? 128 : 32, 1};
+    return {attn_tiles(s, cu_host, G, 128, &per) * Hk >= 256 ? 128 : 32, 1, 128};
 }
-// New tokens over a cache of up to max_len tokens.
-kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk, int max_len)
+// New tokens over a cache: a row sees up to `span` keys.
+kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk, int max_len, int window)
 {
-    kla::AttnPlan p;
-    p.rows = (long)longest(s, cu_host) * G <= 32 ? 32 : 128;
+    kla::AttnPlan p = {128, 1, 128};
+    const int most_new = longest(s, cu_host);
+    if ((long)most_new * G <= 32) p.rows = 32;
     long per;
-    const long units = attn_tiles(s, cu_host, G, p.rows, &per) * Hk;
-    if (units == 0) { p.splits = 1; return p; }
-    const long want = p.rows == 32 ? (1024 + units - 1) / units : (512 + units - 1) / units;
-    const long most = p.rows == 32 ? ((long)max_len + 127) / 128 : ((long)max_len + 255) / 256;
-    p.splits = (int)(want < most ? want : most);
-    if (p.splits < 1) p.splits = 1;
+    const long units = attn_tiles(s, cu_host, G, p.rows, &per) * Hk, span = window && window + (long)most_new < max_len ? window + most_new : max_len;
+    if (units == 0) return p;
+    // Single tokens and drafts: a workgroup takes about 3 us until its first keys are there, one after the other on a CU (its tiles take all of the LDS), so
+    // that few keys to a part cost bandwidth; below one workgroup for each CU parts of 128 keys still gain.  (bf16, D = 128: 32 tokens over 4000 to 32000
+    // keys, 4 key heads: parts for 512, 1024 and 2048 workgroups 242, 228 and 230 us; 16 x 5 tokens over 2000 to 8000: 47, 57 and 76 us; one token
+    // over 4096: parts of 128 and 256 keys 11.1 and 12.4 us.)  More rows: two workgroups to a CU; parts are written and read in fp32 (four
+    // sequences of 300 to 518 new tokens over 4126 to 13917: for 512, 1024 and 2048 workgroups 234, 257 and 284 us).
+    if (p.rows == 32) {
+        const long fill = (256 + units - 1) / units, most = (span + 1023) / 1024;
+        long want = (1024 + units - 1) / units;
+        if (want > most) want = most > fill ? most : fill;
+        p.chunk = 128;
+        p.splits = (int)(want < (span + 127) / 128 ? want : (span + 127) / 128);
+    } else {
+        p.chunk = 256;
+        const long want = (512 + units - 1) / units, most = (span + 255) / 256;
+        p.splits = (int)(want < most ? want : most);
+    }
     if (p.splits > 64) p.splits = 64;
+    if (p.splits < 1) p.splits = 1;
     return p;
 }
 template <typename T>
@@ -79,7 +93,7 @@ kla::AttnArgs<T> attn_args(const void* q, long ld_q, const void* k, long ld_k, c
     kla::AttnArgs<T> a = {};
     a.q = static_cast<const T*>(q); a.ld_q = ld_q; a.k = static_cast<const T*>(k); a.ld_k = ld_k; a.v = static_cast<const T*>(v); a.ld_v = ld_v;
     a.o = static_cast<T*>(o); a.lse = lse; a.seqs = s; a.H = z.H; a.Hk = z.Hk; a.G = z.H / z.Hk;
-    a.scale = scale; a.window = window; a.causal = opts & KLA_ATTN_CAUSAL; a.splits = 1; a.M = M;
+    a.scale = scale; a.window = window; a.causal = opts & KLA_ATTN_CAUSAL; a.splits = 1; a.chunk = 128; a.M = M;
     return a;
 }
 // Backward: the query rows that see a tile of 128 keys are taken in parts where there are fewer than two such tiles for each CU.
@@ -106,7 +120,7 @@ BwdWork bwd_work(char* base, int parts, long M, const AttnSizes& z)
     w.bytes = c.used;
     return w;
 }
-struct ExtendWork { float *part_o, *part_lse; size_t bytes; };
+struct ExtendWork { float *part_o, *part_lse; int* part_count; size_t bytes; };
 ExtendWork extend_work(char* base, const kla::AttnPlan& p, long M, int H, int D)
 {
     Carve c{base};
@@ -114,6 +128,7 @@ ExtendWork extend_work(char* base, const kla::AttnPlan& p, long M, int H, int D)
     if (p.splits > 1) {
         w.part_o = c.take<float>((size_t)p.splits * M * H * D);
         w.part_lse = c.take<float>((size_t)p.splits * M * H);
+        w.part_count = c.take<int>((size_t)M * H);
     }
     w.bytes = c.used;
     return w;
@@ -192,12 +207,12 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
                           : run(attn_args<float>(q, ld_q, k, ld_k, v, ld_v, out, l, s, M, z, scale, window, opts));
 }
 
-size_t kla_attn_extend_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t* cu_seqlens_host, int n_seq, int max_len, kla_dtype dt)
+size_t kla_attn_extend_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t* cu_seqlens_host, int n_seq, int window, int max_len, kla_dtype dt)
 {
     kla::Seqs s;
     long M;
-    if (attn_sizes({N, T, H, Hk, D}, dt) || max_len < 0 || take_seqs(n_seq > 0 ? cu_seqlens_host : nullptr, cu_seqlens_host, n_seq, N, T, &s, &M)) return 0;
-    return extend_work(nullptr, extend_plan(s, cu_seqlens_host, H / Hk, Hk, max_len), M, H, D).bytes;
+    if (attn_sizes({N, T, H, Hk, D}, dt) || max_len < 0 || window < 0 || take_seqs(n_seq > 0 ? cu_seqlens_host : nullptr, cu_seqlens_host, n_seq, N, T, &s, &M)) return 0;
+    return extend_work(nullptr, extend_plan(s, cu_seqlens_host, H / Hk, Hk, max_len, window), M, H, D).bytes;
 }
 
 int kla_attn_extend(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* k_cache, void* v_cache, const int32_t* page_table,
@@ -219,14 +234,14 @@ int kla_attn_extend(const void* q, long ld_q, const void* k, long ld_k, const vo
                   v_cache == k || v_cache == v || v_cache == o))
         return KLA_ERR_SHAPE;
     if (!aligned(16, {q, k, v, o, k_cache, v_cache}) || !aligned(4, {lse, page_table, cached})) return KLA_ERR_ALIGN;
-    const kla::AttnPlan p = extend_plan(s, cu_seqlens_host, H / Hk, Hk, max_len);
+    const kla::AttnPlan p = extend_plan(s, cu_seqlens_host, H / Hk, Hk, max_len, window);
     const ExtendWork w = extend_work(static_cast<char*>(workspace), p, M, H, D);
     if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.k_cache = static_cast<decltype(a.k_cache)>(k_cache); a.v_cache = static_cast<decltype(a.v_cache)>(v_cache);
         a.table = page_table; a.ld_table = ld_table; a.cached = cached; a.n_pages = n_pages; a.page_shift = shift; a.max_pages = max_pages;
-        a.splits = p.splits; a.part_o = w.part_o; a.part_lse = w.part_lse;
+        a.splits = p.splits; a.chunk = p.chunk; a.part_o = w.part_o; a.part_lse = w.part_lse; a.part_count = w.part_count;
         a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);
         if (const hipError_t e = kla::launch_attn_fwd(a, D, p, true, st)) return status(e);
         return p.splits > 1 ? status(kla::launch_attn_join(a, D, st)) : (int)KLA_OK;

@@ -200,7 +200,7 @@ PyObject* attn_extend(PyObject*, PyObject* const* a, Py_ssize_t n)
         const NoGil no_gil;
         if (!o.defined()) o = fresh(*c.q, c.q->sizes(), c.type);
         if (!l.defined() && a[12] == Py_True) l = fresh(*c.q, {c.N, c.T, c.H}, at::kFloat);
-        const at::Tensor ws = bytes(*c.q, api.extend_bytes((int)c.N, (int)c.T, (int)c.H, (int)c.Hk, (int)c.D, c.cu.host, c.cu.n_seq, most, c.dt));
+        const at::Tensor ws = bytes(*c.q, api.extend_bytes((int)c.N, (int)c.T, (int)c.H, (int)c.Hk, (int)c.D, c.cu.host, c.cu.n_seq, c.window, most, c.dt));
         check(api.extend(ptr(c.q), c.ld_q, ptr(c.k), c.ld_k, ptr(c.v), c.ld_v, ptr(s.k), ptr(s.v), ints_of(s.table), s.ld_table, ints_of(s.cached), at_of(o), f_of(l),
                          c.scale, c.window, c.cu.device(), c.cu.host, c.cu.n_seq, (int)c.N, (int)c.T, (int)c.H, (int)c.Hk, (int)c.D, (int)s.n_pages, (int)s.page,
                          (int)s.max_pages, most, c.dt, at_of(ws), size_of(ws), stream()));
@@ -225,7 +225,7 @@ PyObject* attn_step(PyObject*, PyObject* const* a, Py_ssize_t n)
     try {
         const NoGil no_gil;
         if (!o.defined()) o = fresh(*c.q, c.q->sizes(), c.type);
-        const at::Tensor ws = bytes(*c.q, api.extend_bytes((int)c.N, 1, (int)c.H, (int)c.Hk, (int)c.D, nullptr, 0, most, c.dt));
+        const at::Tensor ws = bytes(*c.q, api.extend_bytes((int)c.N, 1, (int)c.H, (int)c.Hk, (int)c.D, nullptr, 0, (int)window, most, c.dt));
         check(api.step(ptr(c.q), c.ld_q, ptr(c.k), c.ld_k, ptr(c.v), c.ld_v, ptr(s.k), ptr(s.v), ints_of(s.table), s.ld_table, ints_of(s.cached), at_of(o), c.scale,
                        (int)window, (int)c.N, (int)c.H, (int)c.Hk, (int)c.D, (int)s.n_pages, (int)s.page, (int)s.max_pages, most, c.dt, at_of(ws), size_of(ws),
                        stream()));

@@ -13,12 +13,6 @@ namespace kla {
 
 namespace {
 
-// a scalar load (the index is the same in all lanes)
-__device__ __forceinline__ int uniform_load(const int* p, long i)
-{
-    return ((const __attribute__((address_space(4))) int*)(uintptr_t)p)[i];
-}
-
 // RW waves of 32 rows each that share tiles of keys (KW = 1), or KW waves that divide the keys of 32 rows (RW = 1).
 template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     static_assert(RW == 1 || KW == 1, "one way to share the work");
@@ -34,14 +28,28 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
 
     struct Keys { int n; int cached; int total; long tok0; int hk; };
 
-    // Copies of the K and V rows of keys j0 .. j0 + BN - 1 (those beyond `last` repeat it) by the waves of a team
-    static __device__ __forceinline__ void copy(const AttnArgs<T>& a, const Keys& k, int j0, int last, char* stage, int wave, int lane)
+    static constexpr int ROWS = BN / RW;                 // of a tile that one wave copies
+    static constexpr int GROUPS = (ROWS + 15) / 16;      // of rows of one page: pages begin at multiples of 16 keys
+    // The table's entries for this wave's rows of the tile at j0, lane g that of group g.  They are asked for a tile ahead of the copies that need them.
+    static __device__ __forceinline__ int entries(const AttnArgs<T>& a, const Keys& k, int j0, int last, int wave, int lane)
     {
-        constexpr int RPI = Tile::RPI, ROWS = BN / RW, NI = ROWS / RPI;
+        if (!PAGED) return 0;
+        // (one that is there in any case: no condition, and no move of the value, stands between the load and the wait for it)
+        const int j = max(min(min(j0 + wave * ROWS + 16 * (lane % GROUPS), last), k.cached - 1), 0);
+        return a.table[k.n * a.ld_table + (j >> a.page_shift)];
+    }
+    // Copies of the K and V rows of keys j0 .. j0 + BN - 1 (those beyond `last` repeat it) by the waves of a team
+    static __device__ __forceinline__ void copy(const AttnArgs<T>& a, const Keys& k, int j0, int last, int ids, char* stage, int wave, int lane)
+    {
+        constexpr int RPI = Tile::RPI, NI = ROWS / RPI;
         static_assert(ROWS % RPI == 0 && 16 % RPI == 0, "whole copy instructions");
         const long ldk = a.ld_k * (long)sizeof(T), ldv = a.ld_v * (long)sizeof(T);
         const char* kn = reinterpret_cast<const char*>(a.k) + k.tok0 * ldk + (long)k.hk * Tile::RB;
         const char* vn = reinterpret_cast<const char*>(a.v) + k.tok0 * ldv + (long)k.hk * Tile::RB;
+        long pages[GROUPS];                              // where this key head's rows of a group's page begin
+#pragma unroll
+        for (int g = 0; g < GROUPS && PAGED; ++g)
+            pages[g] = (((long)min(max(__builtin_amdgcn_readlane(ids, g), 0), a.n_pages - 1) * a.Hk + k.hk) << a.page_shift) * Tile::RB;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES;
@@ -49,18 +57,11 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
             const int piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16;
             const char *ks, *vs;
             if constexpr (PAGED) {
-                ks = kn + (long)max(j - k.cached, 0) * ldk;
-                vs = vn + (long)max(j - k.cached, 0) * ldv;
-                // (the rows of an instruction are of one page: pages begin at multiples of 16 keys)
-                const int jb = min(j0 + first, last);
-                if (jb < k.cached) {
-                    const int id = uniform_load(a.table, k.n * a.ld_table + (jb >> a.page_shift));
-                    const long page = min(max(id, 0), a.n_pages - 1);
-                    const long at = ((((page * a.Hk + k.hk) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * Tile::RB);
-                    const bool old = j < k.cached;
-                    ks = old ? reinterpret_cast<const char*>(a.k_cache) + at : ks;
-                    vs = old ? reinterpret_cast<const char*>(a.v_cache) + at : vs;
-                }
+                const bool old = j < k.cached;
+                const int fresh = max(j - k.cached, 0);
+                const long at = pages[(i * RPI) / 16] + (long)(j & ((1 << a.page_shift) - 1)) * Tile::RB;
+                ks = old ? reinterpret_cast<const char*>(a.k_cache) + at : kn + (long)fresh * ldk;
+                vs = old ? reinterpret_cast<const char*>(a.v_cache) + at : vn + (long)fresh * ldv;
             } else {
                 ks = kn + (long)j * ldk;
                 vs = vn + (long)j * ldv;
@@ -162,14 +163,21 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s.o[dt][e] = 0.f;
-        if (tb < te) copy(a, k, j_first + tb * BN, last, ring, KW > 1 ? 0 : wave, lane);
+        const int cw = KW > 1 ? 0 : wave;
+        int ids = 0;
+        if (tb < te) {
+            copy(a, k, j_first + tb * BN, last, entries(a, k, j_first + tb * BN, last, cw, lane), ring, cw, lane);
+            ids = entries(a, k, j_first + (tb + 1) * BN, last, cw, lane);
+        }
         for (int t = tb; t < te; ++t) {
             // the copies of this tile have landed, and the other stage is no longer read
+            if constexpr (PAGED) asm volatile("" : "+v"(ids));       // (awaited with the copies, not behind the ones that follow)
             if constexpr (RW > 1) wait_copies_and_barrier();
             else wait_copies();
             const int j0 = j_first + t * BN;
             char* stage = ring + ((t - tb) & 1) * STAGE;
-            if (t + 1 < te) copy(a, k, j0 + BN, last, ring + ((t - tb + 1) & 1) * STAGE, KW > 1 ? 0 : wave, lane);
+            if (t + 1 < te) copy(a, k, j0 + BN, last, ids, ring + ((t - tb + 1) & 1) * STAGE, cw, lane);
+            ids = entries(a, k, j0 + 2 * BN, last, cw, lane);
             if (j0 > r.hi_most || j0 + BN - 1 < r.lo_least) continue;
             tile<CAREFUL>(r, s, stage, j0, last, row_off, col_off, h);
         }
@@ -185,18 +193,18 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     }
 
     // 4 consecutive features of one row
-    static __device__ __forceinline__ void store4(const AttnArgs<T>& a, int split, long row, int d, float x0, float x1, float x2, float x3)
+    static __device__ __forceinline__ void store4(const AttnArgs<T>& a, int split, int parts, long row, int d, float x0, float x1, float x2, float x3)
     {
         const Floats<4> x = {{x0, x1, x2, x3}};
-        if (a.splits > 1) store_vec<float, 4>(a.part_o + ((long)split * a.M * a.H + row) * D + d, x);
+        if (parts > 1) store_vec<float, 4>(a.part_o + ((long)split * a.M * a.H + row) * D + d, x);
         else store_vec<T, 4>(a.o + row * D + d, x);
     }
-    // l = 0: no keys here (a split's part), or scores that are all -inf (the quotient is a NaN)
-    static __device__ __forceinline__ float inverse(const AttnArgs<T>& a, float l) { return a.splits > 1 && l == 0.f ? 0.f : 1.f / l; }
-    static __device__ __forceinline__ void store_lse(const AttnArgs<T>& a, int split, long row, float m, float l)
+    // l = 0: scores that are all -inf, whose quotient is a NaN, or no key of a part that this row sees
+    static __device__ __forceinline__ float inverse(int parts, float l) { return parts > 1 && l == 0.f ? 0.f : 1.f / l; }
+    static __device__ __forceinline__ void store_lse(const AttnArgs<T>& a, int split, int parts, long row, float m, float l)
     {
         const float lse = m + __log2f(l);                // base 2
-        if (a.splits > 1) a.part_lse[(long)split * a.M * a.H + row] = lse;
+        if (parts > 1) a.part_lse[(long)split * a.M * a.H + row] = lse;
         else if (a.lse) a.lse[row] = lse * kLn2;
     }
 
@@ -213,19 +221,26 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         if (!find_rows(a.seqs, a.G, 32 * RW, a.per, a.tiles - 1 - unit / a.splits / a.Hk, &at)) return;
         k.n = at.n; k.tok0 = at.tok0;
         k.cached = 0;
-        if constexpr (PAGED) k.cached = (int)min((long)max(uniform_load(a.cached, at.n), 0), (long)a.max_pages << a.page_shift);
+        if constexpr (PAGED) k.cached = (int)min((long)max(a.cached[at.n], 0), (long)a.max_pages << a.page_shift);
         k.total = k.cached + at.len;
         const int rows = at.len * a.G, row0 = at.tile * 32 * RW;
         const int t_first = row0 / a.G, t_last = min(row0 + 32 * RW - 1, rows - 1) / a.G;
         // keys of the tile's rows, and this part of them
         const int k_first = a.window ? max(0, k.cached + t_first - a.window + 1) : 0, k_last = a.causal ? k.cached + t_last : k.total - 1;
         const int j_first = k_first / BN * BN, nt = (k_last - j_first) / BN + 1;
-        const int s0 = (int)((long)nt * split / a.splits), s1 = (int)((long)nt * (split + 1) / a.splits);
+        // as many parts as leave a.chunk keys to each, `splits` at most
+        const int part = max(a.chunk / BN, (nt + a.splits - 1) / a.splits), s0 = (int)min((long)nt, (long)split * part), s1 = min(nt, s0 + part);
         int tb = s0, te = s1;
         if constexpr (KW > 1) {
             tb = s0 + (int)((long)(s1 - s0) * wave / KW);
             te = s0 + (int)((long)(s1 - s0) * (wave + 1) / KW);
         }
+        const long out0 = k.tok0 * a.H + (long)k.hk * a.G;
+        auto out_row = [&](int rr) { const int tt = rr / a.G; return out0 + (long)tt * a.H + (rr - tt * a.G); };
+        if (s0 >= s1) return;                            // (the first part is never empty)
+        const int parts = (nt + part - 1) / part;
+        if (a.splits > 1 && split == 0)
+            for (int i = threadIdx.x; i < 32 * RW && row0 + i < rows; i += 64 * W) a.part_count[out_row(row0 + i)] = parts;
         // this wave's rows
         const int w0 = row0 + (KW > 1 ? 0 : 32 * wave), row = min(w0 + n, rows - 1);
         const int t = row / a.G, head = k.hk * a.G + (row - t * a.G);
@@ -258,19 +273,17 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         } else {
             if (__any(again)) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
         }
-        const long out0 = k.tok0 * a.H + (long)k.hk * a.G;
-        auto out_row = [&](int rr) { const int tt = rr / a.G; return out0 + (long)tt * a.H + (rr - tt * a.G); };
         const float mc = s.m == -__builtin_inff() ? s.m : s.mc;
         if constexpr (KW == 1) {
             if (w0 + n < rows) {
                 const long to = out_row(row);
-                const float f = inverse(a, s.l);
+                const float f = inverse(parts, s.l);
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        store4(a, split, to, 32 * dt + 8 * i + 4 * h, s.o[dt][4 * i] * f, s.o[dt][4 * i + 1] * f, s.o[dt][4 * i + 2] * f, s.o[dt][4 * i + 3] * f);
-                if (h == 0) store_lse(a, split, to, mc, s.l);
+                        store4(a, split, parts, to, 32 * dt + 8 * i + 4 * h, s.o[dt][4 * i] * f, s.o[dt][4 * i + 1] * f, s.o[dt][4 * i + 2] * f, s.o[dt][4 * i + 3] * f);
+                if (h == 0) store_lse(a, split, parts, to, mc, s.l);
             }
         } else {
             // the waves' parts, [wave][D + 2][32]: O^T, reference, sum
@@ -297,7 +310,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                     l = fmaf(w[i], part[i * PW + (D + 1) * 32 + n], l);
                 }
                 const long to = out_row(rr);
-                const float f = inverse(a, l);
+                const float f = inverse(parts, l);
 #pragma unroll
                 for (int d = 0; d < D / (2 * KW); d += 4) {
                     float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -305,9 +318,9 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                     for (int i = 0; i < KW; ++i)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = fmaf(w[i], part[i * PW + (d0 + d + e) * 32 + n], x[e]);
-                    store4(a, split, to, d0 + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+                    store4(a, split, parts, to, d0 + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
                 }
-                if (threadIdx.x < 32) store_lse(a, split, to, m, l);
+                if (threadIdx.x < 32) store_lse(a, split, parts, to, m, l);
             }
         }
     }
@@ -336,36 +349,67 @@ template <typename T, int D, int RW, int KW, bool PAGED> hipError_t launch(AttnA
     return hipSuccess;
 }
 
-// The parts of a row joined: sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A workgroup has 256 / (D / 4) rows, a thread four features.
-template <typename T, int D> __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs<T> a, long row0)
+// The parts of a row joined: sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A row has D / 4 threads for its features times SG for its parts, so that all
+// of a row's parts are on their way at once (64 at most: lane s of every wave has part s's weight).
+template <typename T, int D, int SG> __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs<T> a, long row0)
 {
-    constexpr int TPR = D / 4;
-    const long rows = a.M * a.H, row = row0 + (long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    if (row >= rows) return;
-    const int d = (threadIdx.x % TPR) * 4;
-    float m = -__builtin_inff();
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * rows + row]);
-    float l = 0.f;
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * SG), BATCH = 8;
+    __shared__ float4 part[256];
+    const long rows = a.M * a.H;
+    const int lane = threadIdx.x & 63, quad = threadIdx.x % TPR, group = threadIdx.x / TPR % SG;
+    static_assert(TPR * SG % 64 == 0, "a wave has one row");
+    const long row = row0 + (long)blockIdx.x * ROWS + threadIdx.x / (TPR * SG);
+    const bool here = row < rows;
+    const int parts = here ? a.part_count[row] : 0;
+    float lse = -__builtin_inff();
+    if (here && lane < a.splits) lse = a.part_lse[lane * rows + row];
+    if (lane >= parts) lse = -__builtin_inff();          // (nothing was written there)
+    float m = lse;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    const float w = m == -__builtin_inff() ? 0.f : exp2_hw(lse - m);
+    const float l = wave_sum(w);
     Floats<4> x = {{0.f, 0.f, 0.f, 0.f}};
-    for (int s = 0; s < a.splits; ++s) {
-        const float w = m == -__builtin_inff() ? 0.f : exp2_hw(a.part_lse[s * rows + row] - m);
-        const Floats<4> o = load_vec<float, 4>(a.part_o + (s * rows + row) * D + d);
-        l += w;
+    if (parts > 1)                                       // (one part is the result, and stands in o)
+        for (int s0 = 0; s0 < parts; s0 += SG * BATCH) {
+            Floats<4> o[BATCH];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.v[i] = fmaf(w, o.v[i], x.v[i]);
+            for (int i = 0; i < BATCH; ++i) {
+                const int s = s0 + group + i * SG;
+                o[i] = Floats<4>{{0.f, 0.f, 0.f, 0.f}};
+                if (s < parts) o[i] = load_vec<float, 4>(a.part_o + (s * rows + row) * D + 4 * quad);
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const float ws = __shfl(w, min(s0 + group + i * SG, 63), 64);       // (0 from `parts` on)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x.v[e] = fmaf(ws, o[i].v[e], x.v[e]);
+            }
+        }
+    if constexpr (SG > 1) {
+        part[threadIdx.x] = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < SG; ++g) {
+            const float4 y = part[threadIdx.x + g * TPR];
+            x.v[0] += y.x; x.v[1] += y.y; x.v[2] += y.z; x.v[3] += y.w;
+        }
     }
-    const float f = 1.f / l;                             // (no key in any part: a NaN, as scores that are all -inf)
+    if (parts < 2) return;
+    const float f = 1.f / l;                             // (scores that are all -inf: a NaN)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] *= f;
-    store_vec<T, 4>(a.o + row * D + d, x);
-    if (a.lse && d == 0) a.lse[row] = (m + __log2f(l)) * kLn2;
+    for (int e = 0; e < 4; ++e) x.v[e] *= f;
+    store_vec<T, 4>(a.o + row * D + 4 * quad, x);
+    if (a.lse && quad == 0) a.lse[row] = (m + __log2f(l)) * kLn2;
 }
 
-template <typename T, int D> hipError_t join(const AttnArgs<T>& a, hipStream_t st)
+template <typename T, int D, int SG> hipError_t join(const AttnArgs<T>& a, hipStream_t st)
 {
-    const long per = 256 / (D / 4), blocks = (a.M * a.H + per - 1) / per, most = most_blocks(256);
+    constexpr long per = 256 / (D / 4 * SG);
+    const long blocks = (a.M * a.H + per - 1) / per, most = most_blocks(256);
     for (long b = 0; b < blocks; b += most) {
-        attn_join_kernel<T, D><<<dim3((unsigned)(blocks - b < most ? blocks - b : most)), dim3(256), 0, st>>>(a, b * per);
+        attn_join_kernel<T, D, SG><<<dim3((unsigned)(blocks - b < most ? blocks - b : most)), dim3(256), 0, st>>>(a, b * per);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
@@ -385,7 +429,11 @@ template <typename T> hipError_t launch_attn_fwd(const AttnArgs<T>& a, int D, co
     if (a.tiles == 0) return hipSuccess;
     return D == 64 ? pick<T, 64>(a, p, paged, st) : pick<T, 128>(a, p, paged, st);
 }
-template <typename T> hipError_t launch_attn_join(const AttnArgs<T>& a, int D, hipStream_t st) { return D == 64 ? join<T, 64>(a, st) : join<T, 128>(a, st); }
+template <typename T> hipError_t launch_attn_join(const AttnArgs<T>& a, int D, hipStream_t st)
+{
+    if (a.splits > 8) return D == 64 ? join<T, 64, 8>(a, st) : join<T, 128, 8>(a, st);
+    return D == 64 ? join<T, 64, 4>(a, st) : join<T, 128, 2>(a, st);
+}
 
 template hipError_t launch_attn_fwd<float>(const AttnArgs<float>&, int, const AttnPlan&, bool, hipStream_t);
 template hipError_t launch_attn_fwd<bf16_t>(const AttnArgs<bf16_t>&, int, const AttnPlan&, bool, hipStream_t);

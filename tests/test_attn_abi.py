@@ -130,16 +130,16 @@ def test_queries():
     assert lib.kla_attn_bwd_workspace_bytes(8, 4096, 8, 8, 128, None, 0, BF16) == 2 * 4 * rows      # a float or two for each row
     assert lib.kla_attn_bwd_workspace_bytes(1, 512, 8, 2, 128, None, 0, BF16) > 2 * 4 * 512 * 8     # and parts of dk, dv where workgroups are few
     wrong = np.array([0, 30, 63], dtype=np.int32)
-    for q, more in ((lib.kla_attn_bwd_workspace_bytes, (BF16,)), (lib.kla_attn_extend_workspace_bytes, (4096, BF16))):
+    for q, more in ((lib.kla_attn_bwd_workspace_bytes, (BF16,)), (lib.kla_attn_extend_workspace_bytes, (0, 4096, BF16))):
         assert q(1, 64, 8, 4, 64, CU.ctypes.data, 2, *more) > 0
         for bad in ((-1, 64, 8, 4, 64, None, 0), (1, -1, 8, 4, 64, None, 0), (1, 64, 8, 3, 64, None, 0), (1, 64, 8, 4, 65, None, 0), (1, 64, 0, 4, 64, None, 0),
                     (1, 64, 8, 4, 64, None, 2), (2, 64, 8, 4, 64, CU.ctypes.data, 2), (1, 64, 8, 4, 64, wrong.ctypes.data, 2)):
             assert q(*bad, *more) == 0, bad
         assert q(1, 64, 8, 4, 64, None, 0, *more[:-1], 7) == 0
     e = lib.kla_attn_extend_workspace_bytes
-    assert e(4, 1, 8, 4, 64, None, 0, 16, BF16) == 0                       # short caches: one part, no workspace
-    assert e(4, 1, 8, 4, 64, None, 0, -1, BF16) == 0
-    assert e(1, 1, 8, 4, 64, None, 0, 4096, BF16) >= 2 * 8 * 65 * 4
+    assert e(4, 1, 8, 4, 64, None, 0, 0, 16, BF16) == 0                       # short caches: one part, no workspace
+    assert e(4, 1, 8, 4, 64, None, 0, 0, -1, BF16) == 0 and e(4, 1, 8, 4, 64, None, 0, -1, 4096, BF16) == 0
+    assert e(1, 1, 8, 4, 64, None, 0, 0, 4096, BF16) >= 2 * 8 * 65 * 4
 
 
 def test_nothing_to_do():
