@@ -262,6 +262,7 @@ template <typename T> struct AttnBwdArgs {
     const T* d_o; T* dq; T* dk; T* dv;
     float* row_lse; float* row_delta;
     int parts; float* part_dk; float* part_dv;
+    int* bad;                                            // [workgroups of dk, dv | of dq]: something was not finite, nothing was stored
     long key_tiles, key_per;                             // tiles of 128 keys: in all; of one sequence (fixed lengths)
 };
 template <typename T> hipError_t launch_attn_bwd(const AttnBwdArgs<T>& a, int D, hipStream_t st);

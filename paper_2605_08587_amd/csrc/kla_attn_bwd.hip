@@ -66,8 +66,9 @@ template <typename E, int NDT> __device__ __forceinline__ void store_row(E* row,
 // ---- dk, dv -----------------------------------------------------------------------------------------------------------------------
 template <typename T, int D> struct Dkv {
     using Tile = RowTile<T, D>;
-    static constexpr int BM = sizeof(T) == 4 ? 32 : 64;  // query rows of a tile
-    static constexpr int TILE = BM * Tile::RB, STAGE = 2 * TILE, VECS = 2 * STAGE, LDS = VECS + 2 * 512;
+    static constexpr bool VL = sizeof(T) == 2 && D == 128;                // the tile's rows of V stand in LDS, not in registers
+    static constexpr int BM = sizeof(T) == 4 || VL ? 32 : 64;             // query rows of a tile
+    static constexpr int TILE = BM * Tile::RB, STAGE = 2 * TILE, VECS = 2 * STAGE, VROWS = VECS + 2 * 512, LDS = VROWS + (VL ? 128 * Tile::RB : 0);
     static constexpr int NDT = D / 32;
 
     struct Place { int len, rows; long tok0; int hk; };
@@ -94,44 +95,46 @@ template <typename T, int D> struct Dkv {
         }
     }
 
-    struct Keys { u32x4 k[Tile::NC], v[Tile::NC]; int lo, hi; int lo_least, lo_most, hi_least, hi_most; float c; };
+    struct Keys { u32x4 k[Tile::NC], v[VL ? 1 : Tile::NC]; const char* rows; int lo, hi; int lo_least, lo_most, hi_least, hi_most; float c; };
 
     template <bool CAREFUL>
     static __device__ __forceinline__ void block(const Keys& key, floatx16 (&dk)[NDT], floatx16 (&dv)[NDT], const char* q, const char* g, const float* vecs, int m0,
                                                  int row_off, int col_off, int h)
     {
-        floatx16 s, ds;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const floatx4 d = *reinterpret_cast<const floatx4*>(vecs + 64 + 8 * i + 4 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { s[4 * i + e] = 0.f; ds[4 * i + e] = -d[e]; }
-        }
-#pragma unroll
-        for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(s, Tile::row_slot(q, row_off, c), key.k[c]);
-#pragma unroll
-        for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(ds, Tile::row_slot(g, row_off, c), key.v[c]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const floatx4 l = *reinterpret_cast<const floatx4*>(vecs + 8 * i + 4 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[4 * i + e] = exp2_hw(fmaf(s[4 * i + e], key.c, -l[e]));
-                ds[4 * i + e] *= s[4 * i + e];
-            }
-        }
         // rows m0 .. m0 + 31 against the rows lo .. hi - 1 that see this lane's key
         const bool masked = m0 < key.lo_most || m0 + 32 > key.hi_least;
         const int lo = key.lo - m0 - 4 * h, hi = key.hi - m0 - 4 * h;
         auto seen = [&](int e) { return acc_row(e) >= lo && acc_row(e) < hi; };
+        floatx16 s, ds;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+        for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(s, Tile::row_slot(q, row_off, c), key.k[c]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const floatx4 d = *reinterpret_cast<const floatx4*>(vecs + 64 + 8 * i + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ds[4 * i + e] = -d[e];
+        }
+#pragma unroll
+        for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(ds, Tile::row_slot(g, row_off, c), VL ? Tile::row_slot(key.rows, row_off, c) : key.v[VL ? 0 : c]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const floatx4 l = *reinterpret_cast<const floatx4*>(vecs + 8 * i + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * i + e] = exp2_hw(fmaf(s[4 * i + e], key.c, -l[e]));
+        }
         if (masked) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[e] = seen(e) ? s[e] : 0.f;
-                ds[e] = seen(e) ? ds[e] : 0.f;
-            }
+            for (int e = 0; e < 16; ++e) s[e] = seen(e) ? s[e] : 0.f;
         }
         add_product<CAREFUL, T, D>(dv, g, col_off, s, masked, seen);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ds[e] *= s[e];
+        if (masked) {                                    // (0 times what is not finite)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ds[e] = seen(e) ? ds[e] : 0.f;
+        }
         add_product<CAREFUL, T, D>(dk, q, col_off, ds, masked, seen);
     }
 
@@ -157,17 +160,17 @@ template <typename T, int D> struct Dkv {
         }
     }
 
-    static __device__ __forceinline__ void run(const AttnBwdArgs<T>& a, char* lds)
+    // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, long unit, char* lds)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int n = lane & 31, h = lane >> 5;
         // the first keys of a sequence are seen by the most rows: they go first
-        const long unit = a.f.unit0 + blockIdx.x;
         const int part = (int)(unit % a.parts);
         Place p;
         p.hk = (int)(unit / a.parts % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, 1, 128, a.key_per, unit / a.parts / a.f.Hk, &at)) return;
+        if (!find_rows(a.f.seqs, 1, 128, a.key_per, unit / a.parts / a.f.Hk, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int k0 = at.tile * 128, G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : 0;
         // the rows that see key j: lo .. hi - 1
@@ -183,16 +186,30 @@ template <typename T, int D> struct Dkv {
             const char* kp = reinterpret_cast<const char*>(a.f.k + (p.tok0 + j) * a.f.ld_k + (long)p.hk * D);
             const char* vp = reinterpret_cast<const char*>(a.f.v + (p.tok0 + j) * a.f.ld_v + (long)p.hk * D);
 #pragma unroll
-            for (int c = 0; c < Tile::NC; ++c) { key.k[c] = ld16(kp + (2 * c + h) * 16); key.v[c] = ld16(vp + (2 * c + h) * 16); }
+            for (int c = 0; c < Tile::NC; ++c) {
+                key.k[c] = ld16(kp + (2 * c + h) * 16);
+                if constexpr (!VL) key.v[c] = ld16(vp + (2 * c + h) * 16);
+            }
+        }
+        key.rows = lds + VROWS + 32 * wave * Tile::RB;
+        if constexpr (VL) {                              // each wave its own (awaited with the first tile)
+#pragma unroll
+            for (int i = 0; i < 32 / Tile::RPI; ++i) {
+                const int row = i * Tile::RPI + lane / Tile::PIECES;
+                const char* vp = reinterpret_cast<const char*>(a.f.v + (p.tok0 + min(w0 + row, p.len - 1)) * a.f.ld_v + (long)p.hk * D);
+                dma16_from(vp + ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16, lds + VROWS + (32 * wave + i * Tile::RPI) * Tile::RB);
+            }
         }
         const int j0 = min(w0, p.len - 1), j1 = min(w0 + 31, p.len - 1);
         key.lo = lo_of(j); key.hi = hi_of(j);
         key.lo_least = lo_of(j0); key.lo_most = lo_of(j1);
         key.hi_least = hi_of(j0); key.hi_most = w0 >= p.len ? -1 : hi_of(j1);        // (a wave without keys passes over every tile)
         floatx16 dk[NDT], dv[NDT];
-        pass<false>(a, p, key, dk, dv, tb, te, lds, wave, lane);
-        if (__syncthreads_or(!all_finite(dk) || !all_finite(dv))) pass<true>(a, p, key, dk, dv, tb, te, lds, wave, lane);
-        if (w0 + n >= p.len) return;
+        pass<CAREFUL>(a, p, key, dk, dv, tb, te, lds, wave, lane);
+        if constexpr (!CAREFUL) {
+            if (__syncthreads_or(!all_finite(dk) || !all_finite(dv))) return false;
+        }
+        if (w0 + n >= p.len) return true;
         const long row = (p.tok0 + j) * a.f.Hk + p.hk;
         if (a.parts > 1) {
             const long to = ((long)part * a.f.M * a.f.Hk + row) * D;
@@ -202,6 +219,7 @@ template <typename T, int D> struct Dkv {
             store_row<T>(a.dk + row * D, dk, a.f.scale, h);
             store_row<T>(a.dv + row * D, dv, 1.f, h);
         }
+        return true;
     }
 };
 
@@ -274,15 +292,15 @@ template <typename T, int D> struct Dq {
         }
     }
 
-    static __device__ __forceinline__ void run(const AttnBwdArgs<T>& a, char* lds)
+    // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, long unit, char* lds)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int n = lane & 31, h = lane >> 5;
-        const long unit = a.f.unit0 + blockIdx.x;
         Place p;
         p.hk = (int)(unit % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, a.f.G, 128, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, &at)) return;
+        if (!find_rows(a.f.seqs, a.f.G, 128, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : p.len;
         const int row0 = at.tile * 128, t_first = row0 / G, t_last = min(row0 + 127, p.rows - 1) / G;
@@ -305,9 +323,12 @@ template <typename T, int D> struct Dq {
         r.lo = lo_of(t); r.lo_least = lo_of(u0); r.lo_most = lo_of(u1);
         r.hi = hi_of(t); r.hi_least = hi_of(u0); r.hi_most = w0 >= p.rows ? -1 : hi_of(u1);
         floatx16 dq[NDT];
-        pass<false>(a, p, r, dq, tb, te, last, lds, wave, lane);
-        if (__syncthreads_or(!all_finite(dq))) pass<true>(a, p, r, dq, tb, te, last, lds, wave, lane);
+        pass<CAREFUL>(a, p, r, dq, tb, te, last, lds, wave, lane);
+        if constexpr (!CAREFUL) {
+            if (__syncthreads_or(!all_finite(dq))) return false;
+        }
         if (w0 + n < p.rows) store_row<T>(a.dq + to * D, dq, a.f.scale, h);
+        return true;
     }
 };
 
@@ -331,12 +352,34 @@ template <typename T> __global__ __launch_bounds__(256) void attn_parts_kernel(c
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_dkv_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
-    Dkv<T, D>::run(a, lds);
+    const long unit = a.f.unit0 + blockIdx.x;
+    const bool done = Dkv<T, D>::template run<false>(a, unit, lds);
+    if (threadIdx.x == 0) a.bad[unit] = !done;
 }
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_dq_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
-    Dq<T, D>::run(a, lds);
+    const long unit = a.f.unit0 + blockIdx.x;
+    const bool done = Dq<T, D>::template run<false>(a, unit, lds);
+    if (threadIdx.x == 0) a.bad[a.key_tiles * a.f.Hk * a.parts + unit] = !done;
+}
+// The work of workgroups that found something not finite, once more with products that keep it apart.  (A kernel of its own: what those products need
+// would take registers from the ordinary ones.  Without such work it reads the flags.)
+template <typename T, int D> __global__ __launch_bounds__(256, 1) void attn_again_kernel(const AttnBwdArgs<T> a)
+{
+    extern __shared__ char lds[];
+    const long first = a.key_tiles * a.f.Hk * a.parts, all = first + a.f.tiles * a.f.Hk;
+    for (long base = (long)blockIdx.x * 256; base < all; base += (long)gridDim.x * 256) {
+        // 256 flags at a time
+        const long mine = base + threadIdx.x;
+        if (!__syncthreads_or(mine < all && a.bad[mine])) continue;
+        for (long unit = base; unit < base + 256 && unit < all; ++unit) {
+            if (!a.bad[unit]) continue;
+            if (unit < first) Dkv<T, D>::template run<true>(a, unit, lds);
+            else Dq<T, D>::template run<true>(a, unit - first, lds);
+            __syncthreads();
+        }
+    }
 }
 
 template <typename A, typename K> hipError_t launch_units(A& a, K kernel, int lds, long units, hipStream_t st)
@@ -363,6 +406,9 @@ template <typename T, int D> hipError_t bwd(AttnBwdArgs<T> a, hipStream_t st)
     }
     if (const hipError_t e = launch_units(a, attn_dkv_kernel<T, D>, Dkv<T, D>::LDS, a.key_tiles * a.f.Hk * a.parts, st)) return e;
     if (const hipError_t e = launch_units(a, attn_dq_kernel<T, D>, Dq<T, D>::LDS, a.f.tiles * a.f.Hk, st)) return e;
+    constexpr int LDS = Dkv<T, D>::LDS > Dq<T, D>::LDS ? Dkv<T, D>::LDS : Dq<T, D>::LDS;
+    const long flags = (a.key_tiles * a.f.Hk * a.parts + a.f.tiles * a.f.Hk + 255) / 256;
+    if (const hipError_t e = launch_units(a, attn_again_kernel<T, D>, LDS, flags < 1024 ? flags : 1024, st)) return e;
     if (a.parts > 1) {
         const long n = a.f.M * a.f.Hk * D, sums = (2 * n / 4 + 255) / 256;
         for (long b = 0; b < sums; b += most) {

@@ -267,12 +267,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         State s;
         char* ring = lds + (KW > 1 ? wave * 2 * STAGE : 0);
         pass<false>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
-        const bool again = !all_finite(s);
-        if constexpr (RW > 1) {
-            if (__syncthreads_or(again)) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
-        } else {
-            if (__any(again)) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
-        }
+        if (__syncthreads_or(!all_finite(s))) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
         const float mc = s.m == -__builtin_inff() ? s.m : s.mc;
         if constexpr (KW == 1) {
             if (w0 + n < rows) {
