@@ -191,6 +191,14 @@ __device__ __forceinline__ void add_product(floatx16 (&acc)[NDT], const char* ti
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void wait_copies_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// This thread, for a second run of a workgroup's work behind a first: what is derived from it anew is not kept in registers through the first.
+__device__ __forceinline__ int thread_again()
+{
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 // max and sum over the two halves of a wave, in every lane
 __device__ __forceinline__ float halves_max(float x)
 {
@@ -207,7 +215,7 @@ __device__ __forceinline__ float halves_sum(float x)
 // The query heads of one key head are rows of their own: row r of (sequence, key head) is token r / G, head hk G + r % G.  A key head's tiles of
 // `rows` rows (packed batches: tile `idx` counted over the sequences in order); false: there is none.
 struct RowPlace { int n; int tile; int len; long tok0; };
-__device__ __forceinline__ bool find_rows(const Seqs& s, int G, int rows, long per, long idx, RowPlace* p)
+__device__ __forceinline__ bool find_rows(const Seqs& s, int G, int rows, long per, long idx, int lane, RowPlace* p)
 {
     if (!s.cu) {                                         // tiles of one number of all sequences beside each other
         p->n = (int)(idx % s.n_seq);
@@ -216,7 +224,6 @@ __device__ __forceinline__ bool find_rows(const Seqs& s, int G, int rows, long p
         p->tok0 = (long)p->n * s.T;
         return p->tile < per;
     }
-    const int lane = threadIdx.x & 63;
     for (int base = 0; base < s.n_seq; base += 64) {
         const int n = min(base + lane, s.n_seq - 1);
         const int c0 = s.cu[n], len = base + lane < s.n_seq ? s.cu[n + 1] - c0 : 0;
@@ -262,7 +269,6 @@ template <typename T> struct AttnBwdArgs {
     const T* d_o; T* dq; T* dk; T* dv;
     float* row_lse; float* row_delta;
     int parts; float* part_dk; float* part_dv;
-    int* bad;                                            // [workgroups of dk, dv | of dq]: something was not finite, nothing was stored
     long key_tiles, key_per;                             // tiles of 128 keys: in all; of one sequence (fixed lengths)
 };
 template <typename T> hipError_t launch_attn_bwd(const AttnBwdArgs<T>& a, int D, hipStream_t st);

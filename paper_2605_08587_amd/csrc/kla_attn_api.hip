@@ -106,15 +106,13 @@ int attn_bwd_parts(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
     const long parts = want < most ? want : most;
     return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
 }
-struct BwdWork { float *row_lse, *row_delta, *part_dk, *part_dv; int* bad; size_t bytes; };
-BwdWork bwd_work(char* base, int parts, const kla::Seqs& s, const int32_t* cu_host, long M, const AttnSizes& z)
+struct BwdWork { float *row_lse, *row_delta, *part_dk, *part_dv; size_t bytes; };
+BwdWork bwd_work(char* base, int parts, long M, const AttnSizes& z)
 {
     Carve c{base};
     BwdWork w = {};
     w.row_lse = c.take<float>((size_t)M * z.H);
     w.row_delta = c.take<float>((size_t)M * z.H);
-    long per;
-    w.bad = c.take<int>((size_t)(attn_tiles(s, cu_host, 1, 128, &per) * parts + attn_tiles(s, cu_host, z.H / z.Hk, 128, &per)) * z.Hk);
     if (parts > 1) {
         w.part_dk = c.take<float>((size_t)parts * M * z.Hk * z.D);
         w.part_dv = c.take<float>((size_t)parts * M * z.Hk * z.D);
@@ -169,7 +167,7 @@ size_t kla_attn_bwd_workspace_bytes(int N, int T, int H, int Hk, int D, const in
     long M;
     const AttnSizes z = {N, T, H, Hk, D};
     if (attn_sizes(z, dt) || take_seqs(n_seq > 0 ? cu_seqlens_host : nullptr, cu_seqlens_host, n_seq, N, T, &s, &M)) return 0;
-    return bwd_work(nullptr, attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk), s, cu_seqlens_host, M, z).bytes;
+    return bwd_work(nullptr, attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk), M, z).bytes;
 }
 
 int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, const void* o, const float* lse, const void* d_o, void* dq,
@@ -189,7 +187,7 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
     if (M > 0 && (dq == dk || dq == dv || dk == dv)) return KLA_ERR_SHAPE;
     if (!aligned(16, {q, k, v, o, d_o, dq, dk, dv}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
     const int parts = attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk);
-    const BwdWork w = bwd_work(static_cast<char*>(workspace), parts, s, cu_seqlens_host, M, z);
+    const BwdWork w = bwd_work(static_cast<char*>(workspace), parts, M, z);
     if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
@@ -198,7 +196,7 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
         kla::AttnBwdArgs<E> b = {};
         b.f = a;
         b.d_o = static_cast<const E*>(d_o); b.dq = static_cast<Q>(dq); b.dk = static_cast<Q>(dk); b.dv = static_cast<Q>(dv);
-        b.row_lse = w.row_lse; b.row_delta = w.row_delta; b.parts = parts; b.part_dk = w.part_dk; b.part_dv = w.part_dv; b.bad = w.bad;
+        b.row_lse = w.row_lse; b.row_delta = w.row_delta; b.parts = parts; b.part_dk = w.part_dk; b.part_dv = w.part_dv;
         b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 128, &b.f.per);
         b.key_tiles = attn_tiles(s, cu_seqlens_host, 1, 128, &b.key_per);
         return status(kla::launch_attn_bwd(b, D, st));

@@ -161,16 +161,17 @@ template <typename T, int D> struct Dkv {
     }
 
     // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
-    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, long unit, char* lds)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, int thread, char* lds)
     {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+        const long unit = a.f.unit0 + blockIdx.x;
         const int n = lane & 31, h = lane >> 5;
         // the first keys of a sequence are seen by the most rows: they go first
         const int part = (int)(unit % a.parts);
         Place p;
         p.hk = (int)(unit / a.parts % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, 1, 128, a.key_per, unit / a.parts / a.f.Hk, &at)) return true;
+        if (!find_rows(a.f.seqs, 1, 128, a.key_per, unit / a.parts / a.f.Hk, lane, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int k0 = at.tile * 128, G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : 0;
         // the rows that see key j: lo .. hi - 1
@@ -293,14 +294,15 @@ template <typename T, int D> struct Dq {
     }
 
     // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
-    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, long unit, char* lds)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, int thread, char* lds)
     {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+        const long unit = a.f.unit0 + blockIdx.x;
         const int n = lane & 31, h = lane >> 5;
         Place p;
         p.hk = (int)(unit % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, a.f.G, 128, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, &at)) return true;
+        if (!find_rows(a.f.seqs, a.f.G, 128, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, lane, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : p.len;
         const int row0 = at.tile * 128, t_first = row0 / G, t_last = min(row0 + 127, p.rows - 1) / G;
@@ -352,34 +354,12 @@ template <typename T> __global__ __launch_bounds__(256) void attn_parts_kernel(c
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_dkv_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
-    const long unit = a.f.unit0 + blockIdx.x;
-    const bool done = Dkv<T, D>::template run<false>(a, unit, lds);
-    if (threadIdx.x == 0) a.bad[unit] = !done;
+    if (!Dkv<T, D>::template run<false>(a, threadIdx.x, lds)) Dkv<T, D>::template run<true>(a, thread_again(), lds);
 }
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_dq_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
-    const long unit = a.f.unit0 + blockIdx.x;
-    const bool done = Dq<T, D>::template run<false>(a, unit, lds);
-    if (threadIdx.x == 0) a.bad[a.key_tiles * a.f.Hk * a.parts + unit] = !done;
-}
-// The work of workgroups that found something not finite, once more with products that keep it apart.  (A kernel of its own: what those products need
-// would take registers from the ordinary ones.  Without such work it reads the flags.)
-template <typename T, int D> __global__ __launch_bounds__(256, 1) void attn_again_kernel(const AttnBwdArgs<T> a)
-{
-    extern __shared__ char lds[];
-    const long first = a.key_tiles * a.f.Hk * a.parts, all = first + a.f.tiles * a.f.Hk;
-    for (long base = (long)blockIdx.x * 256; base < all; base += (long)gridDim.x * 256) {
-        // 256 flags at a time
-        const long mine = base + threadIdx.x;
-        if (!__syncthreads_or(mine < all && a.bad[mine])) continue;
-        for (long unit = base; unit < base + 256 && unit < all; ++unit) {
-            if (!a.bad[unit]) continue;
-            if (unit < first) Dkv<T, D>::template run<true>(a, unit, lds);
-            else Dq<T, D>::template run<true>(a, unit - first, lds);
-            __syncthreads();
-        }
-    }
+    if (!Dq<T, D>::template run<false>(a, threadIdx.x, lds)) Dq<T, D>::template run<true>(a, thread_again(), lds);
 }
 
 template <typename A, typename K> hipError_t launch_units(A& a, K kernel, int lds, long units, hipStream_t st)
@@ -406,9 +386,6 @@ template <typename T, int D> hipError_t bwd(AttnBwdArgs<T> a, hipStream_t st)
     }
     if (const hipError_t e = launch_units(a, attn_dkv_kernel<T, D>, Dkv<T, D>::LDS, a.key_tiles * a.f.Hk * a.parts, st)) return e;
     if (const hipError_t e = launch_units(a, attn_dq_kernel<T, D>, Dq<T, D>::LDS, a.f.tiles * a.f.Hk, st)) return e;
-    constexpr int LDS = Dkv<T, D>::LDS > Dq<T, D>::LDS ? Dkv<T, D>::LDS : Dq<T, D>::LDS;
-    const long flags = (a.key_tiles * a.f.Hk * a.parts + a.f.tiles * a.f.Hk + 255) / 256;
-    if (const hipError_t e = launch_units(a, attn_again_kernel<T, D>, LDS, flags < 1024 ? flags : 1024, st)) return e;
     if (a.parts > 1) {
         const long n = a.f.M * a.f.Hk * D, sums = (2 * n / 4 + 255) / 256;
         for (long b = 0; b < sums; b += most) {

@@ -72,10 +72,10 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     }
 
     // The new tokens whose first row lies in this tile go into their pages.
-    static __device__ __forceinline__ void store_new(const AttnArgs<T>& a, const Keys& k, int t0, int t1)
+    static __device__ __forceinline__ void store_new(const AttnArgs<T>& a, const Keys& k, int t0, int t1, int thread)
     {
         constexpr int P = Tile::PIECES;
-        for (int i = threadIdx.x; i < (t1 - t0) * P; i += 64 * W) {
+        for (int i = thread; i < (t1 - t0) * P; i += 64 * W) {
             const int t = t0 + i / P, pos = k.cached + t;
             const long page = (long)pos >> a.page_shift;
             if (page >= a.max_pages) continue;
@@ -208,9 +208,10 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         else if (a.lse) a.lse[row] = lse * kLn2;
     }
 
-    static __device__ __forceinline__ void run(const AttnArgs<T>& a, char* lds)
+    // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnArgs<T>& a, int thread, char* lds)
     {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
         const int n = lane & 31, h = lane >> 5;
         // heaviest tiles (the last ones of their sequences) first; the parts of a tile and the key heads beside each other
         const long unit = a.unit0 + blockIdx.x;
@@ -218,7 +219,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         Keys k;
         k.hk = (int)(unit / a.splits % a.Hk);
         RowPlace at;
-        if (!find_rows(a.seqs, a.G, 32 * RW, a.per, a.tiles - 1 - unit / a.splits / a.Hk, &at)) return;
+        if (!find_rows(a.seqs, a.G, 32 * RW, a.per, a.tiles - 1 - unit / a.splits / a.Hk, lane, &at)) return true;
         k.n = at.n; k.tok0 = at.tok0;
         k.cached = 0;
         if constexpr (PAGED) k.cached = (int)min((long)max(a.cached[at.n], 0), (long)a.max_pages << a.page_shift);
@@ -237,10 +238,10 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         }
         const long out0 = k.tok0 * a.H + (long)k.hk * a.G;
         auto out_row = [&](int rr) { const int tt = rr / a.G; return out0 + (long)tt * a.H + (rr - tt * a.G); };
-        if (s0 >= s1) return;                            // (the first part is never empty)
+        if (s0 >= s1) return true;                       // (the first part is never empty)
         const int parts = (nt + part - 1) / part;
-        if (a.splits > 1 && split == 0)
-            for (int i = threadIdx.x; i < 32 * RW && row0 + i < rows; i += 64 * W) a.part_count[out_row(row0 + i)] = parts;
+        if (a.splits > 1 && split == 0 && !CAREFUL)
+            for (int i = thread; i < 32 * RW && row0 + i < rows; i += 64 * W) a.part_count[out_row(row0 + i)] = parts;
         // this wave's rows
         const int w0 = row0 + (KW > 1 ? 0 : 32 * wave), row = min(w0 + n, rows - 1);
         const int t = row / a.G, head = k.hk * a.G + (row - t * a.G);
@@ -259,15 +260,17 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         r.hi_least = a.causal ? k.cached + tw0 : k.total - 1;
         r.hi_most = w0 >= rows ? -1 : a.causal ? k.cached + tw1 : k.total - 1;       // (no rows of its own: every tile is passed over)
         if constexpr (PAGED) {
-            if (split == 0) {                            // tokens whose first row lies in this tile
+            if (split == 0 && !CAREFUL) {                    // tokens whose first row lies in this tile
                 const int u0 = (row0 + a.G - 1) / a.G, u1 = min(at.len, (row0 + 32 * RW + a.G - 1) / a.G);
-                store_new(a, k, u0, u1);
+                store_new(a, k, u0, u1, thread);
             }
         }
         State s;
         char* ring = lds + (KW > 1 ? wave * 2 * STAGE : 0);
-        pass<false>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
-        if (__syncthreads_or(!all_finite(s))) pass<true>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
+        pass<CAREFUL>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);
+        if constexpr (!CAREFUL) {
+            if (__syncthreads_or(!all_finite(s))) return false;
+        }
         const float mc = s.m == -__builtin_inff() ? s.m : s.mc;
         if constexpr (KW == 1) {
             if (w0 + n < rows) {
@@ -294,7 +297,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                 part[wave * PW + (D + 1) * 32 + n] = s.l;
             }
             __syncthreads();
-            const int rr = row0 + n, d0 = (threadIdx.x >> 5) * (D / (2 * KW));
+            const int rr = row0 + n, d0 = (thread >> 5) * (D / (2 * KW));
             if (rr < rows) {
                 float m = -__builtin_inff(), l = 0.f, w[KW];
 #pragma unroll
@@ -315,9 +318,10 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                         for (int e = 0; e < 4; ++e) x[e] = fmaf(w[i], part[i * PW + (d0 + d + e) * 32 + n], x[e]);
                     store4(a, split, parts, to, d0 + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
                 }
-                if (threadIdx.x < 32) store_lse(a, split, parts, to, m, l);
+                if (thread < 32) store_lse(a, split, parts, to, m, l);
             }
         }
+        return true;
     }
 };
 
@@ -325,7 +329,8 @@ template <typename T, int D, int RW, int KW, bool PAGED>
 __global__ __launch_bounds__(64 * RW * KW, KW > 1 ? 1 : 2) void attn_fwd_kernel(const AttnArgs<T> a)
 {
     extern __shared__ char lds[];
-    Fwd<T, D, RW, KW, PAGED>::run(a, lds);
+    using F = Fwd<T, D, RW, KW, PAGED>;
+    if (!F::template run<false>(a, threadIdx.x, lds)) F::template run<true>(a, thread_again(), lds);
 }
 
 template <typename T, int D, int RW, int KW, bool PAGED> hipError_t launch(AttnArgs<T> a, hipStream_t st)
