@@ -199,6 +199,13 @@ __device__ __forceinline__ int thread_again()
     return t;
 }
 
+// What was loaded is there: without this the compiler, which does not know of the copies, would wait for such loads inside the loop over the tiles, and
+// with them for the copies issued since.
+__device__ __forceinline__ void settle(u32x4& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
+// row i of rows `stride` bytes apart (one multiplication of 32 bits)
+__device__ __forceinline__ const char* row_at(const char* p, int i, uint32_t stride) { return p + (uint64_t)(uint32_t)i * stride; }
+
 // max and sum over the two halves of a wave, in every lane
 __device__ __forceinline__ float halves_max(float x)
 {

@@ -14,13 +14,14 @@ using kla::bf16_t;
 static_assert(KLA_ATTN_CAUSAL == (int)kla::kAttnCausal, "option bits");
 
 constexpr int kMaxAttnRows = 1 << 30;                    // tokens times query heads of a key head, and positions (32-bit numbers)
+constexpr int kMaxAttnGroup = 1 << 16;                   // query heads of a key head
 constexpr long kMaxAttnStride = 1L << 28;                // elements from one token to the next
 
 struct AttnSizes { int N, T, H, Hk, D; };
 int attn_sizes(const AttnSizes& z, int dt)
 {
     if (!dt_ok(dt)) return KLA_ERR_DTYPE;
-    if (z.N < 0 || z.T < 0 || z.H <= 0 || z.Hk <= 0 || z.H % z.Hk || (z.D != 64 && z.D != 128) || (long)z.H * z.D > kMaxAttnStride ||
+    if (z.N < 0 || z.T < 0 || z.H <= 0 || z.Hk <= 0 || z.H % z.Hk || z.H / z.Hk > kMaxAttnGroup || (z.D != 64 && z.D != 128) || (long)z.H * z.D > kMaxAttnStride ||
         (long)z.T * (z.H / z.Hk) > kMaxAttnRows)
         return KLA_ERR_SHAPE;
     return KLA_OK;

@@ -72,25 +72,44 @@ template <typename T, int D> struct Dkv {
     static constexpr int NDT = D / 32;
 
     struct Place { int len, rows; long tok0; int hk; };
+    // The first row of a tile, and which head of which token it is: it goes on by BM, without a division
+    struct Front {
+        int m0, token, head;
+        __device__ __forceinline__ void next(int G)
+        {
+            m0 += BM;
+            token += BM / G;
+            head += BM % G;
+            if (head >= G) { head -= G; ++token; }
+        }
+    };
 
-    static __device__ __forceinline__ void copy(const AttnBwdArgs<T>& a, const Place& p, int m0, char* lds, int stage, int wave, int lane)
+    static __device__ __forceinline__ void copy(const AttnBwdArgs<T>& a, const Place& p, const Front& f, char* lds, int stage, int wave, int lane)
     {
         constexpr int RPI = Tile::RPI, ROWS = BM / 4, NI = ROWS / RPI;
-        const long ld = a.f.ld_q * (long)sizeof(T);
-        const char* q = reinterpret_cast<const char*>(a.f.q) + p.tok0 * ld + (long)p.hk * a.f.G * Tile::RB;
-        const char* g = reinterpret_cast<const char*>(a.d_o) + (p.tok0 * a.f.H + (long)p.hk * a.f.G) * Tile::RB;
+        const uint32_t ld = (uint32_t)(a.f.ld_q * sizeof(T)), ldo = (uint32_t)a.f.H * Tile::RB;      // (at most 2^30)
+        const char* q = reinterpret_cast<const char*>(a.f.q) + (p.tok0 + f.token) * (long)ld + (long)p.hk * a.f.G * Tile::RB;
+        const char* g = reinterpret_cast<const char*>(a.d_o) + ((p.tok0 + f.token) * a.f.H + (long)p.hk * a.f.G) * Tile::RB;
         char* at = lds + stage * STAGE;
+        // row f.m0 + i as a token and a head of it: (x + 1/2) / G is at least 1/2G from any whole number, far more than x below 2^17 loses in fp32
+        const float over = 1.f / (float)a.f.G;
+        auto split = [&](int i, int* head) {
+            const int x = f.head + min(i, p.rows - 1 - f.m0), t = (int)(((float)x + 0.5f) * over);
+            *head = x - t * a.f.G;
+            return t;
+        };
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES, r = min(m0 + row, p.rows - 1);
-            const int t = r / a.f.G, head = r - t * a.f.G;
-            const int piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16;
-            dma16_from(q + (long)t * ld + head * Tile::RB + piece, at + first * Tile::RB);
-            dma16_from(g + ((long)t * a.f.H + head) * Tile::RB + piece, at + TILE + first * Tile::RB);
+            const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES;
+            int head;
+            const int t = split(row, &head), piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16 + head * Tile::RB;
+            dma16_from(row_at(q, t, ld) + piece, at + first * Tile::RB);
+            dma16_from(row_at(g, t, ldo) + piece, at + TILE + first * Tile::RB);
         }
         if (wave < 2) {
-            const int r = min(m0 + lane, p.rows - 1), t = r / a.f.G;
-            const long row = (p.tok0 + t) * a.f.H + (long)p.hk * a.f.G + (r - t * a.f.G);
+            int head;
+            const int t = split(lane, &head);
+            const long row = (p.tok0 + f.token + t) * a.f.H + (long)p.hk * a.f.G + head;
             dma4_from((wave ? a.row_delta : a.row_lse) + row, lds + VECS + stage * 512 + wave * 256);
         }
     }
@@ -110,6 +129,7 @@ template <typename T, int D> struct Dkv {
         for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
         for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(s, Tile::row_slot(q, row_off, c), key.k[c]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const floatx4 d = *reinterpret_cast<const floatx4*>(vecs + 64 + 8 * i + 4 * h);
@@ -118,6 +138,7 @@ template <typename T, int D> struct Dkv {
         }
 #pragma unroll
         for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(ds, Tile::row_slot(g, row_off, c), VL ? Tile::row_slot(key.rows, row_off, c) : key.v[VL ? 0 : c]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const floatx4 l = *reinterpret_cast<const floatx4*>(vecs + 8 * i + 4 * h);
@@ -128,6 +149,7 @@ template <typename T, int D> struct Dkv {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = seen(e) ? s[e] : 0.f;
         }
+        __builtin_amdgcn_sched_barrier(0);
         add_product<CAREFUL, T, D>(dv, g, col_off, s, masked, seen);
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] *= s[e];
@@ -135,6 +157,7 @@ template <typename T, int D> struct Dkv {
 #pragma unroll
             for (int e = 0; e < 16; ++e) ds[e] = seen(e) ? ds[e] : 0.f;
         }
+        __builtin_amdgcn_sched_barrier(0);
         add_product<CAREFUL, T, D>(dk, q, col_off, ds, masked, seen);
     }
 
@@ -145,11 +168,13 @@ template <typename T, int D> struct Dkv {
         const int h = lane >> 5, row_off = Tile::row_offset(lane & 31, h), col_off = Tile::col_offset(lane);
         clear(dk);
         clear(dv);
-        if (tb < te) copy(a, p, tb * BM, lds, 0, wave, lane);
+        Front front = {tb * BM, tb * BM / a.f.G, tb * BM % a.f.G};
+        if (tb < te) copy(a, p, front, lds, 0, wave, lane);
         for (int t = tb; t < te; ++t) {
             wait_copies_and_barrier();
             const int stage = (t - tb) & 1;
-            if (t + 1 < te) copy(a, p, (t + 1) * BM, lds, stage ^ 1, wave, lane);
+            front.next(a.f.G);
+            if (t + 1 < te) copy(a, p, front, lds, stage ^ 1, wave, lane);
 #pragma unroll 1
             for (int b = 0; b < BM / 32; ++b) {
                 const int m0 = t * BM + 32 * b;
@@ -191,6 +216,11 @@ template <typename T, int D> struct Dkv {
                 key.k[c] = ld16(kp + (2 * c + h) * 16);
                 if constexpr (!VL) key.v[c] = ld16(vp + (2 * c + h) * 16);
             }
+        }
+#pragma unroll
+        for (int c = 0; c < Tile::NC; ++c) {
+            settle(key.k[c]);
+            if constexpr (!VL) settle(key.v[c]);
         }
         key.rows = lds + VROWS + 32 * wave * Tile::RB;
         if constexpr (VL) {                              // each wave its own (awaited with the first tile)
@@ -236,15 +266,15 @@ template <typename T, int D> struct Dq {
     static __device__ __forceinline__ void copy(const AttnBwdArgs<T>& a, const Place& p, int j0, int last, char* at, int wave, int lane)
     {
         constexpr int RPI = Tile::RPI, ROWS = BN / 4, NI = ROWS / RPI;
-        const long ldk = a.f.ld_k * (long)sizeof(T), ldv = a.f.ld_v * (long)sizeof(T);
-        const char* k = reinterpret_cast<const char*>(a.f.k) + p.tok0 * ldk + (long)p.hk * Tile::RB;
-        const char* v = reinterpret_cast<const char*>(a.f.v) + p.tok0 * ldv + (long)p.hk * Tile::RB;
+        const uint32_t ldk = (uint32_t)(a.f.ld_k * sizeof(T)), ldv = (uint32_t)(a.f.ld_v * sizeof(T));
+        const char* k = reinterpret_cast<const char*>(a.f.k) + p.tok0 * (long)ldk + (long)p.hk * Tile::RB;
+        const char* v = reinterpret_cast<const char*>(a.f.v) + p.tok0 * (long)ldv + (long)p.hk * Tile::RB;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES, j = min(j0 + row, last);
             const int piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16;
-            dma16_from(k + (long)j * ldk + piece, at + first * Tile::RB);
-            dma16_from(v + (long)j * ldv + piece, at + TILE + first * Tile::RB);
+            dma16_from(row_at(k, j, ldk) + piece, at + first * Tile::RB);
+            dma16_from(row_at(v, j, ldv) + piece, at + TILE + first * Tile::RB);
         }
     }
 
@@ -321,6 +351,10 @@ template <typename T, int D> struct Dq {
 #pragma unroll
             for (int c = 0; c < Tile::NC; ++c) { r.q[c] = ld16(q + (2 * c + h) * 16); r.g[c] = ld16(g + (2 * c + h) * 16); }
         }
+#pragma unroll
+        for (int c = 0; c < Tile::NC; ++c) { settle(r.q[c]); settle(r.g[c]); }
+        settle(r.lse);
+        settle(r.delta);
         const int u0 = min(w0, p.rows - 1) / G, u1 = min(w0 + 31, p.rows - 1) / G;
         r.lo = lo_of(t); r.lo_least = lo_of(u0); r.lo_most = lo_of(u1);
         r.hi = hi_of(t); r.hi_least = hi_of(u0); r.hi_most = w0 >= p.rows ? -1 : hi_of(u1);

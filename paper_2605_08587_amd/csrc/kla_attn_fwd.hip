@@ -43,9 +43,9 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     {
         constexpr int RPI = Tile::RPI, NI = ROWS / RPI;
         static_assert(ROWS % RPI == 0 && 16 % RPI == 0, "whole copy instructions");
-        const long ldk = a.ld_k * (long)sizeof(T), ldv = a.ld_v * (long)sizeof(T);
-        const char* kn = reinterpret_cast<const char*>(a.k) + k.tok0 * ldk + (long)k.hk * Tile::RB;
-        const char* vn = reinterpret_cast<const char*>(a.v) + k.tok0 * ldv + (long)k.hk * Tile::RB;
+        const uint32_t ldk = (uint32_t)(a.ld_k * sizeof(T)), ldv = (uint32_t)(a.ld_v * sizeof(T));      // (at most 2^30)
+        const char* kn = reinterpret_cast<const char*>(a.k) + k.tok0 * (long)ldk + (long)k.hk * Tile::RB;
+        const char* vn = reinterpret_cast<const char*>(a.v) + k.tok0 * (long)ldv + (long)k.hk * Tile::RB;
         long pages[GROUPS];                              // where this key head's rows of a group's page begin
 #pragma unroll
         for (int g = 0; g < GROUPS && PAGED; ++g)
@@ -60,11 +60,11 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                 const bool old = j < k.cached;
                 const int fresh = max(j - k.cached, 0);
                 const long at = pages[(i * RPI) / 16] + (long)(j & ((1 << a.page_shift) - 1)) * Tile::RB;
-                ks = old ? reinterpret_cast<const char*>(a.k_cache) + at : kn + (long)fresh * ldk;
-                vs = old ? reinterpret_cast<const char*>(a.v_cache) + at : vn + (long)fresh * ldv;
+                ks = old ? reinterpret_cast<const char*>(a.k_cache) + at : row_at(kn, fresh, ldk);
+                vs = old ? reinterpret_cast<const char*>(a.v_cache) + at : row_at(vn, fresh, ldv);
             } else {
-                ks = kn + (long)j * ldk;
-                vs = vn + (long)j * ldv;
+                ks = row_at(kn, j, ldk);
+                vs = row_at(vn, j, ldv);
             }
             dma16_from(ks + piece, stage + first * Tile::RB);
             dma16_from(vs + piece, stage + TILE + first * Tile::RB);
@@ -265,6 +265,8 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                 store_new(a, k, u0, u1, thread);
             }
         }
+#pragma unroll
+        for (int c = 0; c < Tile::NC; ++c) settle(r.q[c]);
         State s;
         char* ring = lds + (KW > 1 ? wave * 2 * STAGE : 0);
         pass<CAREFUL>(a, k, r, s, j_first, tb, te, k_last, ring, wave, lane);

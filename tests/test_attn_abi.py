@@ -202,3 +202,8 @@ def test_python_refusals():
         if "out" not in bad:
             with pytest.raises((ValueError, TypeError), match=what):
                 kla.kla_attn_extend(q, k, k, **d)
+
+
+@pytest.mark.parametrize("f", [fwd, bwd, extend, step])
+def test_groups_beyond_the_limit(f):
+    assert f(H=(1 << 16) + 1, Hk=1, ld_q=1 << 23) == E_SHAPE
