@@ -468,7 +468,7 @@ int kla_gated_norm_bwd(const void *x, long ld_x, const void *gate, long ld_gate,
  * H a multiple of Hk: query head h reads key head h / (H / Hk).
  *   - q [N, T, H, D], k, v [N, T, Hk, D] dt: tokens ld_q, ld_k, ld_v elements apart (column ranges of a wider tensor), the heads of a
  *     token contiguous.  D is 64 or 128.  Rows start at multiples of 16 bytes: pointers and strides are (else KLA_ERR_ALIGN).
- *   - T H / Hk at most 2^30, H / Hk at most 2^16, H D and strides at most 2^28 elements, scale positive and finite.
+ *   - T H / Hk at most 2^30, H / Hk at most 2^16, H D and strides at most 2^24 elements, scale positive and finite.
  *   - Scores, softmax and sums are fp32; weights are rounded to dt where they are multiplied with values, outputs once.
  *     Results are deterministic (no atomics).  A key that a query does not see has no part in its row, also where it holds a NaN.  A
  *     row whose scores are all -inf, or one of whose scores is +inf or NaN, is NaN.

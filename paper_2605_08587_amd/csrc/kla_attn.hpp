@@ -189,6 +189,8 @@ __device__ __forceinline__ void add_product(floatx16 (&acc)[NDT], const char* ti
 
 // All of this wave's copies have landed, and its LDS reads are done; then every wave's.
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// all but the last N of them
+template <int N> __device__ __forceinline__ void wait_but_and_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_copies_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // This thread, for a second run of a workgroup's work behind a first: what is derived from it anew is not kept in registers through the first.
@@ -202,6 +204,7 @@ __device__ __forceinline__ int thread_again()
 // What was loaded is there: without this the compiler, which does not know of the copies, would wait for such loads inside the loop over the tiles, and
 // with them for the copies issued since.
 __device__ __forceinline__ void settle(u32x4& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void settle(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
 // row i of rows `stride` bytes apart (one multiplication of 32 bits)
 __device__ __forceinline__ const char* row_at(const char* p, int i, uint32_t stride) { return p + (uint64_t)(uint32_t)i * stride; }

@@ -15,7 +15,7 @@ static_assert(KLA_ATTN_CAUSAL == (int)kla::kAttnCausal, "option bits");
 
 constexpr int kMaxAttnRows = 1 << 30;                    // tokens times query heads of a key head, and positions (32-bit numbers)
 constexpr int kMaxAttnGroup = 1 << 16;                   // query heads of a key head
-constexpr long kMaxAttnStride = 1L << 28;                // elements from one token to the next
+constexpr long kMaxAttnStride = 1L << 24;                // elements from one token to the next
 
 struct AttnSizes { int N, T, H, Hk, D; };
 int attn_sizes(const AttnSizes& z, int dt)
@@ -53,10 +53,11 @@ int longest(const kla::Seqs& s, const int32_t* cu_host)
 }
 // The forward over whole sequences: four waves of 32 rows each to a workgroup, which share every tile of keys, unless that gives too few workgroups
 // for the CUs; then four waves share 32 rows and divide the keys.
-kla::AttnPlan attn_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
+kla::AttnPlan attn_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk, int D)
 {
     long per;
-    return {attn_tiles(s, cu_host, G, 128, &per) * Hk >= 256 ? 128 : 32, 1, 128};
+    const long units = attn_tiles(s, cu_host, G, 128, &per) * Hk;
+    return {units >= (D == 64 ? 320 : 256) ? 128 : 32, 1, 128};
 }
 // New tokens over a cache: a row sees up to `span` keys.
 kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk, int max_len, int window)
@@ -152,7 +153,7 @@ int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void*
     if (M > 0 && (!q || !k || !v || !o)) return KLA_ERR_NULL;
     if (M > 0 && (o == q || o == k || o == v)) return KLA_ERR_SHAPE;                   // (other workgroups still read them)
     if (!aligned(16, {q, k, v, o}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
-    const kla::AttnPlan p = attn_plan(s, cu_seqlens_host, H / Hk, Hk);
+    const kla::AttnPlan p = attn_plan(s, cu_seqlens_host, H / Hk, Hk, D);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);

@@ -390,7 +390,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
     extern __shared__ char lds[];
     if (!Dkv<T, D>::template run<false>(a, threadIdx.x, lds)) Dkv<T, D>::template run<true>(a, thread_again(), lds);
 }
-template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_dq_kernel(const AttnBwdArgs<T> a)
+template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 ? (D == 128 ? 1 : 2) : D == 64 ? 3 : 2) void attn_dq_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
     if (!Dq<T, D>::template run<false>(a, threadIdx.x, lds)) Dq<T, D>::template run<true>(a, thread_again(), lds);

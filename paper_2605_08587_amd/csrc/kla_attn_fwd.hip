@@ -43,7 +43,8 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     {
         constexpr int RPI = Tile::RPI, NI = ROWS / RPI;
         static_assert(ROWS % RPI == 0 && 16 % RPI == 0, "whole copy instructions");
-        const uint32_t ldk = (uint32_t)(a.ld_k * sizeof(T)), ldv = (uint32_t)(a.ld_v * sizeof(T));      // (at most 2^30)
+        // (strides at most 2^26 bytes: 63 of them fit 32 bits)
+        const uint32_t ldk = (uint32_t)(a.ld_k * sizeof(T)), ldv = (uint32_t)(a.ld_v * sizeof(T));
         const char* kn = reinterpret_cast<const char*>(a.k) + k.tok0 * (long)ldk + (long)k.hk * Tile::RB;
         const char* vn = reinterpret_cast<const char*>(a.v) + k.tok0 * (long)ldv + (long)k.hk * Tile::RB;
         long pages[GROUPS];                              // where this key head's rows of a group's page begin
@@ -53,21 +54,19 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES;
-            const int j = min(j0 + row, last);
             const int piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16;
-            const char *ks, *vs;
+            char* to = stage + first * Tile::RB;
             if constexpr (PAGED) {
+                const int j = min(j0 + row, last), fresh = max(j - k.cached, 0);
                 const bool old = j < k.cached;
-                const int fresh = max(j - k.cached, 0);
                 const long at = pages[(i * RPI) / 16] + (long)(j & ((1 << a.page_shift) - 1)) * Tile::RB;
-                ks = old ? reinterpret_cast<const char*>(a.k_cache) + at : row_at(kn, fresh, ldk);
-                vs = old ? reinterpret_cast<const char*>(a.v_cache) + at : row_at(vn, fresh, ldv);
+                dma16_from((old ? reinterpret_cast<const char*>(a.k_cache) + at : row_at(kn, fresh, ldk)) + piece, to);
+                dma16_from((old ? reinterpret_cast<const char*>(a.v_cache) + at : row_at(vn, fresh, ldv)) + piece, to + TILE);
             } else {
-                ks = row_at(kn, j, ldk);
-                vs = row_at(vn, j, ldv);
+                const int i0 = min(row, last - j0);      // (tiles begin at keys that are there)
+                dma16(row_at(kn, j0, ldk), (int)(i0 * ldk + piece), to);
+                dma16(row_at(vn, j0, ldv), (int)(i0 * ldv + piece), to + TILE);
             }
-            dma16_from(ks + piece, stage + first * Tile::RB);
-            dma16_from(vs + piece, stage + TILE + first * Tile::RB);
         }
     }
 
@@ -328,7 +327,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
 };
 
 template <typename T, int D, int RW, int KW, bool PAGED>
-__global__ __launch_bounds__(64 * RW * KW, KW > 1 ? 1 : 2) void attn_fwd_kernel(const AttnArgs<T> a)
+__global__ __launch_bounds__(64 * RW * KW, KW > 1 ? (D == 64 && sizeof(T) == 2 ? 2 : 1) : D == 64 ? 3 : 2) void attn_fwd_kernel(const AttnArgs<T> a)
 {
     extern __shared__ char lds[];
     using F = Fwd<T, D, RW, KW, PAGED>;
