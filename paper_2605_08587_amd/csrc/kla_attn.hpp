@@ -279,6 +279,7 @@ template <typename T> struct AttnBwdArgs {
     const T* d_o; T* dq; T* dk; T* dv;
     float* row_lse; float* row_delta;
     int parts; float* part_dk; float* part_dv;
+    bool beside;                                         // dk, dv and dq in one launch, rows of dq in tiles of 64 (else of 128: f.tiles)
     long key_tiles, key_per;                             // tiles of 128 keys: in all; of one sequence (fixed lengths)
 };
 template <typename T> hipError_t launch_attn_bwd(const AttnBwdArgs<T>& a, int D, hipStream_t st);

@@ -98,7 +98,12 @@ kla::AttnArgs<T> attn_args(const void* q, long ld_q, const void* k, long ld_k, c
     a.scale = scale; a.window = window; a.causal = opts & KLA_ATTN_CAUSAL; a.splits = 1; a.chunk = 128; a.M = M;
     return a;
 }
-// Backward: the query rows that see a tile of 128 keys are taken in parts where there are fewer than two such tiles for each CU.
+// Backward: below so many tiles of 128 query rows (two for each CU) dk, dv and dq run beside each other in one launch, dq's tiles half as large and with their keys
+// in two parts.  bf16: 2048 tokens, 8 heads of 64 and 128 76 -> 44 and 117 -> 66 us; at 768 tiles 238 and 399 us apart, 248 and 422 beside.  fp32: 777
+// tokens, 8 heads over 2 of 64 132 -> 56 us, 2048 tokens and 8 of 128 571 -> 315 us.
+constexpr long kAttnBeside = 512;
+// The query rows that see a tile of 128 keys are taken in parts where there are fewer than two such tiles for each CU.  (More parts cost more in sums
+// than they even out: bf16, D = 128, 4096 tokens, 8 heads, 3 sequences 399 us whole, 471 in two parts.)
 int attn_bwd_parts(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
 {
     long per;
@@ -200,6 +205,8 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
         b.d_o = static_cast<const E*>(d_o); b.dq = static_cast<Q>(dq); b.dk = static_cast<Q>(dk); b.dv = static_cast<Q>(dv);
         b.row_lse = w.row_lse; b.row_delta = w.row_delta; b.parts = parts; b.part_dk = w.part_dk; b.part_dv = w.part_dv;
         b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 128, &b.f.per);
+        b.beside = b.f.tiles * Hk < kAttnBeside;
+        if (b.beside) b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 64, &b.f.per);
         b.key_tiles = attn_tiles(s, cu_seqlens_host, 1, 128, &b.key_per);
         return status(kla::launch_attn_bwd(b, D, st));
     };

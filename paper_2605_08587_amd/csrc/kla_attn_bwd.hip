@@ -186,10 +186,9 @@ template <typename T, int D> struct Dkv {
     }
 
     // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
-    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, int thread, char* lds)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, long unit, int thread, char* lds)
     {
         const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-        const long unit = a.f.unit0 + blockIdx.x;
         const int n = lane & 31, h = lane >> 5;
         // the first keys of a sequence are seen by the most rows: they go first
         const int part = (int)(unit % a.parts);
@@ -255,17 +254,20 @@ template <typename T, int D> struct Dkv {
 };
 
 // ---- dq ---------------------------------------------------------------------------------------------------------------------------
-template <typename T, int D> struct Dq {
+// Four waves: RW of 32 rows each, which share tiles of keys, times KW = 4 / RW that divide the tiles, in step, and add up what they have.
+template <typename T, int D, int RW> struct Dq {
     using Tile = RowTile<T, D>;
-    static constexpr int BN = sizeof(T) == 4 ? 32 : 64;  // keys of a tile
-    static constexpr int TILE = BN * Tile::RB, STAGE = 2 * TILE, LDS = 2 * STAGE;
+    static constexpr int KW = 4 / RW;
+    static constexpr int BN = sizeof(T) == 4 || KW > 1 ? 32 : 64;         // keys of a tile
+    static constexpr int TILE = BN * Tile::RB, STAGE = 2 * TILE, LDS = KW * 2 * STAGE;
     static constexpr int NDT = D / 32;
+    static_assert(KW == 1 || (KW - 1) * RW * 32 * D * 4 <= LDS, "room for the other waves' sums");
 
     struct Place { int len, rows; long tok0; int hk; };
 
     static __device__ __forceinline__ void copy(const AttnBwdArgs<T>& a, const Place& p, int j0, int last, char* at, int wave, int lane)
     {
-        constexpr int RPI = Tile::RPI, ROWS = BN / 4, NI = ROWS / RPI;
+        constexpr int RPI = Tile::RPI, ROWS = BN / RW, NI = ROWS / RPI;
         const uint32_t ldk = (uint32_t)(a.f.ld_k * sizeof(T)), ldv = (uint32_t)(a.f.ld_v * sizeof(T));
         const char* k = reinterpret_cast<const char*>(a.f.k) + p.tok0 * (long)ldk + (long)p.hk * Tile::RB;
         const char* v = reinterpret_cast<const char*>(a.f.v) + p.tok0 * (long)ldv + (long)p.hk * Tile::RB;
@@ -302,44 +304,68 @@ template <typename T, int D> struct Dq {
         add_product<CAREFUL, T, D>(dq, k, col_off, ds, masked, seen);
     }
 
+    // Tiles tb .. te - 1: in step i the waves of part kw have tile tb + KW i + kw
     template <bool CAREFUL>
     static __device__ __forceinline__ void pass(const AttnBwdArgs<T>& a, const Place& p, const Rows& r, floatx16 (&dq)[NDT], int tb, int te, int last, char* lds,
-                                                int wave, int lane)
+                                                int rw, int kw, int lane)
     {
         const int h = lane >> 5, row_off = Tile::row_offset(lane & 31, h), col_off = Tile::col_offset(lane);
         clear(dq);
-        copy(a, p, tb * BN, last, lds, wave, lane);
-        for (int t = tb; t < te; ++t) {
+        char* ring = lds + kw * 2 * STAGE;
+        if (tb + kw < te) copy(a, p, (tb + kw) * BN, last, ring, rw, lane);
+        int stage = 0;
+        for (int t = tb + kw; t - kw < te; t += KW, stage ^= 1) {
             wait_copies_and_barrier();
-            const int stage = (t - tb) & 1;
-            if (t + 1 < te) copy(a, p, (t + 1) * BN, last, lds + (stage ^ 1) * STAGE, wave, lane);
+            if (t + KW < te) copy(a, p, (t + KW) * BN, last, ring + (stage ^ 1) * STAGE, rw, lane);
+            if (t >= te) continue;
 #pragma unroll 1
             for (int b = 0; b < BN / 32; ++b) {
                 const int j0 = t * BN + 32 * b;
                 if (j0 > min(r.hi_most, last) || j0 + 31 < r.lo_least) continue;
-                const char* k = lds + stage * STAGE + 32 * b * Tile::RB;
+                const char* k = ring + stage * STAGE + 32 * b * Tile::RB;
                 block<CAREFUL>(r, dq, k, k + TILE, j0, last, row_off, col_off, h);
             }
+        }
+        if constexpr (KW > 1) {                          // [kw - 1][rw][D][32]
+            __syncthreads();
+            float* part = reinterpret_cast<float*>(lds);
+            const int n = lane & 31;
+            if (kw > 0) {
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) part[(((kw - 1) * RW + rw) * D + 32 * dt + acc_row(e) + 4 * h) * 32 + n] = dq[dt][e];
+            }
+            __syncthreads();
+            if (kw == 0) {
+#pragma unroll
+                for (int w = 1; w < KW; ++w)
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) dq[dt][e] += part[(((w - 1) * RW + rw) * D + 32 * dt + acc_row(e) + 4 * h) * 32 + n];
+            }
+            __syncthreads();
         }
     }
 
     // false: something is not finite, nothing was stored (CAREFUL stores whatever comes out)
-    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, int thread, char* lds)
+    template <bool CAREFUL> static __device__ __forceinline__ bool run(const AttnBwdArgs<T>& a, long unit, int thread, char* lds)
     {
         const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
-        const long unit = a.f.unit0 + blockIdx.x;
+        const int rw = wave % RW, kw = wave / RW;
         const int n = lane & 31, h = lane >> 5;
         Place p;
         p.hk = (int)(unit % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, a.f.G, 128, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, lane, &at)) return true;
+        if (!find_rows(a.f.seqs, a.f.G, 32 * RW, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, lane, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : p.len;
-        const int row0 = at.tile * 128, t_first = row0 / G, t_last = min(row0 + 127, p.rows - 1) / G;
+        const int row0 = at.tile * 32 * RW, t_first = row0 / G, t_last = min(row0 + 32 * RW - 1, p.rows - 1) / G;
         auto lo_of = [&](int t) { return max(0, t - window + 1) * (int)a.f.causal; };
         auto hi_of = [&](int t) { return a.f.causal ? t : p.len - 1; };
         const int last = hi_of(t_last), tb = lo_of(t_first) / BN, te = last / BN + 1;
-        const int w0 = row0 + 32 * wave, row = min(w0 + n, p.rows - 1), t = row / G;
+        const int w0 = row0 + 32 * rw, row = min(w0 + n, p.rows - 1), t = row / G;
         const long to = (p.tok0 + t) * a.f.H + (long)p.hk * G + (row - t * G);
         Rows r;
         r.c = a.f.scale * kLog2e;
@@ -359,11 +385,11 @@ template <typename T, int D> struct Dq {
         r.lo = lo_of(t); r.lo_least = lo_of(u0); r.lo_most = lo_of(u1);
         r.hi = hi_of(t); r.hi_least = hi_of(u0); r.hi_most = w0 >= p.rows ? -1 : hi_of(u1);
         floatx16 dq[NDT];
-        pass<CAREFUL>(a, p, r, dq, tb, te, last, lds, wave, lane);
+        pass<CAREFUL>(a, p, r, dq, tb, te, last, lds, rw, kw, lane);
         if constexpr (!CAREFUL) {
             if (__syncthreads_or(!all_finite(dq))) return false;
         }
-        if (w0 + n < p.rows) store_row<T>(a.dq + to * D, dq, a.f.scale, h);
+        if (kw == 0 && w0 + n < p.rows) store_row<T>(a.dq + to * D, dq, a.f.scale, h);
         return true;
     }
 };
@@ -385,15 +411,27 @@ template <typename T> __global__ __launch_bounds__(256) void attn_parts_kernel(c
     store_vec<T, 4>((second ? dv : dk) + at, x);
 }
 
+template <typename K, typename A> __device__ __forceinline__ void run_unit(const A& a, long unit, char* lds)
+{
+    if (!K::template run<false>(a, unit, threadIdx.x, lds)) K::template run<true>(a, unit, thread_again(), lds);
+}
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_dkv_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
-    if (!Dkv<T, D>::template run<false>(a, threadIdx.x, lds)) Dkv<T, D>::template run<true>(a, thread_again(), lds);
+    run_unit<Dkv<T, D>>(a, a.f.unit0 + blockIdx.x, lds);
 }
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 ? (D == 128 ? 1 : 2) : D == 64 ? 3 : 2) void attn_dq_kernel(const AttnBwdArgs<T> a)
 {
     extern __shared__ char lds[];
-    if (!Dq<T, D>::template run<false>(a, threadIdx.x, lds)) Dq<T, D>::template run<true>(a, thread_again(), lds);
+    run_unit<Dq<T, D, 4>>(a, a.f.unit0 + blockIdx.x, lds);
+}
+// Both beside each other, dq's rows in smaller tiles: where neither fills the GPU
+template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void attn_bwd_kernel(const AttnBwdArgs<T> a)
+{
+    extern __shared__ char lds[];
+    const long dq = a.f.tiles * a.f.Hk, unit = a.f.unit0 + blockIdx.x;
+    if (unit < dq) run_unit<Dq<T, D, 2>>(a, unit, lds);
+    else run_unit<Dkv<T, D>>(a, unit - dq, lds);
 }
 
 template <typename A, typename K> hipError_t launch_units(A& a, K kernel, int lds, long units, hipStream_t st)
@@ -418,8 +456,13 @@ template <typename T, int D> hipError_t bwd(AttnBwdArgs<T> a, hipStream_t st)
         attn_rows_kernel<T, D><<<dim3((unsigned)(blocks - b < most ? blocks - b : most)), dim3(256), 0, st>>>(a, b * PER);
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    if (const hipError_t e = launch_units(a, attn_dkv_kernel<T, D>, Dkv<T, D>::LDS, a.key_tiles * a.f.Hk * a.parts, st)) return e;
-    if (const hipError_t e = launch_units(a, attn_dq_kernel<T, D>, Dq<T, D>::LDS, a.f.tiles * a.f.Hk, st)) return e;
+    if (a.beside) {
+        constexpr int LDS = Dkv<T, D>::LDS > Dq<T, D, 2>::LDS ? Dkv<T, D>::LDS : Dq<T, D, 2>::LDS;
+        if (const hipError_t e = launch_units(a, attn_bwd_kernel<T, D>, LDS, (a.key_tiles * a.parts + a.f.tiles) * a.f.Hk, st)) return e;
+    } else {
+        if (const hipError_t e = launch_units(a, attn_dkv_kernel<T, D>, Dkv<T, D>::LDS, a.key_tiles * a.f.Hk * a.parts, st)) return e;
+        if (const hipError_t e = launch_units(a, attn_dq_kernel<T, D>, Dq<T, D, 4>::LDS, a.f.tiles * a.f.Hk, st)) return e;
+    }
     if (a.parts > 1) {
         const long n = a.f.M * a.f.Hk * D, sums = (2 * n / 4 + 255) / 256;
         for (long b = 0; b < sums; b += most) {
