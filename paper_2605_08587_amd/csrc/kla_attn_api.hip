@@ -64,9 +64,14 @@ kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int
 {
     kla::AttnPlan p = {128, 1, 128};
     const int most_new = longest(s, cu_host);
-    if ((long)most_new * G <= 32) p.rows = 32;
-    long per;
-    const long units = attn_tiles(s, cu_host, G, p.rows, &per) * Hk, span = window && window + (long)most_new < max_len ? window + most_new : max_len;
+    const long span = window && window + (long)most_new < max_len ? window + most_new : max_len;
+    long per, units = attn_tiles(s, cu_host, G, 128, &per) * Hk;
+    // Rows in tiles of 32 with their keys divided among the waves, too, where larger tiles in parts of 256 keys would leave CUs idle (fp32, three
+    // sequences of 54 to 160 new tokens over 115 to 852, 8 heads over 2 of 64: 31 us a call in tiles of 128, 20 of 32; bf16, 16 tokens over 1000 17 and 12 us).
+    if ((long)most_new * G <= 32 || units * ((span + 255) / 256) < 256) {
+        p.rows = 32;
+        units = attn_tiles(s, cu_host, G, 32, &per) * Hk;
+    }
     if (units == 0) return p;
     // Single tokens and drafts: a workgroup takes about 3 us until its first keys are there, one after the other on a CU (its tiles take all of the LDS), so
     // that few keys to a part cost bandwidth; below one workgroup for each CU parts of 128 keys still gain.  (bf16, D = 128: 32 tokens over 4000 to 32000
