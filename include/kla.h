@@ -477,19 +477,22 @@ int kla_gated_norm_bwd(const void *x, long ld_x, const void *gate, long ld_gate,
 enum { KLA_ATTN_CAUSAL = 1 };
 
 /*   o           [N, T, H, D] dt                     out
- *   lse         [N, T, H] fp32                      out  or NULL if unwanted; what the backward takes */
+ *   lse         [N, T, H] fp32                      out  or NULL if unwanted; what the backward takes
+ *   rest        [N, T, H, D] bf16                   out  or NULL if unwanted: what the rounding of o leaves out (dt = bf16 only, else
+ *                                                        KLA_ERR_DTYPE), for a backward whose dq and dk do not carry that rounding */
 int kla_attn_fwd(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
-                 void *o, float *lse, float scale, int window,
+                 void *o, float *lse, void *rest, float scale, int window,
                  const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
                  int N, int T, int H, int Hk, int D, kla_dtype dt, void *hip_stream, unsigned opts);
 
-/* Gradients of sum <d_o, o> from the inputs and outputs of the forward (o, lse).
- *   o, d_o [N, T, H, D] dt, lse [N, T, H] fp32      in   contiguous
+/* Gradients of sum <d_o, o> from the inputs and outputs of the forward (o, lse and, unless NULL, rest).
+ *   o, d_o, rest [N, T, H, D] dt, lse [N, T, H] fp32   in   contiguous
  *   dq [N, T, H, D], dk, dv [N, T, Hk, D] dt        out  contiguous
  * workspace 256-byte aligned. */
 size_t kla_attn_bwd_workspace_bytes(int N, int T, int H, int Hk, int D, const int32_t *cu_seqlens_host, int n_seq, kla_dtype dt);
 int kla_attn_bwd(const void *q, long ld_q, const void *k, long ld_k, const void *v, long ld_v,
-                 const void *o, const float *lse, const void *d_o, void *dq, void *dk, void *dv, float scale, int window,
+                 const void *o, const float *lse, const void *rest, const void *d_o, void *dq, void *dk, void *dv,
+                 float scale, int window,
                  const int32_t *cu_seqlens_dev, const int32_t *cu_seqlens_host, int n_seq,
                  int N, int T, int H, int Hk, int D, kla_dtype dt,
                  void *workspace, size_t workspace_bytes, void *hip_stream, unsigned opts);

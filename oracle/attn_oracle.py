@@ -54,7 +54,7 @@ def backward(q, k, v, d_o, scale, first=0, causal=True, window=0):
     return dq.reshape(n, H, D), dk, dv
 
 
-def bounds(q, k, v, scale, u, d_o=None, first=0, causal=True, window=0):
+def bounds(q, k, v, scale, u, d_o=None, first=0, causal=True, window=0, rest=False):
     """How far each element may be from the two functions above: o, lse and, with d_o, dq, dk, dv.  u: half a step of the type that outputs, weights and
     their gradients are rounded to.  With e = 2^-24, to first order:
       a score is a sum of D products (D e of the sum of their sizes) times a rounded constant, less a rounded reference: rho of its weight,
@@ -63,7 +63,8 @@ def bounds(q, k, v, scale, u, d_o=None, first=0, causal=True, window=0):
       weights are rounded by u where they meet v, and the quotient by the sum of weights brings rho and 2 n e once more:
           do = u |o| + (u + 2 rho + 4 n e) sum p |v|;     dlse = rho + 2 n e + 4 e (|lse| + 1);
       delta = <d_o, o> takes o with its error; a weight formed again from lse is off by rho + dlse; ds = p (dp - delta) is rounded by u:
-          dds = |ds| (u + rho + dlse) + p (D e |d_o|.|v| + <|d_o|, do> + D e |d_o|.|o|)."""
+          dds = |ds| (u + rho + dlse) + p (D e |d_o|.|v| + <|d_o|, do> + D e |d_o|.|o|);
+      rest: o comes with what its rounding left out, rounded in turn: u^2 |o| in the place of u |o| there."""
     n, H, D = q.shape
     m, Hk, _ = k.shape
     G, e = H // Hk, 2.0 ** -24
@@ -93,7 +94,7 @@ def bounds(q, k, v, scale, u, d_o=None, first=0, causal=True, window=0):
         dp = np.einsum("hgd,jhd->hgj", g, vv)
         ds = p * (dp - (p * dp).sum(-1, keepdims=True))
         r = (rho + b_lse[i])[..., None]
-        b_delta = (abs(g) * b_o[i]).sum(-1) + D * e * (abs(g) * abs(o)).sum(-1)
+        b_delta = (abs(g) * (b_o[i] - (u - u * u) * abs(o) * rest)).sum(-1) + D * e * (abs(g) * abs(o)).sum(-1)
         b_ds = abs(ds) * (u + r) + p * (D * e * np.einsum("hgd,jhd->hgj", abs(g), abs(vv)) + b_delta[..., None])
         dq = scale * np.einsum("hgj,jhd->hgd", ds, kk)
         b_q[i] = (u + e) * abs(dq) + scale * np.einsum("hgj,jhd->hgd", b_ds + 2 * N * e * abs(ds), abs(kk))

@@ -21,9 +21,9 @@ _SEQS = [_vp, _vp, _i]
 _IN = [_vp, _l] * 3
 _CACHE = [_vp, _vp, _vp, _l, _vp]
 SIGNATURES = {
-    "kla_attn_fwd": (_i, [*_IN, _vp, _vp, _f, _i, *_SEQS, *[_i] * 6, _vp, _u]),
+    "kla_attn_fwd": (_i, [*_IN, _vp, _vp, _vp, _f, _i, *_SEQS, *[_i] * 6, _vp, _u]),
     "kla_attn_bwd_workspace_bytes": (_z, [*[_i] * 5, _vp, _i, _i]),
-    "kla_attn_bwd": (_i, [*_IN, *[_vp] * 6, _f, _i, *_SEQS, *[_i] * 6, _vp, _z, _vp, _u]),
+    "kla_attn_bwd": (_i, [*_IN, *[_vp] * 7, _f, _i, *_SEQS, *[_i] * 6, _vp, _z, _vp, _u]),
     "kla_attn_extend_workspace_bytes": (_z, [*[_i] * 5, _vp, *[_i] * 4]),
     "kla_attn_extend": (_i, [*_IN, *_CACHE, _vp, _vp, _f, _i, *_SEQS, *[_i] * 10, _vp, _z, _vp]),
     "kla_attn_step": (_i, [*_IN, *_CACHE, _vp, _f, _i, *[_i] * 9, _vp, _z, _vp]),
@@ -50,12 +50,13 @@ def _heads(q, k, v, lead):
     return H, Hk, D, dt, (_rows("q", q, 2), _rows("k", k, 2), _rows("v", v, 2))
 
 
-def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, want_lse=True, out=None, lse=None):
+def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, want_lse=True, out=None, lse=None, rest=None):
     """Softmax attention of q [N,T,H,D] over k, v [N,T,Hk,D] of the same sequence (D 64 or 128, H a multiple of Hk): returns (o, lse), lse [N,T,H]
     fp32 the logarithms of the rows' sums (None unless want_lse).  causal: a token sees those up to itself, and with window > 0 only the last
-    `window` of them; scale: of the scores, D ** -0.5 by default.  Packed batches by cu_seqlens as in kla_chunk_fwd."""
+    `window` of them; scale: of the scores, D ** -0.5 by default.  Packed batches by cu_seqlens as in kla_chunk_fwd.  rest: a bfloat16 tensor like o that
+    receives what o's rounding leaves out, for kla_attn_bwd."""
     host = _host(cu_seqlens, cu_seqlens_host)
-    r = _native("attn_fwd", "kla_attn_fwd", q, k, v, _scale(scale, q), bool(causal), window, cu_seqlens, host, bool(want_lse), out, lse)
+    r = _native("attn_fwd", "kla_attn_fwd", q, k, v, _scale(scale, q), bool(causal), window, cu_seqlens, host, bool(want_lse), out, lse, rest)
     if r is not None:
         return r
     H, Hk, D, dt, ld = _heads(q, k, v, 2)
@@ -64,21 +65,22 @@ def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu
     _sizes(window)
     _check("out", out, (N, T, H, D), q.dtype)
     _check("lse", lse, (N, T, H), torch.float32)
-    _on_gpu(q, k, v, cu_seqlens, out, lse)
-    _dev(cu_seqlens, out, lse)
-    given = out, lse
+    _check("rest", rest, (N, T, H, D), torch.bfloat16)
+    _on_gpu(q, k, v, cu_seqlens, out, lse, rest)
+    _dev(cu_seqlens, out, lse, rest)
+    given = out, lse, rest
     if out is None:
         out = torch.empty((N, T, H, D), dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
         lse = torch.empty((N, T, H), dtype=torch.float32, device=q.device)
-    _call("kla_attn_fwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(out), _ptr(lse), _scale(scale, q), int(window), _ptr(cu_seqlens), cu_hp,
-          n_seq, N, T, H, Hk, D, dt, _stream(), KLA_ATTN_CAUSAL if causal else 0)
+    _call("kla_attn_fwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(out), _ptr(lse), _ptr(rest), _scale(scale, q), int(window), _ptr(cu_seqlens),
+          cu_hp, n_seq, N, T, H, Hk, D, dt, _stream(), KLA_ATTN_CAUSAL if causal else 0)
     _written(*given)
     return out, lse
 
 
-def kla_attn_bwd(q, k, v, o, lse, d_o, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, workspace=None):
-    """Backward of kla_attn_fwd, from what it returned: a dict of dq, dk, dv."""
+def kla_attn_bwd(q, k, v, o, lse, d_o, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, workspace=None, rest=None):
+    """Backward of kla_attn_fwd, from what it returned (and left in rest): a dict of dq, dk, dv."""
     for name, t in (("o", o), ("lse", lse), ("d_o", d_o)):
         if t is None:
             raise ValueError("%s is required" % name)
@@ -89,12 +91,13 @@ def kla_attn_bwd(q, k, v, o, lse, d_o, scale=None, causal=True, window=0, cu_seq
     _check("o", o, (N, T, H, D), q.dtype)
     _check("d_o", d_o, (N, T, H, D), q.dtype)
     _check("lse", lse, (N, T, H), torch.float32)
-    _on_gpu(q, k, v, o, lse, d_o, cu_seqlens, workspace)
-    _dev(o, lse, d_o, cu_seqlens, workspace)
+    _check("rest", rest, (N, T, H, D), torch.bfloat16)
+    _on_gpu(q, k, v, o, lse, d_o, cu_seqlens, workspace, rest)
+    _dev(o, lse, d_o, cu_seqlens, workspace, rest)
     if workspace is None:
         workspace = _workspace(int(lib().kla_attn_bwd_workspace_bytes(N, T, H, Hk, D, cu_hp, n_seq, dt)), q)
     g = {name: torch.empty(t.shape, dtype=t.dtype, device=t.device) for name, t in (("dq", q), ("dk", k), ("dv", v))}
-    _call("kla_attn_bwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(o), _ptr(lse), _ptr(d_o), *(_ptr(t) for t in g.values()),
+    _call("kla_attn_bwd", _ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], _ptr(o), _ptr(lse), _ptr(rest), _ptr(d_o), *(_ptr(t) for t in g.values()),
           _scale(scale, q), int(window), _ptr(cu_seqlens), cu_hp, n_seq, N, T, H, Hk, D, dt, _ptr(workspace), _ws_bytes(workspace), _stream(),
           KLA_ATTN_CAUSAL if causal else 0)
     return g
@@ -105,20 +108,23 @@ class _Attn(torch.autograd.Function):
     def forward(ctx, q, k, v, scale, causal, window, cu_seqlens, cu_seqlens_host):
         ctx.offsets = _Offsets(cu_seqlens, cu_seqlens_host)
         wanted = any(ctx.needs_input_grad)
-        o, lse = kla_attn_fwd(q, k, v, scale, causal, window, cu_seqlens, cu_seqlens_host, want_lse=wanted)
-        ctx.save_for_backward(q, k, v, o, lse)
+        rest = torch.empty(q.shape, dtype=q.dtype, device=q.device) if wanted and q.dtype == torch.bfloat16 else None
+        o, lse = kla_attn_fwd(q, k, v, scale, causal, window, cu_seqlens, cu_seqlens_host, want_lse=wanted, rest=rest)
+        ctx.save_for_backward(q, k, v, o, lse, rest)
         ctx.misc = (scale, causal, window)
         return o
 
     @staticmethod
     def backward(ctx, d_o):
         _no_second("kla_attn")
-        g = kla_attn_bwd(*ctx.saved_tensors, d_o.contiguous(), *ctx.misc, **ctx.offsets.check())
+        *saved, rest = ctx.saved_tensors
+        g = kla_attn_bwd(*saved, d_o.contiguous(), *ctx.misc, rest=rest, **ctx.offsets.check())
         return (*g.values(), None, None, None, None, None)
 
 
 def kla_attn(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None):
-    """Differentiable kla_attn_fwd: o, gradients with respect to q, k and v.  The graph holds q, k, v, o and the rows' lse."""
+    """Differentiable kla_attn_fwd: o, gradients with respect to q, k and v.  The graph holds q, k, v, o, the rows' lse and, in bfloat16, what o's
+    rounding leaves out."""
     host = _host(cu_seqlens, cu_seqlens_host)
     if _eager():
         r = _native("attn_train", "kla_attn_fwd", q, k, v, _scale(scale, q), bool(causal), window, cu_seqlens, host)

@@ -261,7 +261,7 @@ __device__ __forceinline__ bool find_rows(const Seqs& s, int G, int rows, long p
 // ---- launchers --------------------------------------------------------------------------------------------------------------------
 template <typename T> struct AttnArgs {
     const T* q; long ld_q; const T* k; long ld_k; const T* v; long ld_v;                  // rows of new tokens
-    T* o; float* lse;                                    // lse: or NULL
+    T* o; float* lse; T* rest;                           // lse, rest: or NULL; rest: what o's rounding leaves out
     Seqs seqs; int H, Hk, G;
     float scale; int window; bool causal;
     // the cache of earlier tokens: pages [n_pages][Hk][1 << page_shift][D]; table [n_seq][max_pages], rows ld_table apart
@@ -275,7 +275,7 @@ template <typename T> struct AttnArgs {
 // Backward: d_o, dq like o, dk, dv [tokens][Hk][D]; row_lse, row_delta [tokens][H]: the rows' lse (base 2) and <d_o, o>; part_dk, part_dv
 // [parts][tokens][Hk][D] where the query rows of a tile of keys are taken in `parts` parts.
 template <typename T> struct AttnBwdArgs {
-    AttnArgs<T> f;                                       // (o, lse: the forward's; tiles, per, unit0: of a launch)
+    AttnArgs<T> f;                                       // (o, lse, rest: the forward's; tiles, per, unit0: of a launch)
     const T* d_o; T* dq; T* dk; T* dv;
     float* row_lse; float* row_delta;
     int parts; float* part_dk; float* part_dv;

@@ -150,7 +150,7 @@ ExtendWork extend_work(char* base, const kla::AttnPlan& p, long M, int H, int D)
 
 extern "C" {
 
-int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* o, float* lse, float scale, int window,
+int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, void* o, float* lse, void* rest, float scale, int window,
                  const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int n_seq, int N, int T, int H, int Hk, int D, kla_dtype dt, void* hip_stream,
                  unsigned opts)
 {
@@ -162,10 +162,13 @@ int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void*
     if (const int e = take_seqs(cu_seqlens_dev, cu_seqlens_host, n_seq, N, T, &s, &M)) return e;
     if (M > 0 && (!q || !k || !v || !o)) return KLA_ERR_NULL;
     if (M > 0 && (o == q || o == k || o == v)) return KLA_ERR_SHAPE;                   // (other workgroups still read them)
-    if (!aligned(16, {q, k, v, o}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
+    if (rest && dt != KLA_BF16) return KLA_ERR_DTYPE;
+    if (rest && (rest == q || rest == k || rest == v || rest == o)) return KLA_ERR_SHAPE;
+    if (!aligned(16, {q, k, v, o, rest}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
     const kla::AttnPlan p = attn_plan(s, cu_seqlens_host, H / Hk, Hk, D);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
+        a.rest = static_cast<decltype(a.rest)>(rest);
         a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);
         return status(kla::launch_attn_fwd(a, D, p, false, st));
     };
@@ -182,7 +185,7 @@ size_t kla_attn_bwd_workspace_bytes(int N, int T, int H, int Hk, int D, const in
     return bwd_work(nullptr, attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk), M, z).bytes;
 }
 
-int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, const void* o, const float* lse, const void* d_o, void* dq,
+int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void* v, long ld_v, const void* o, const float* lse, const void* rest, const void* d_o, void* dq,
                  void* dk, void* dv, float scale, int window, const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, int n_seq, int N, int T, int H,
                  int Hk, int D, kla_dtype dt, void* workspace, size_t workspace_bytes, void* hip_stream, unsigned opts)
 {
@@ -195,9 +198,10 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
     if (M > 0 && (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv)) return KLA_ERR_NULL;
     if (M > 0)
         for (const void* out : {dq, dk, dv})
-            for (const void* in : {q, k, v, o, d_o}) if (out == in) return KLA_ERR_SHAPE;
+            for (const void* in : {q, k, v, o, rest, d_o}) if (out == in) return KLA_ERR_SHAPE;
     if (M > 0 && (dq == dk || dq == dv || dk == dv)) return KLA_ERR_SHAPE;
-    if (!aligned(16, {q, k, v, o, d_o, dq, dk, dv}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
+    if (rest && dt != KLA_BF16) return KLA_ERR_DTYPE;
+    if (!aligned(16, {q, k, v, o, rest, d_o, dq, dk, dv}) || !aligned(4, {lse})) return KLA_ERR_ALIGN;
     const int parts = attn_bwd_parts(s, cu_seqlens_host, H / Hk, Hk);
     const BwdWork w = bwd_work(static_cast<char*>(workspace), parts, M, z);
     if (const int e = take_workspace(workspace, workspace_bytes, w.bytes)) return e;
@@ -207,6 +211,7 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
         using E = std::remove_pointer_t<Q>;
         kla::AttnBwdArgs<E> b = {};
         b.f = a;
+        b.f.rest = static_cast<Q>(const_cast<void*>(rest));
         b.d_o = static_cast<const E*>(d_o); b.dq = static_cast<Q>(dq); b.dk = static_cast<Q>(dk); b.dv = static_cast<Q>(dv);
         b.row_lse = w.row_lse; b.row_delta = w.row_delta; b.parts = parts; b.part_dk = w.part_dk; b.part_dv = w.part_dv;
         b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 128, &b.f.per);

@@ -71,20 +71,20 @@ struct Attn : Heads {
         opts = causal == Py_True ? KLA_ATTN_CAUSAL : 0;
         return true;
     }
-    void fwd(at::Tensor& o, at::Tensor& lse, bool want_lse) const
+    void fwd(at::Tensor& o, at::Tensor& lse, bool want_lse, const at::Tensor& rest = at::Tensor()) const
     {
         if (!o.defined()) o = fresh(*q, q->sizes(), type);
         if (!lse.defined() && want_lse) lse = fresh(*q, {N, T, H}, at::kFloat);
-        check(api.fwd(ptr(q), ld_q, ptr(k), ld_k, ptr(v), ld_v, at_of(o), f_of(lse), scale, window, cu.device(), cu.host, cu.n_seq, (int)N, (int)T, (int)H,
-                      (int)Hk, (int)D, dt, stream(), opts));
+        check(api.fwd(ptr(q), ld_q, ptr(k), ld_k, ptr(v), ld_v, at_of(o), f_of(lse), at_of(rest), scale, window, cu.device(), cu.host, cu.n_seq, (int)N, (int)T,
+                      (int)H, (int)Hk, (int)D, dt, stream(), opts));
     }
-    void bwd(const at::Tensor& o, const at::Tensor& lse, const at::Tensor& d_o, at::Tensor (&g)[3]) const
+    void bwd(const at::Tensor& o, const at::Tensor& lse, const at::Tensor* rest, const at::Tensor& d_o, at::Tensor (&g)[3]) const
     {
         const at::Tensor ws = bytes(*q, api.bwd_bytes((int)N, (int)T, (int)H, (int)Hk, (int)D, cu.host, cu.n_seq, dt));
         g[0] = fresh(*q, q->sizes(), type);
         g[1] = fresh(*k, k->sizes(), type);
         g[2] = fresh(*v, v->sizes(), type);
-        check(api.bwd(ptr(q), ld_q, ptr(k), ld_k, ptr(v), ld_v, o.data_ptr(), f_of(lse), d_o.data_ptr(), at_of(g[0]), at_of(g[1]), at_of(g[2]), scale, window,
+        check(api.bwd(ptr(q), ld_q, ptr(k), ld_k, ptr(v), ld_v, o.data_ptr(), f_of(lse), ptr(rest), d_o.data_ptr(), at_of(g[0]), at_of(g[1]), at_of(g[2]), scale, window,
                       cu.device(), cu.host, cu.n_seq, (int)N, (int)T, (int)H, (int)Hk, (int)D, dt, at_of(ws), size_of(ws), stream(), opts));
     }
 };
@@ -93,9 +93,10 @@ struct AttnNode : public torch::autograd::Function<AttnNode> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v,
                                                   const Attn* c, const at::Tensor* host)
     {
-        at::Tensor o, lse;
-        c->fwd(o, lse, true);
-        ctx->save_for_backward({q, k, v, o, lse});
+        at::Tensor o, lse, rest;
+        if (c->dt == KLA_BF16) rest = fresh(q, q.sizes(), c->type);
+        c->fwd(o, lse, true, rest);
+        ctx->save_for_backward({q, k, v, o, lse, rest});
         ctx->saved_data["scale"] = (double)c->scale;
         ctx->saved_data["window"] = (int64_t)c->window;
         ctx->saved_data["opts"] = (int64_t)c->opts;
@@ -113,29 +114,29 @@ struct AttnNode : public torch::autograd::Function<AttnNode> {
         c.scale = (float)ctx->saved_data["scale"].toDouble();
         c.window = (int)ctx->saved_data["window"].toInt();
         c.opts = (unsigned)ctx->saved_data["opts"].toInt();
-        const at::Tensor *o = gpu(s[3], c.type, c.q->sizes()), *lse = gpu(s[4], at::kFloat, {c.N, c.T, c.H});
-        taken(o && lse && together({o, lse}), "kla_attn");
+        const at::Tensor *o = gpu(s[3], c.type, c.q->sizes()), *lse = gpu(s[4], at::kFloat, {c.N, c.T, c.H}), *rest;
+        taken(o && lse && gpu_or_none(s[5], at::kBFloat16, c.q->sizes(), &rest) && together({o, lse, rest}), "kla_attn");
         if (!grads[0].defined()) return {at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
-        refused("kla_attn_bwd", [&] { c.bwd(*o, *lse, grads[0].contiguous(), g); });
+        refused("kla_attn_bwd", [&] { c.bwd(*o, *lse, rest, grads[0].contiguous(), g); });
         return {g[0], g[1], g[2], at::Tensor(), at::Tensor()};
     }
 };
 
-// attn_fwd(q, k, v, scale, causal, window, cu, cu_host, want_lse, out, lse) -> (o, lse)
+// attn_fwd(q, k, v, scale, causal, window, cu, cu_host, want_lse, out, lse, rest) -> (o, lse)
 PyObject* attn_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     Attn c;
-    const at::Tensor *out, *lse;
-    if (n != 11 || !api.fwd || !c.take(a[0], a[1], a[2], a[6], a[7]) || !c.options(a[3], a[4], a[5]) || !gpu_or_none(a[9], c.type, c.q->sizes(), &out) ||
-        !gpu_or_none(a[10], at::kFloat, {c.N, c.T, c.H}, &lse) || !together({out, lse}))
+    const at::Tensor *out, *lse, *rest;
+    if (n != 12 || !api.fwd || !c.take(a[0], a[1], a[2], a[6], a[7]) || !c.options(a[3], a[4], a[5]) || !gpu_or_none(a[9], c.type, c.q->sizes(), &out) ||
+        !gpu_or_none(a[10], at::kFloat, {c.N, c.T, c.H}, &lse) || !gpu_or_none(a[11], at::kBFloat16, c.q->sizes(), &rest) || !together({out, lse, rest}))
         Py_RETURN_NONE;
     at::Tensor o = value(out), l = value(lse);
     try {
         const NoGil no_gil;
-        c.fwd(o, l, a[8] == Py_True);
+        c.fwd(o, l, a[8] == Py_True, value(rest));
     } catch (const Refused& e) { return PyLong_FromLong(e.code); }
-    written({out, lse});
+    written({out, lse, rest});
     return pair(o, l);
     END_HANDLE_TH_ERRORS
 }

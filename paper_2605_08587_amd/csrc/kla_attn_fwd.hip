@@ -196,7 +196,17 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
     {
         const Floats<4> x = {{x0, x1, x2, x3}};
         if (parts > 1) store_vec<float, 4>(a.part_o + ((long)split * a.M * a.H + row) * D + d, x);
-        else store_vec<T, 4>(a.o + row * D + d, x);
+        else {
+            store_vec<T, 4>(a.o + row * D + d, x);
+            if constexpr (sizeof(T) == 2 && !PAGED) {
+                if (a.rest) {
+                    Floats<4> y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y.v[e] = x.v[e] - to_float(rounded<T>(x.v[e]));
+                    store_vec<T, 4>(a.rest + row * D + d, y);
+                }
+            }
+        }
     }
     // l = 0: scores that are all -inf, whose quotient is a NaN, or no key of a part that this row sees
     static __device__ __forceinline__ float inverse(int parts, float l) { return parts > 1 && l == 0.f ? 0.f : 1.f / l; }

@@ -34,7 +34,7 @@ def within(name, x, ref, bound):
         name, abs(x - ref).flat[over.argmax()], np.unravel_index(over.argmax(), x.shape), bound.flat[over.argmax()])
 
 
-def check(lengths, q, k, v, o, lse, scale, causal, window, d_o=None, grads=None, tag=""):
+def check(lengths, q, k, v, o, lse, scale, causal, window, d_o=None, grads=None, tag="", rest=False):
     """Flattened tokens [M, heads, D] of sequences of these lengths, against the oracle."""
     u, at = U[q.dtype], 0
     for n in lengths:
@@ -43,7 +43,7 @@ def check(lengths, q, k, v, o, lse, scale, causal, window, d_o=None, grads=None,
         kw = dict(causal=causal, window=window)
         ro, rl = ao.forward(*a, scale, **kw)
         g = None if d_o is None else f64(d_o[here])
-        b = ao.bounds(*a, scale, u, d_o=g, **kw)
+        b = ao.bounds(*a, scale, u, d_o=g, rest=rest, **kw)
         within(tag + " o", o[here], ro, b[0])
         within(tag + " lse", lse[here], rl, b[1])
         if g is not None:

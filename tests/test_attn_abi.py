@@ -30,11 +30,11 @@ WS = dict(ws=0x100000, ws_bytes=1 << 40)
 
 
 def fwd(**o):
-    return _call("kla_attn_fwd", dict(**IN, o=0x4000, lse=None, scale=0.125, window=0, **SEQS, **SIZES, dt=BF16, stream=None, opts=1), o)
+    return _call("kla_attn_fwd", dict(**IN, o=0x4000, lse=None, rest=None, scale=0.125, window=0, **SEQS, **SIZES, dt=BF16, stream=None, opts=1), o)
 
 
 def bwd(**o):
-    return _call("kla_attn_bwd", dict(**IN, o=0x4000, lse=0x5000, do=0x6000, dq=0x7000, dk=0x8000, dv=0x9000, scale=0.125, window=0, **SEQS, **SIZES, dt=BF16,
+    return _call("kla_attn_bwd", dict(**IN, o=0x4000, lse=0x5000, rest=None, do=0x6000, dq=0x7000, dk=0x8000, dv=0x9000, scale=0.125, window=0, **SEQS, **SIZES, dt=BF16,
                                       **WS, stream=None, opts=1), o)
 
 
@@ -117,6 +117,15 @@ def test_outputs_apart_from_inputs():
         for c in ("kc", "vc"):
             for p in (0x1000, 0x2000, 0x3000, 0x4000):
                 assert f(**{c: p}) == E_SHAPE
+
+
+def test_remainder():
+    for f in (fwd, bwd):
+        assert f(rest=0xb000, dt=F32) == E_DTYPE and f(rest=0xb008) == E_ALIGN
+    for p in (0x1000, 0x2000, 0x3000, 0x4000):
+        assert fwd(rest=p) == E_SHAPE
+    for out in ("dq", "dk", "dv"):
+        assert bwd(rest=0xb000, **{out: 0xb000}) == E_SHAPE
 
 
 def test_workspace():

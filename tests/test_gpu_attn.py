@@ -32,12 +32,15 @@ def _run(kla, dtype, lead, H, Hk, D, causal=True, window=0, lengths=None, wide=F
     kw = dict(scale=scale, causal=causal, window=window)
     if cu is not None:
         kw.update(cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
-    o, lse = kla.kla_attn_fwd(q, k, v, **kw)
-    g = kla.kla_attn_bwd(q, k, v, o, lse, d_o, **kw)
-    torch.cuda.synchronize()
     flat = lambda t: t.flatten(0, 1)
-    check([lead[1]] * lead[0] if lengths is None else lengths, flat(q), flat(k), flat(v), flat(o), flat(lse), D ** -0.5 if scale is None else scale,
-          causal, window, flat(d_o), [flat(g[x]) for x in ("dq", "dk", "dv")])
+    for rest in (None,) + ((torch.full_like(d_o, float("nan")),) if dtype == torch.bfloat16 else ()):
+        o, lse = kla.kla_attn_fwd(q, k, v, rest=rest, **kw)
+        g = kla.kla_attn_bwd(q, k, v, o, lse, d_o, rest=rest, **kw)
+        torch.cuda.synchronize()
+        check([lead[1]] * lead[0] if lengths is None else lengths, flat(q), flat(k), flat(v), flat(o), flat(lse), D ** -0.5 if scale is None else scale,
+              causal, window, flat(d_o), [flat(g[x]) for x in ("dq", "dk", "dv")], rest=rest is not None)
+        if rest is not None and rest.numel():                # half a step of o at most, and no less than what was left out
+            assert (rest.double().abs() <= 2.0 ** -8 * o.double().abs() + 1e-30).all()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -89,6 +92,22 @@ def test_scores_far_apart(kla):
     k = k * torch.linspace(0.01, 2, 400, device="cuda")[None, :, None, None]
     o, lse = kla.kla_attn_fwd(q, k, v)
     check([400], q[0], k[0], v[0], o[0], lse[0], 0.125, True, 0)
+
+
+def test_remainder(kla):
+    """o and rest together are o before its rounding: what the other rounding of the way, of the weights, leaves is within its own bound."""
+    q, k, v, _ = _inputs(20, torch.bfloat16, (1, 150), 4, 2, 64)
+    rest = torch.empty_like(q)
+    o, _lse = kla.kla_attn_fwd(q, k, v, rest=rest)
+    a = [f64(t[0]) for t in (q, k, v)]
+    ref, bound = ao.forward(*a, 0.125)[0], ao.bounds(*a, 0.125, 2.0 ** -8)[0]
+    both = f64(o[0]) + f64(rest[0])
+    assert (abs(both - ref) <= bound - (2.0 ** -8 - 2.0 ** -16) * abs(ref)).all()
+    assert np.linalg.norm(both - ref) < 0.85 * np.linalg.norm(f64(o[0]) - ref)
+    with pytest.raises(kla.KlaError, match="DTYPE"):
+        kla.kla_attn_fwd(q.float(), k.float(), v.float(), rest=rest)
+    with pytest.raises(TypeError, match="rest"):
+        kla.kla_attn_fwd(q, k, v, rest=rest.float())
 
 
 NAN, INF = float("nan"), float("inf")
@@ -181,8 +200,9 @@ def test_autograd(kla, monkeypatch, native):
     q, k, v, d_o = _inputs(14, torch.bfloat16, (1, 260), 8, 2, 64, wide=True)
     cu = offsets([100, 0, 160])
     kw = dict(window=50, scale=0.2, cu_seqlens=cu.cuda(), cu_seqlens_host=cu)
-    o, lse = kla.kla_attn_fwd(q, k, v, **kw)
-    g = kla.kla_attn_bwd(q, k, v, o, lse, d_o, **kw)
+    rest = torch.empty_like(d_o)
+    o, lse = kla.kla_attn_fwd(q, k, v, rest=rest, **kw)
+    g = kla.kla_attn_bwd(q, k, v, o, lse, d_o, rest=rest, **kw)
     leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
     y = kla.kla_attn(*leaves, **kw)
     assert torch.equal(bits(y.detach()), bits(o))
