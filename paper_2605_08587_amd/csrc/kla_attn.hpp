@@ -272,7 +272,7 @@ template <typename T> struct AttnArgs {
     long tiles, per;                                     // tiles of query rows of a key head: in all; of one sequence (fixed lengths)
     long unit0;                                          // first workgroup of this launch
 };
-// Backward: d_o, dq like o, dk, dv [tokens][Hk][D]; row_lse, row_delta [tokens][H]: the rows' lse (base 2) and <d_o, o>; part_dk, part_dv
+// Backward: d_o, dq like o, dk, dv [tokens][Hk][D]; row_lse, row_delta [tokens][H]: the rows' lse (base 2) and -<d_o, o>; part_dk, part_dv
 // [parts][tokens][Hk][D] where the query rows of a tile of keys are taken in `parts` parts.
 template <typename T> struct AttnBwdArgs {
     AttnArgs<T> f;                                       // (o, lse, rest: the forward's; tiles, per, unit0: of a launch)

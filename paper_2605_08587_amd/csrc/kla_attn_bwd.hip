@@ -39,7 +39,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attn_rows_ke
 #pragma unroll
     for (int d = LANES / 2; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
     if (row < rows && l == 0) {
-        a.row_delta[row] = sum;
+        a.row_delta[row] = -sum;                         // (where the sums of dp begin)
         a.row_lse[row] = a.f.lse[row] * kLog2e;
     }
 }
@@ -141,7 +141,7 @@ template <typename T, int D> struct Dkv {
         for (int i = 0; i < 4; ++i) {
             const floatx4 d = *reinterpret_cast<const floatx4*>(vecs + 64 + 8 * i + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ds[4 * i + e] = -d[e];
+            for (int e = 0; e < 4; ++e) ds[4 * i + e] = d[e];
         }
 #pragma unroll
         for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(ds, Tile::row_slot(g, row_off, c), VL ? Tile::row_slot(key.rows, row_off, c) : key.v[VL ? 0 : c]);
@@ -287,14 +287,14 @@ template <typename T, int D, int RW> struct Dq {
         }
     }
 
-    struct Rows { u32x4 q[Tile::NC], g[Tile::NC]; int lo, hi; int lo_least, lo_most, hi_least, hi_most; float c, lse, delta; };
+    struct Rows { u32x4 q[Tile::NC], g[Tile::NC]; int lo, hi; int lo_least, lo_most, hi_least, hi_most; float c, lse; floatx16 delta; };
 
     template <bool CAREFUL>
     static __device__ __forceinline__ void block(const Rows& r, floatx16 (&dq)[NDT], const char* k, const char* v, int j0, int last, int row_off, int col_off, int h)
     {
-        floatx16 s, ds;
+        floatx16 s, ds = r.delta;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) { s[e] = 0.f; ds[e] = -r.delta; }
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
         for (int c = 0; c < Tile::NC; ++c) mma32x32<T>(s, Tile::row_slot(k, row_off, c), r.q[c]);
 #pragma unroll
@@ -377,7 +377,7 @@ template <typename T, int D, int RW> struct Dq {
         Rows r;
         r.c = a.f.scale * kLog2e;
         r.lse = a.row_lse[to];
-        r.delta = a.row_delta[to];
+        float delta = a.row_delta[to];
         {
             const char* q = reinterpret_cast<const char*>(a.f.q + (p.tok0 + t) * a.f.ld_q + (long)(p.hk * G + (row - t * G)) * D);
             const char* g = reinterpret_cast<const char*>(a.d_o + to * D);
@@ -387,7 +387,9 @@ template <typename T, int D, int RW> struct Dq {
 #pragma unroll
         for (int c = 0; c < Tile::NC; ++c) { settle(r.q[c]); settle(r.g[c]); }
         settle(r.lse);
-        settle(r.delta);
+        settle(delta);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) r.delta[e] = delta;
         const int u0 = min(w0, p.rows - 1) / G, u1 = min(w0 + 31, p.rows - 1) / G;
         r.lo = lo_of(t); r.lo_least = lo_of(u0); r.lo_most = lo_of(u1);
         r.hi = hi_of(t); r.hi_least = hi_of(u0); r.hi_most = w0 >= p.rows ? -1 : hi_of(u1);
