@@ -222,40 +222,43 @@ __device__ __forceinline__ float halves_sum(float x)
 }
 
 // ---- rows of a batch --------------------------------------------------------------------------------------------------------------
-// The query heads of one key head are rows of their own: row r of (sequence, key head) is token r / G, head hk G + r % G.  A key head's tiles of
-// `rows` rows (packed batches: tile `idx` counted over the sequences in order); false: there is none.
+// The query heads of one key head are rows of their own: row r of (sequence, key head) is token r / G, head hk G + r % G, and a key head's rows are taken in
+// tiles of ROWS.  Fixed lengths: tiles of one number of all sequences beside each other, `per` for each sequence.  Packed: tile k of sequence n
+// has the place floor(cu[n] G / ROWS) + n + k, which nothing has to count (some places stay empty); a wave looks at 64 sequences at once.  false: an empty place.
 struct RowPlace { int n; int tile; int len; long tok0; };
-__device__ __forceinline__ bool find_rows(const Seqs& s, int G, int rows, long per, long idx, int lane, RowPlace* p)
+template <int ROWS> __device__ __forceinline__ bool find_rows(const Seqs& s, int G, long per, long idx, int lane, RowPlace* p)
 {
-    if (!s.cu) {                                         // tiles of one number of all sequences beside each other
+    if (!s.cu) {
         p->n = (int)(idx % s.n_seq);
         p->tile = (int)(idx / s.n_seq);
         p->len = s.T;
         p->tok0 = (long)p->n * s.T;
         return p->tile < per;
     }
-    for (int base = 0; base < s.n_seq; base += 64) {
-        const int n = min(base + lane, s.n_seq - 1);
-        const int c0 = s.cu[n], len = base + lane < s.n_seq ? s.cu[n + 1] - c0 : 0;
-        const int mine = (int)(((long)len * G + rows - 1) / rows);
-        int sum = mine;                                  // inclusive prefix sum over the lanes
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += o;
-        }
-        const unsigned long long here = __ballot(idx < sum);
-        if (here) {
-            const int l = __builtin_ctzll(here);
-            p->n = base + l;
-            p->tile = (int)idx - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(mine, l));
-            p->len = __builtin_amdgcn_readlane(len, l);
+    // the last sequence whose first place is at most idx (places grow with every sequence, and the first one's is 0)
+    int lo = 0, step = (s.n_seq + 63) / 64;
+    for (;;) {
+        const int n = (int)min(lo + (long)lane * step, (long)s.n_seq);                // (cu has n_seq + 1 entries)
+        const int c0 = s.cu[n];
+        const long first = (long)c0 * G / ROWS + n;
+        const int l = 63 - __builtin_clzll(__ballot(n < s.n_seq && first <= idx));
+        lo = __builtin_amdgcn_readlane(n, l);
+        if (step == 1) {
+            p->n = lo;
             p->tok0 = __builtin_amdgcn_readlane(c0, l);
-            return true;
+            break;
         }
-        idx -= __builtin_amdgcn_readlane(sum, 63);
+        step = (step + 63) / 64;
     }
-    return false;
+    p->len = s.cu[p->n + 1] - (int)p->tok0;
+    const long k = idx - (p->tok0 * G / ROWS + p->n);
+    p->tile = (int)k;
+    return k < ((long)p->len * G + ROWS - 1) / ROWS;
+}
+inline long row_places(const Seqs& s, long M, int G, int rows, long* per)
+{
+    *per = ((long)s.T * G + rows - 1) / rows;
+    return s.cu ? M * G / rows + s.n_seq : *per * s.n_seq;
 }
 
 // ---- launchers --------------------------------------------------------------------------------------------------------------------
@@ -269,7 +272,7 @@ template <typename T> struct AttnArgs {
     // keys in up to `splits` (at most 64) parts of at least `chunk` each (a multiple of 128): part_o [splits][tokens H][D] and part_lse [splits][tokens H] (base 2), where there are
     // several; part_count [tokens H]: how many there are
     int splits, chunk; float* part_o; float* part_lse; int* part_count; long M;
-    long tiles, per;                                     // tiles of query rows of a key head: in all; of one sequence (fixed lengths)
+    long tiles, per;                                     // places of tiles of query rows of a key head: in all; of one sequence (fixed lengths)
     long unit0;                                          // first workgroup of this launch
 };
 // Backward: d_o, dq like o, dk, dv [tokens][Hk][D]; row_lse, row_delta [tokens][H]: the rows' lse (base 2) and -<d_o, o>; part_dk, part_dv
@@ -280,7 +283,7 @@ template <typename T> struct AttnBwdArgs {
     float* row_lse; float* row_delta;
     int parts; float* part_dk; float* part_dv;
     bool beside;                                         // dk, dv and dq in one launch, rows of dq in tiles of 64 (else of 128: f.tiles)
-    long key_tiles, key_per;                             // tiles of 128 keys: in all; of one sequence (fixed lengths)
+    long key_tiles, key_per;                             // places of tiles of 128 keys: in all; of one sequence (fixed lengths)
 };
 template <typename T> hipError_t launch_attn_bwd(const AttnBwdArgs<T>& a, int D, hipStream_t st);
 

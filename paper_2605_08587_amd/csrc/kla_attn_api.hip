@@ -30,16 +30,15 @@ int attn_check(const AttnSizes& z, long ld_q, long ld_k, long ld_v, float scale,
 {
     if (const int e = attn_sizes(z, dt)) return e;
     if (ld_q < (long)z.H * z.D || ld_k < (long)z.Hk * z.D || ld_v < (long)z.Hk * z.D || ld_q > kMaxAttnStride || ld_k > kMaxAttnStride || ld_v > kMaxAttnStride ||
-        !(scale > 0.f) || isinf(scale) || window < 0)
+        !(scale > 0.f) || isinf(scale * kla::kLog2e) || window < 0)
         return KLA_ERR_SHAPE;
     const long vec = 16 / (long)elem_bytes(dt);
     return ld_q % vec || ld_k % vec || ld_v % vec ? KLA_ERR_ALIGN : KLA_OK;
 }
 // Tiles of `rows` query rows of one key head
-long attn_tiles(const kla::Seqs& s, const int32_t* cu_host, int G, int rows, long* per)
+long attn_tiles(const kla::Seqs& s, const int32_t* cu_host, int G, int rows)
 {
-    *per = ((long)s.T * G + rows - 1) / rows;
-    if (!s.cu) return *per * s.n_seq;
+    if (!s.cu) return ((long)s.T * G + rows - 1) / rows * s.n_seq;
     long tiles = 0;
     for (int i = 0; i < s.n_seq; ++i) tiles += ((long)(cu_host[i + 1] - cu_host[i]) * G + rows - 1) / rows;
     return tiles;
@@ -55,8 +54,7 @@ int longest(const kla::Seqs& s, const int32_t* cu_host)
 // for the CUs; then four waves share 32 rows and divide the keys.
 kla::AttnPlan attn_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk, int D)
 {
-    long per;
-    const long units = attn_tiles(s, cu_host, G, 128, &per) * Hk;
+    const long units = attn_tiles(s, cu_host, G, 128) * Hk;
     return {units >= (D == 64 ? 320 : 256) ? 128 : 32, 1, 128};
 }
 // New tokens over a cache: a row sees up to `span` keys.
@@ -65,12 +63,12 @@ kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int
     kla::AttnPlan p = {128, 1, 128};
     const int most_new = longest(s, cu_host);
     const long span = window && window + (long)most_new < max_len ? window + most_new : max_len;
-    long per, units = attn_tiles(s, cu_host, G, 128, &per) * Hk;
+    long units = attn_tiles(s, cu_host, G, 128) * Hk;
     // Rows in tiles of 32 with their keys divided among the waves, too, where larger tiles in parts of 256 keys would leave CUs idle (fp32, three
     // sequences of 54 to 160 new tokens over 115 to 852, 8 heads over 2 of 64: 31 us a call in tiles of 128, 20 of 32; bf16, 16 tokens over 1000 17 and 12 us).
     if ((long)most_new * G <= 32 || units * ((span + 255) / 256) < 256) {
         p.rows = 32;
-        units = attn_tiles(s, cu_host, G, 32, &per) * Hk;
+        units = attn_tiles(s, cu_host, G, 32) * Hk;
     }
     if (units == 0) return p;
     // Single tokens and drafts: a workgroup takes about 3 us until its first keys are there, one after the other on a CU (its tiles take all of the LDS), so
@@ -111,8 +109,7 @@ constexpr long kAttnBeside = 512;
 // than they even out: bf16, D = 128, 4096 tokens, 8 heads, 3 sequences 399 us whole, 471 in two parts.)
 int attn_bwd_parts(const kla::Seqs& s, const int32_t* cu_host, int G, int Hk)
 {
-    long per;
-    const long units = attn_tiles(s, cu_host, 1, 128, &per) * Hk;
+    const long units = attn_tiles(s, cu_host, 1, 128) * Hk;
     if (units == 0 || units >= 512) return 1;
     const long want = (512 + units - 1) / units, most = ((long)longest(s, cu_host) * G + 255) / 256;
     const long parts = want < most ? want : most;
@@ -169,7 +166,7 @@ int kla_attn_fwd(const void* q, long ld_q, const void* k, long ld_k, const void*
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     auto run = [&](auto a) {
         a.rest = static_cast<decltype(a.rest)>(rest);
-        a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);
+        a.tiles = kla::row_places(s, M, a.G, p.rows, &a.per);
         return status(kla::launch_attn_fwd(a, D, p, false, st));
     };
     return dt == KLA_BF16 ? run(attn_args<bf16_t>(q, ld_q, k, ld_k, v, ld_v, o, lse, s, M, z, scale, window, opts))
@@ -214,10 +211,9 @@ int kla_attn_bwd(const void* q, long ld_q, const void* k, long ld_k, const void*
         b.f.rest = static_cast<Q>(const_cast<void*>(rest));
         b.d_o = static_cast<const E*>(d_o); b.dq = static_cast<Q>(dq); b.dk = static_cast<Q>(dk); b.dv = static_cast<Q>(dv);
         b.row_lse = w.row_lse; b.row_delta = w.row_delta; b.parts = parts; b.part_dk = w.part_dk; b.part_dv = w.part_dv;
-        b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 128, &b.f.per);
-        b.beside = b.f.tiles * Hk < kAttnBeside;
-        if (b.beside) b.f.tiles = attn_tiles(s, cu_seqlens_host, a.G, 64, &b.f.per);
-        b.key_tiles = attn_tiles(s, cu_seqlens_host, 1, 128, &b.key_per);
+        b.beside = attn_tiles(s, cu_seqlens_host, a.G, 128) * Hk < kAttnBeside;
+        b.f.tiles = kla::row_places(s, M, a.G, b.beside ? 64 : 128, &b.f.per);
+        b.key_tiles = kla::row_places(s, M, 1, 128, &b.key_per);
         return status(kla::launch_attn_bwd(b, D, st));
     };
     void* out = const_cast<void*>(o);
@@ -261,7 +257,7 @@ int kla_attn_extend(const void* q, long ld_q, const void* k, long ld_k, const vo
         a.k_cache = static_cast<decltype(a.k_cache)>(k_cache); a.v_cache = static_cast<decltype(a.v_cache)>(v_cache);
         a.table = page_table; a.ld_table = ld_table; a.cached = cached; a.n_pages = n_pages; a.page_shift = shift; a.max_pages = max_pages;
         a.splits = p.splits; a.chunk = p.chunk; a.part_o = w.part_o; a.part_lse = w.part_lse; a.part_count = w.part_count;
-        a.tiles = attn_tiles(s, cu_seqlens_host, a.G, p.rows, &a.per);
+        a.tiles = kla::row_places(s, M, a.G, p.rows, &a.per);
         if (const hipError_t e = kla::launch_attn_fwd(a, D, p, true, st)) return status(e);
         return p.splits > 1 ? status(kla::launch_attn_join(a, D, st)) : (int)KLA_OK;
     };

@@ -202,7 +202,7 @@ template <typename T, int D> struct Dkv {
         Place p;
         p.hk = (int)(unit / a.parts % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, 1, 128, a.key_per, unit / a.parts / a.f.Hk, lane, &at)) return true;
+        if (!find_rows<128>(a.f.seqs, 1, a.key_per, unit / a.parts / a.f.Hk, lane, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int k0 = at.tile * 128, G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : 0;
         // the rows that see key j: lo .. hi - 1
@@ -365,7 +365,7 @@ template <typename T, int D, int RW> struct Dq {
         Place p;
         p.hk = (int)(unit % a.f.Hk);
         RowPlace at;
-        if (!find_rows(a.f.seqs, a.f.G, 32 * RW, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, lane, &at)) return true;
+        if (!find_rows<32 * RW>(a.f.seqs, a.f.G, a.f.per, a.f.tiles - 1 - unit / a.f.Hk, lane, &at)) return true;
         p.len = at.len; p.tok0 = at.tok0; p.rows = at.len * a.f.G;
         const int G = a.f.G, window = a.f.window ? min(a.f.window, p.len) : p.len;
         const int row0 = at.tile * 32 * RW, t_first = row0 / G, t_last = min(row0 + 32 * RW - 1, p.rows - 1) / G;

@@ -234,7 +234,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         Keys k;
         k.hk = (int)(unit / a.splits % a.Hk);
         RowPlace at;
-        if (!find_rows(a.seqs, a.G, 32 * RW, a.per, a.tiles - 1 - unit / a.splits / a.Hk, lane, &at)) return true;
+        if (!find_rows<32 * RW>(a.seqs, a.G, a.per, a.tiles - 1 - unit / a.splits / a.Hk, lane, &at)) return true;
         k.n = at.n; k.tok0 = at.tok0;
         k.cached = 0;
         if constexpr (PAGED) k.cached = (int)min((long)max(a.cached[at.n], 0), (long)a.max_pages << a.page_shift);

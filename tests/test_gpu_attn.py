@@ -72,6 +72,29 @@ def test_packed(kla, dtype, lengths, H, Hk, D, kw):
     _run(kla, dtype, (1, sum(lengths)), H, Hk, D, lengths=lengths, wide=True, seed=len(lengths), **kw)
 
 
+def test_thousands_of_sequences(kla):
+    """More than 64 x 64 sequences, most of them empty: a tile's sequence is looked for in three steps."""
+    lengths = [0, 1, 0, 0, 2, 0, 0, 0, 0, 1] * 600
+    _run(kla, torch.float32, (1, sum(lengths)), 2, 1, 64, lengths=lengths, seed=19)
+
+
+def test_the_largest_strides(kla):
+    """Tokens 2^24 elements apart, which a tile counts from its first in 32 bits."""
+    g = torch.Generator(device="cuda").manual_seed(21)
+    w = torch.empty(1, 70, 1 << 24, device="cuda")
+    q, k, v = (randn(g, 1, 70, h, 64) for h in (2, 1, 1))
+    far = [w[..., a:a + t.shape[2] * 64].unflatten(-1, (-1, 64)) for a, t in ((0, q), (512, k), ((1 << 24) - 64, v))]
+    for f, t in zip(far, (q, k, v)):
+        f.copy_(t)
+    for lead in (slice(None), slice(0, 1)):                  # (the second: rows of one token each, whose stride says nothing)
+        near, apart = [[t[:, lead] for t in ts] for ts in ((q, k, v), far)]
+        o, lse = kla.kla_attn_fwd(*(t.contiguous() for t in near))
+        o2, lse2 = kla.kla_attn_fwd(*apart)
+        assert torch.equal(bits(o), bits(o2)) and torch.equal(bits(lse), bits(lse2))
+        a, b = (kla.kla_attn_bwd(*ts, o, lse, o) for ts in ([t.contiguous() for t in near], apart))
+        assert all(torch.equal(bits(a[x]), bits(b[x])) for x in a)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_many_workgroups(kla, dtype):
     """Enough rows for the form in which four waves share tiles of keys; a window keeps the oracle quick."""
