@@ -445,10 +445,6 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
 
 template <typename A, typename K> hipError_t launch_units(A& a, K kernel, int lds, long units, hipStream_t st)
 {
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-    }
     const long most = most_blocks(256);
     for (a.f.unit0 = 0; a.f.unit0 < units; a.f.unit0 += most) {
         kernel<<<dim3((unsigned)(units - a.f.unit0 < most ? units - a.f.unit0 : most)), dim3(256), lds, st>>>(a);

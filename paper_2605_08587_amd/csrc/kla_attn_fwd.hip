@@ -354,10 +354,6 @@ template <typename T, int D, int RW, int KW, bool PAGED> hipError_t launch(AttnA
 {
     using F = Fwd<T, D, RW, KW, PAGED>;
     const auto kernel = attn_fwd_kernel<T, D, RW, KW, PAGED>;
-    if (F::LDS > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, F::LDS);
-        if (e != hipSuccess) return e;
-    }
     const long units = a.tiles * a.Hk * a.splits, most = most_blocks(64 * F::W);
     for (a.unit0 = 0; a.unit0 < units; a.unit0 += most) {
         kernel<<<dim3((unsigned)(units - a.unit0 < most ? units - a.unit0 : most)), dim3(64 * F::W), F::LDS, st>>>(a);
