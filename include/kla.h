@@ -471,7 +471,8 @@ int kla_gated_norm_bwd(const void *x, long ld_x, const void *gate, long ld_gate,
  *   - T H / Hk at most 2^30, H / Hk at most 2^16, H D and strides at most 2^24 elements, scale positive and finite.
  *   - Scores, softmax and sums are fp32; weights are rounded to dt where they are multiplied with values, outputs once.
  *     Results are deterministic (no atomics).  A key that a query does not see has no part in its row, also where it holds a NaN.  A
- *     row whose scores are all -inf, or one of whose scores is +inf or NaN, is NaN.
+ *     row whose scores are all -inf, or one of whose scores is +inf or NaN, is NaN; an infinite value makes o infinite, or a NaN where
+ *     its weight is 0 in fp32.
  *   - An output must not overlap an input.
  * ------------------------------------------------------------------------------------------------------------------ */
 enum { KLA_ATTN_CAUSAL = 1 };

@@ -100,6 +100,7 @@ def test_many_workgroups(kla, dtype):
     """Enough rows for the form in which four waves share tiles of keys; a window keeps the oracle quick."""
     _run(kla, dtype, (6, 700), 16, 8, 64 if dtype == torch.float32 else 128, window=90, seed=5)
     _run(kla, dtype, (1, 500), 66, 66, 64, seed=6, wide=True)
+    _run(kla, dtype, (4, 610), 16, 16, 128, window=40, seed=22)
     _run(kla, dtype, (1, 320 * 20), 4, 4, 128, lengths=[320, 321, 319] * 6 + [640], window=70, seed=7, wide=True)
 
 
@@ -144,7 +145,7 @@ def _expected(kind, q, k, v, d_o, scale, causal, window):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("T,H,Hk,causal,window", [(150, 4, 2, True, 0), (150, 4, 2, True, 37), (90, 2, 2, False, 0), (300, 66, 66, True, 50)])
+@pytest.mark.parametrize("T,H,Hk,causal,window", [(150, 4, 2, True, 0), (150, 4, 2, True, 37), (90, 2, 2, False, 0), (300, 66, 66, True, 50), (650, 90, 90, True, 50), (650, 90, 90, False, 0)])
 @pytest.mark.parametrize("where,value", [("v", INF), ("v", NAN), ("v", -INF), ("k", NAN), ("q", NAN), ("d_o", INF), ("d_o", NAN), ("q", INF)])
 def test_what_is_not_finite_stays_where_it_is_seen(kla, dtype, T, H, Hk, causal, window, where, value):
     """One token's row holds an infinity or a NaN: rows and keys that do not meet it are as if it were not there, and those that do are infinite or NaN

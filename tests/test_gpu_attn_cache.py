@@ -89,7 +89,9 @@ def _extend(kla, c, scale=None, window=0, max_len=None, fixed=False, **kw):
     (6, 2, 64, 16, [200, 0, 7], [0, 33, 1], 0), (3, 1, 128, 128, [300, 1000], [50, 70], 0), (4, 4, 128, 16, [77, 300], [130, 1], 40),
     (4, 2, 64, 1024, [900, 1500], [200, 7], 1), (16, 2, 128, 16, [333, 1200], [9, 2], 100), (5, 5, 64, 64, [2000], [300], 0)])
 def test_new_tokens(kla, dtype, H, Hk, D, page, cached, new, window):
-    _extend(kla, Case(len(cached) + page, dtype, H, Hk, D, page, cached, new), window=window)
+    c = Case(len(cached) + page, dtype, H, Hk, D, page, cached, new)
+    _extend(kla, c, window=window)
+    _extend(kla, c, window=window, max_len=2 ** 31 - 1)      # (rows beyond 32: four waves that share tiles)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -167,12 +169,14 @@ def test_sequences_that_share_pages(kla):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
-def test_later_tokens_that_are_not_finite(kla, dtype, value):
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cached,max_len", [(50, None), (50, 2 ** 31 - 1), (3000, None), (3000, 2 ** 31 - 1)])
+def test_later_tokens_that_are_not_finite(kla, dtype, value, D, cached, max_len):
     """A new token's values are seen from it on only, whatever they are."""
-    c = Case(5, dtype, 4, 2, 64, 16, [50], [40])
+    c = Case(5, dtype, 4, 2, D, 16, [cached], [40])
     c.v[0, 20, 1, 3] = value
     kc, vc = c.kc.clone(), c.vc.clone()
-    o = kla.kla_attn_extend(c.q, c.k, c.v, kc, vc, c.table, c.cached)[0]
+    o = kla.kla_attn_extend(c.q, c.k, c.v, kc, vc, c.table, c.cached, max_len=max_len)[0]
     assert torch.isfinite(o[:20]).all() and torch.isfinite(o[:, :2]).all() and torch.isfinite(o[..., 4:]).all()
     x = o[20:, 2:, 3].float()
     assert (torch.isnan(x) if value != value else x == value).all()
