@@ -258,6 +258,7 @@ template <int ROWS> __device__ __forceinline__ bool find_rows(const Seqs& s, int
 inline long row_places(const Seqs& s, long M, int G, int rows, long* per)
 {
     *per = ((long)s.T * G + rows - 1) / rows;
+    if (M == 0) return 0;
     return s.cu ? M * G / rows + s.n_seq : *per * s.n_seq;
 }
 
