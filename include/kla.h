@@ -506,7 +506,8 @@ int kla_attn_bwd(const void *q, long ld_q, const void *k, long ld_k, const void 
  *   cached      [sequences] int32                   in   device; taken as at least 0 and at most max_pages page
  *   o           [N, T, H, D] dt, lse [N, T, H] fp32 or NULL    out
  *   max_len     a bound of cached + new tokens for how the work is cut: results beyond it are right, but slower
- * Only entries of positions in some query's window that lie below `cached` are read, and those of new tokens.  An entry that is no page (below 0 or
+ * Entries matter for positions below `cached` in some query's window, and for new tokens.  Others in the row's first max_pages may be read
+ * too, and the pages that they name, without a part in any result.  An entry that is no page (below 0 or
  * from n_pages on) reads as the nearest page that is one, and nothing is stored through it; nor are new tokens at positions from
  * max_pages page on.  A page that new tokens go to must not be read or written through another entry in the same call.
  * max_pages page at most 2^30.  workspace 256-byte aligned. */

@@ -189,8 +189,6 @@ __device__ __forceinline__ void add_product(floatx16 (&acc)[NDT], const char* ti
 
 // All of this wave's copies have landed, and its LDS reads are done; then every wave's.
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
-// all but the last N of them
-template <int N> __device__ __forceinline__ void wait_but_and_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_copies_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // This thread, for a second run of a workgroup's work behind a first: what is derived from it anew is not kept in registers through the first.

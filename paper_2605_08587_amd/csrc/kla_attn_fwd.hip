@@ -12,7 +12,8 @@
 // bf16, D = 128, 16 heads over 4, 16384 tokens: 1.03 PFLOP/s, 8192 tokens both ways 1.01, where a matrix product of 8192^3 reaches 1.37 on the same card; D = 64: 0.84,
 // bound by the exponentials and the other 4.5 instructions per score.  Tried and left: scores formed a tile ahead and interleaved with this tile's
 // exponentials (two workgroups to a CU do as much: 3 to 10 % slower with a barrier per 32 keys), eight waves to a tile (1 %), tiles of 64 rows
-// (no gain at any size), priorities around the products (none).
+// (no gain at any size), priorities around the products (none), two groups of four waves half a tile apart, so that one's products stand beside the
+// other's exponentials (none; D = 64: 10 % slower), three stages of keys (D = 64: 6 % slower).
 #include "kla_attn.hpp"
 
 namespace kla {
@@ -363,7 +364,8 @@ template <typename T, int D, int RW, int KW, bool PAGED> hipError_t launch(AttnA
 }
 
 // The parts of a row joined: sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A row has D / 4 threads for its features times SG for its parts, so that all
-// of a row's parts are on their way at once (64 at most: lane s of every wave has part s's weight).
+// of a row's parts are on their way at once (64 at most: lane s of every wave has part s's weight).  3.6 us for 16 rows, of which most is the launch
+// and three trips to memory behind each other, 17 us for 26000 rows of 128.
 template <typename T, int D, int SG> __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs<T> a, long row0)
 {
     constexpr int TPR = D / 4, ROWS = 256 / (TPR * SG), BATCH = 8;
