@@ -204,6 +204,18 @@ __device__ __forceinline__ int thread_again()
 __device__ __forceinline__ void settle(u32x4& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void settle(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
+// what all lanes have alike, in a scalar register (quotients come out of the vector ALU, and what is formed from them stays there)
+__device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long wave_uniform(long x)
+{
+    return (long)((uint64_t)(uint32_t)wave_uniform((int)x) | (uint64_t)(uint32_t)wave_uniform((int)(x >> 32)) << 32);
+}
+// Accumulators stay what they are here: registers behind each other (as 16 values each, a loop that scales them moved every one to another register)
+template <int N> __device__ __forceinline__ void keep_whole(floatx16 (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
 // row i of rows `stride` bytes apart (one multiplication of 32 bits)
 __device__ __forceinline__ const char* row_at(const char* p, int i, uint32_t stride) { return p + (uint64_t)(uint32_t)i * stride; }
 
