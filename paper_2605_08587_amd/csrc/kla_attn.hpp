@@ -103,16 +103,32 @@ template <int PIECES> __host__ __device__ constexpr int row_swz(int row)
     if (PIECES == 8) return ((row >> 1 & 1) << 2) | (row >> 2 & 3);
     return ((row & 3) << 2) | (row >> 2 & 3);
 }
+// what all lanes have alike, in a scalar register (quotients come out of the vector ALU, and what is formed from them stays there)
+__device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long wave_uniform(long x)
+{
+    return (long)((uint64_t)(uint32_t)wave_uniform((int)x) | (uint64_t)(uint32_t)wave_uniform((int)(x >> 32)) << 32);
+}
+__device__ __forceinline__ const char* wave_uniform(const char* p) { return reinterpret_cast<const char*>(wave_uniform((long)p)); }
+__device__ __forceinline__ uint32_t lds_place(char* wave_base)
+{
+    return (uint32_t)wave_uniform((int)(uint32_t)(uintptr_t)((__attribute__((address_space(3))) char*)wave_base));
+}
 // 16 bytes per lane from the lane's address to LDS at lds_wave_base + 16 lane (as dma16, with an address of 64 bits)
 __device__ __forceinline__ void dma16_from(const char* lane_address, char* lds_wave_base)
 {
     const uint32_t m = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) char*)lds_wave_base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(lane_address), "s"(m) : "memory");
 }
+// from base + lane_off, base the wave's (as dma16, where the compiler has formed the places on the vector ALU)
+__device__ __forceinline__ void dma16_at(const char* base, int lane_off, char* lds_wave_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(wave_uniform(base)), "s"(lds_place(lds_wave_base)) : "memory");
+}
 // 4 bytes per lane, to lds_wave_base + 4 lane
 __device__ __forceinline__ void dma4_from(const void* lane_address, char* lds_wave_base)
 {
-    const uint32_t m = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) char*)lds_wave_base);
+    const uint32_t m = lds_place(lds_wave_base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(lane_address), "s"(m) : "memory");
 }
 // A tile of rows of D elements of T
@@ -204,12 +220,6 @@ __device__ __forceinline__ int thread_again()
 __device__ __forceinline__ void settle(u32x4& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void settle(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
-// what all lanes have alike, in a scalar register (quotients come out of the vector ALU, and what is formed from them stays there)
-__device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long wave_uniform(long x)
-{
-    return (long)((uint64_t)(uint32_t)wave_uniform((int)x) | (uint64_t)(uint32_t)wave_uniform((int)(x >> 32)) << 32);
-}
 // Accumulators stay what they are here: registers behind each other (as 16 values each, a loop that scales them moved every one to another register)
 template <int N> __device__ __forceinline__ void keep_whole(floatx16 (&x)[N])
 {
