@@ -75,7 +75,7 @@ kla::AttnPlan extend_plan(const kla::Seqs& s, const int32_t* cu_host, int G, int
     // that few keys to a part cost bandwidth; below one workgroup for each CU parts of 128 keys still gain.  (bf16, D = 128: 32 tokens over 4000 to 32000
     // keys, 4 key heads: parts for 512, 1024 and 2048 workgroups 242, 228 and 230 us; 16 x 5 tokens over 2000 to 8000: 47, 57 and 76 us; one token
     // over 4096: parts of 128 and 256 keys 11.1 and 12.4 us.)  More rows: two workgroups to a CU; parts are written and read in fp32 (four
-    // sequences of 300 to 518 new tokens over 4126 to 13917: for 512, 1024 and 2048 workgroups 234, 257 and 284 us).
+    // sequences of 300 to 518 new tokens over 4126 to 13917: for 256, 512, 1024 and 2048 workgroups 220, 215, 233 and 261 us).
     if (p.rows == 32) {
         const long fill = (256 + units - 1) / units, most = (span + 1023) / 1024;
         long want = (1024 + units - 1) / units;
