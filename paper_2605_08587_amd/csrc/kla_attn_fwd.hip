@@ -71,6 +71,17 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
             }
             return;
         }
+        // Keys that are all there: the same, rows a stride apart.  (8 multiplications of 64 bits less for each tile: 4 x 1500 tokens both ways, heads of 64, 39.5 -> 38.1 us.)
+        if (!PAGED && j0 + BN - 1 <= last) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES;
+                const int piece = ((lane % Tile::PIECES) ^ row_swz<Tile::PIECES>(row)) * 16;
+                dma16(row_at(kn, j0 + first, ldk), (int)(lane / Tile::PIECES * ldk) + piece, stage + first * Tile::RB);
+                dma16(row_at(vn, j0 + first, ldv), (int)(lane / Tile::PIECES * ldv) + piece, stage + first * Tile::RB + TILE);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int first = wave * ROWS + i * RPI, row = first + lane / Tile::PIECES;
@@ -83,9 +94,9 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
                 dma16_from((old ? reinterpret_cast<const char*>(a.k_cache) + at : row_at(kn, fresh, ldk)) + piece, to);
                 dma16_from((old ? reinterpret_cast<const char*>(a.v_cache) + at : row_at(vn, fresh, ldv)) + piece, to + TILE);
             } else {
-                const int i0 = min(row, last - j0);      // (tiles begin at keys that are there)
-                dma16(row_at(kn, j0, ldk), (int)(i0 * ldk + piece), to);
-                dma16(row_at(vn, j0, ldv), (int)(i0 * ldv + piece), to + TILE);
+                const int j = min(j0 + row, last);
+                dma16_from(row_at(kn, j, ldk) + piece, to);
+                dma16_from(row_at(vn, j, ldv) + piece, to + TILE);
             }
         }
     }
@@ -193,7 +204,7 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
             if constexpr (PAGED) asm volatile("" : "+v"(ids));       // (awaited with the copies, not behind the ones that follow)
             if constexpr (RW > 1) wait_copies_and_barrier();
             else wait_copies();
-            if constexpr (RW > 1) keep_whole(s.o);
+            if constexpr (RW > 1 || !PAGED) keep_whole(s.o);
             const int j0 = j_first + t * BN;
             char* stage = ring + ((t - tb) & 1) * STAGE;
             if (t + 1 < te) copy(a, k, j0 + BN, last, ids, ring + ((t - tb + 1) & 1) * STAGE, cw, lane);
