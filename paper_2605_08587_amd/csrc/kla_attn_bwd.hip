@@ -9,9 +9,9 @@
 // keys (or rows) as the columns of its accumulators; p and ds come out of S = Q K^T as the B operands of the products behind it.  p and ds are fp32
 // and rounded to the inputs' type where they enter a product; sums are fp32.
 //
-// bf16, 8 x 4096 tokens, 8 heads of 128, causal: dk, dv 601 us (0.91 PFLOP/s), dq 434 us (0.95), delta 32 us (200 MB at 6.3 TB/s);
+// bf16, 8 x 4096 tokens, 8 heads of 128, causal: dk, dv 618 us (0.89 PFLOP/s), dq 441 us (0.94), delta 32 us (200 MB at 6.3 TB/s);
 // bound by the vector ALU beside the matrix pipe, and by the clocks.  6 sequences of 1000 to 5000 tokens, window 1024, 16 heads over 4 of 64: dk, dv
-// 252 us, where 564 workgroups come to 512 places, dq 121 us.
+// 251 us, where 564 workgroups come to 512 places, dq 123 us.
 #include "kla_attn.hpp"
 
 namespace kla {

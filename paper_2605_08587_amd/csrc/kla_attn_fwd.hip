@@ -9,7 +9,7 @@
 // exp(m).  (The quotient does not depend on m.  A factor of 2^8 in place of 2 saves 3 % of the time, but then a row's largest weights are rounded like the others
 // instead of being powers of two: error of o 2.1e-3 of its norm instead of 1.8e-3, of dq behind it 2.7e-3 instead of 2.4e-3; a factor of 1 is no better than 2.)
 //
-// bf16, D = 128, 16 heads over 4, 16384 tokens: 1.05 PFLOP/s, 8192 tokens both ways 1.03, where a matrix product of 8192^3 reaches 1.40 on the same card; D = 64: 0.86,
+// bf16, D = 128, 16 heads over 4, 16384 tokens: 1.06 PFLOP/s, 8192 tokens both ways 1.04, where a matrix product of 8192^3 reaches 1.39 on the same card; D = 64: 0.87,
 // bound by the exponentials and the other 4.5 instructions per score.  Tried and left: scores formed a tile ahead and interleaved with this tile's
 // exponentials (two workgroups to a CU do as much: 3 to 10 % slower with a barrier per 32 keys), eight waves to a tile (1 %), tiles of 64 rows
 // (no gain at any size), priorities around the products (none), two groups of four waves half a tile apart, so that one's products stand beside the
