@@ -72,6 +72,14 @@ def test_packed(kla, dtype, lengths, H, Hk, D, kw):
     _run(kla, dtype, (1, sum(lengths)), H, Hk, D, lengths=lengths, wide=True, seed=len(lengths), **kw)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,H,Hk,window", [(70, 32, 2, 0), (41, 32, 1, 0), (90, 64, 1, 20), (21, 48, 1, 0), (17, 128, 1, 0), (19, 80, 1, 7)])
+def test_wide_groups(kla, dtype, D, T, H, Hk, window):
+    """Heads of a group that fill a tile, divide it, or go over several."""
+    _run(kla, dtype, (1, T), H, Hk, D, window=window, wide=True, seed=T)
+
+
 def test_thousands_of_sequences(kla):
     """More than 64 x 64 sequences, most of them empty: a tile's sequence is looked for in three steps."""
     lengths = [0, 1, 0, 0, 2, 0, 0, 0, 0, 1] * 600
