@@ -103,6 +103,12 @@ def kla_attn_bwd(q, k, v, o, lse, d_o, scale=None, causal=True, window=0, cu_seq
     return g
 
 
+def _at_16_bytes(t):
+    """Contiguous and at a multiple of 16 bytes: a gradient can be a piece of a larger tensor, wherever it begins."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class _Attn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, scale, causal, window, cu_seqlens, cu_seqlens_host):
@@ -118,7 +124,7 @@ class _Attn(torch.autograd.Function):
     def backward(ctx, d_o):
         _no_second("kla_attn")
         *saved, rest = ctx.saved_tensors
-        g = kla_attn_bwd(*saved, d_o.contiguous(), *ctx.misc, rest=rest, **ctx.offsets.check())
+        g = kla_attn_bwd(*saved, _at_16_bytes(d_o), *ctx.misc, rest=rest, **ctx.offsets.check())
         return (*g.values(), None, None, None, None, None)
 
 

@@ -89,6 +89,13 @@ struct Attn : Heads {
     }
 };
 
+// Contiguous and at a multiple of 16 bytes: a gradient can be a piece of a larger tensor, wherever it begins.
+at::Tensor at_16_bytes(const at::Tensor& t)
+{
+    const at::Tensor c = t.contiguous();
+    return reinterpret_cast<uintptr_t>(c.data_ptr()) % 16 ? c.clone() : c;
+}
+
 struct AttnNode : public torch::autograd::Function<AttnNode> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v,
                                                   const Attn* c, const at::Tensor* host)
@@ -117,7 +124,7 @@ struct AttnNode : public torch::autograd::Function<AttnNode> {
         const at::Tensor *o = gpu(s[3], c.type, c.q->sizes()), *lse = gpu(s[4], at::kFloat, {c.N, c.T, c.H}), *rest;
         taken(o && lse && gpu_or_none(s[5], at::kBFloat16, c.q->sizes(), &rest) && together({o, lse, rest}), "kla_attn");
         if (!grads[0].defined()) return {at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
-        refused("kla_attn_bwd", [&] { c.bwd(*o, *lse, rest, grads[0].contiguous(), g); });
+        refused("kla_attn_bwd", [&] { c.bwd(*o, *lse, rest, at_16_bytes(grads[0]), g); });
         return {g[0], g[1], g[2], at::Tensor(), at::Tensor()};
     }
 };

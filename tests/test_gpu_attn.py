@@ -259,6 +259,26 @@ def test_autograd(kla, monkeypatch, native):
         torch.autograd.grad(y, leaves, d_o)
 
 
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("before", [1, 3, 8])
+def test_gradients_at_any_address(kla, monkeypatch, native, dtype, before):
+    """Autograd hands over a piece of a larger gradient, wherever it begins."""
+    if not native:
+        monkeypatch.setattr(kla, "_native", kla._StepByStep)
+    q, k, v, d_o = _inputs(23, dtype, (2, 70), 4, 2, 64)
+    o, lse = kla.kla_attn_fwd(q, k, v)
+    leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+    want = torch.autograd.grad(kla.kla_attn(*leaves), leaves, d_o)
+    seen = []
+    y = kla.kla_attn(*leaves)
+    y.register_hook(lambda g: seen.append(g.data_ptr() % 16))
+    together = torch.cat([torch.zeros(before, device="cuda", dtype=dtype), y.flatten()])
+    have = torch.autograd.grad(together, leaves, torch.cat([torch.ones(before, device="cuda", dtype=dtype), d_o.flatten()]))
+    assert seen == [before * q.element_size() % 16]          # (or this tests nothing)
+    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(have, want))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_gradients_by_differences(kla, dtype):
     """<d, gradient> against the forward's own differences, in steps large enough for its rounding."""
