@@ -50,3 +50,19 @@ def check(lengths, q, k, v, o, lse, scale, causal, window, d_o=None, grads=None,
             for name, x, r, bb in zip(("dq", "dk", "dv"), grads, ao.backward(*a, g, scale, **kw), b[2:]):
                 within(tag + " " + name, x[here], r, bb)
         at += n
+
+
+# Batches that come to at least 512 tiles of 128 query rows: lengths, packed or not, query heads of a key head, key heads, causal, window
+MANY_TILES = {
+    "one head each": ([140], False, 1, 260, True, 0),
+    "groups of three": ([200], False, 3, 104, True, 0),
+    "packed, groups of four, window": ([130, 1, 257, 60], True, 4, 31, True, 70),
+    "packed, window, one head each": ([200, 0, 129, 300], True, 1, 75, True, 33),
+    "both ways": ([150, 150], False, 1, 130, False, 0),
+    "packed, both ways, groups of four": ([129, 64], True, 4, 74, False, 0),
+}
+
+
+def many_tiles(name):
+    lengths, _packed, G, Hk, _causal, _window = MANY_TILES[name]
+    return sum(-(-n * G // 128) for n in lengths) * Hk

@@ -1,12 +1,14 @@
 """Host-side checks of softmax attention that need no GPU: every refusal comes before anything is launched (the pointers are fakes), the workspace queries,
 and what the Python functions refuse."""
 import os
+import re
 
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_08587_amd as kla
+from attn_cases import MANY_TILES, many_tiles
 
 pytestmark = pytest.mark.skipif(not os.path.exists(kla.LIB_PATH), reason="libkla.so not built (python -m paper_2605_08587_amd.build)")
 
@@ -216,3 +218,11 @@ def test_python_refusals():
 @pytest.mark.parametrize("f", [fwd, bwd, extend, step])
 def test_groups_beyond_the_limit(f):
     assert f(H=(1 << 16) + 1, Hk=1, ld_q=1 << 23) == E_SHAPE
+
+
+def test_cases_of_many_tiles_reach_their_kernels():
+    """The batches of MANY_TILES come to as many tiles as the library asks for before it takes the kernels that they are there for."""
+    src = open(os.path.join(os.path.dirname(kla.__file__), "csrc", "kla_attn_api.hip")).read()
+    apart = int(re.search(r"constexpr long kAttnBeside = (\d+);", src).group(1))
+    share = [int(x) for x in re.search(r"units >= \(D == 64 \? (\d+) : (\d+)\) \? 128 : 32", src).groups()]
+    assert min(many_tiles(n) for n in MANY_TILES) >= max(apart, *share)
