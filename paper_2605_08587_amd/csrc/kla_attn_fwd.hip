@@ -409,7 +409,7 @@ template <typename T, int D, int SG> __global__ __launch_bounds__(256) void attn
     float m = lse;
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    const float w = m == -__builtin_inff() ? 0.f : exp2_hw(lse - m);
+    const float w = lse == -__builtin_inff() ? 0.f : exp2_hw(lse - m);          // (a NaN among parts of -inf, which m does not show, stays one)
     const float l = wave_sum(w);
     Floats<4> x = {{0.f, 0.f, 0.f, 0.f}};
     if (parts > 1)                                       // (one part is the result, and stands in o)

@@ -203,6 +203,23 @@ def test_caches_beyond_32_bits(kla):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cached,new,max_len", [(3000, 1, None), (3000, 40, 2 ** 31 - 1), (60, 1, None)])
+def test_scores_that_are_minus_infinity_or_nan(kla, dtype, cached, new, max_len):
+    """Keys in several parts: a NaN among scores of -inf is a NaN in o and lse, as the formulas have it, in whichever part it stands."""
+    for at in (None, 5, cached // 2, cached - 1):
+        c = Case(15, dtype, 4, 2, 64, 16, [cached], [new])
+        c.q[..., 0] = 1.0
+        c.k[..., 0] = -float("inf")
+        c.kc[..., 0] = -float("inf")                         # (the whole cache: every old key, and what holds none)
+        if at is not None:
+            page = c.table[0, at // 16].item()
+            c.kc[page, :, at % 16, 1] = float("nan")
+        o, lse = kla.kla_attn_extend(c.q, c.k, c.v, c.kc, c.vc, c.table, c.cached, want_lse=True, max_len=max_len)
+        assert torch.isnan(o).all(), at
+        assert (lse == -float("inf")).all() if at is None else torch.isnan(lse).all(), at
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_a_prompt_whole_by_chunks_and_by_tokens(kla, dtype):
     """One prompt: at once without a cache, in chunks over one, and its last tokens one at a time in a captured graph whose lengths advance on the device."""
     H, Hk, D, T, page, window = 8, 2, 64, 150, 16, 60
