@@ -3,7 +3,8 @@ Argument marshalling only, as in the package itself: every step runs in the HIP 
 
 kla_attn_fwd / kla_attn_bwd are the two directions and kla_attn the differentiable call; kla_attn_extend takes new tokens of several sequences over
 their cached ones, kla_attn_step one token of each.  q [..., H, D] and k, v [..., Hk, D] may be column ranges of a wider tensor: the heads
-of a token are contiguous, the tokens evenly spaced, and a row starts at a multiple of 16 bytes.
+of a token are contiguous, the tokens evenly spaced and at most 2^24 elements apart, and a row starts at a multiple of 16 bytes.  (Single tokens over
+a cache that are further apart, like q[:, t] of a long batch, are copied first.)
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ from . import _check, _dev, _dt, _ptr, _stream, _written, _ws_bytes, lib
 from .layer import _Offsets, _batch, _call, _eager, _host, _native, _no_second, _on_gpu, _rows, _sizes, _workspace
 
 KLA_ATTN_CAUSAL = 1
+MAX_STRIDE = 2 ** 24                                     # elements from one token to the next
 
 _vp, _i, _l, _f, _z, _u = ctypes.c_void_p, ctypes.c_int, ctypes.c_long, ctypes.c_float, ctypes.c_size_t, ctypes.c_uint
 _SEQS = [_vp, _vp, _i]
@@ -47,7 +49,16 @@ def _heads(q, k, v, lead):
     _check("v", v, (*at, Hk, D), q.dtype)
     if Hk == 0 or H % Hk:
         raise ValueError("%d query heads cannot share %d key heads evenly" % (H, Hk))
-    return H, Hk, D, dt, (_rows("q", q, 2), _rows("k", k, 2), _rows("v", v, 2))
+    ld = _rows("q", q, 2), _rows("k", k, 2), _rows("v", v, 2)
+    for name, n in zip("qkv", ld):
+        if n > MAX_STRIDE:
+            raise ValueError("%s: the tokens are %d elements apart, more than 2^24" % (name, n))
+    return H, Hk, D, dt, ld
+
+
+def _near(*ts):
+    """Single tokens, one of each sequence: a copy of those that are too far apart, like a position of all sequences of a long batch."""
+    return [t.contiguous() if t.dim() > 2 and _rows(name, t, 2) > MAX_STRIDE else t for name, t in zip("qkv", ts)]
 
 
 def kla_attn_fwd(q, k, v, scale=None, causal=True, window=0, cu_seqlens=None, cu_seqlens_host=None, want_lse=True, out=None, lse=None, rest=None):
@@ -165,6 +176,8 @@ def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, w
                     bool(want_lse), out, lse)
         if r is not None:
             return r if r[1] is not None else r[0]
+    if cu_seqlens is None and q.dim() == 4 and q.shape[1] == 1:
+        q, k, v = _near(q, k, v)
     H, Hk, D, dt, ld = _heads(q, k, v, 2)
     N, T = q.shape[:2]
     _, cu_hp, n_seq, n = _batch(q, cu_seqlens, host)
@@ -196,6 +209,7 @@ def kla_attn_step(q, k, v, k_cache, v_cache, page_table, cached, scale=None, win
         r = _native("attn_step", "kla_attn_step", q, k, v, k_cache, v_cache, page_table, cached, _scale(scale, q), window, max_len, out)
         if r is not None:
             return r
+    q, k, v = _near(q, k, v)
     H, Hk, D, dt, ld = _heads(q, k, v, 1)
     B = q.shape[0]
     _sizes(window)

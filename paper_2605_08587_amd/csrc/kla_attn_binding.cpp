@@ -24,6 +24,8 @@ PyObject* bind_attn(PyObject*, PyObject* const* a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+constexpr long kMaxStride = 1L << 24;                    // elements from one token to the next (beyond: Python's half copies or refuses)
+
 // Queries, keys and values of new tokens; lead: leading dimensions, [N, T] or (a step) [B]
 struct Heads {
     const at::Tensor *q, *k, *v;
@@ -42,7 +44,7 @@ struct Heads {
         N = q->size(0); T = lead == 2 ? q->size(1) : 1; H = q->size(lead); D = q->size(lead + 1); Hk = k->size(lead);
         const at::DimVector keys = lead == 2 ? at::DimVector({N, T, Hk, D}) : at::DimVector({N, Hk, D});
         return ints({N, T, H, Hk, D}) && Hk > 0 && H % Hk == 0 && rows(q_, type, q->sizes(), 2, &ld_q) && (k = rows(k_, type, keys, 2, &ld_k)) &&
-               (v = rows(v_, type, keys, 2, &ld_v));
+               (v = rows(v_, type, keys, 2, &ld_v)) && ld_q <= kMaxStride && ld_k <= kMaxStride && ld_v <= kMaxStride;
     }
     bool scaled(PyObject* o)
     {

@@ -215,6 +215,24 @@ def test_python_refusals():
                 kla.kla_attn_extend(q, k, k, **d)
 
 
+def test_python_refuses_tokens_too_far_apart():
+    """By the name of the tensor and the limit; single tokens over a cache are not refused for it."""
+    q = torch.empty_strided((1, 2, 8, 64), (1 << 26, (1 << 24) + 4, 64, 1))
+    k = torch.zeros(1, 2, 4, 64)
+    c, table, cached = torch.zeros(10, 4, 16, 64), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    lse = torch.zeros(1, 2, 8)
+    for f in (lambda a, b, v: kla.kla_attn_fwd(a, b, v), lambda a, b, v: kla.kla_attn(a, b, v), lambda a, b, v: kla.kla_attn_bwd(a, b, v, k, lse, k),
+              lambda a, b, v: kla.kla_attn_extend(a, b, v, c, c, table[:1], cached[:1])):
+        with pytest.raises(ValueError, match=r"q: the tokens .* 2\^24"):
+            f(q, k, k)
+        with pytest.raises(ValueError, match=r"v: the tokens .* 2\^24"):
+            f(k.repeat(1, 1, 2, 1), k, q[:, :, :4])
+    with pytest.raises(RuntimeError, match="GPU"):
+        kla.kla_attn_step(q[0], k[0], k[0], c, c, table, cached)
+    with pytest.raises(RuntimeError, match="GPU"):
+        kla.kla_attn_extend(q.transpose(0, 1), k.transpose(0, 1), k.transpose(0, 1), c, c, table, cached)
+
+
 @pytest.mark.parametrize("f", [fwd, bwd, extend, step])
 def test_groups_beyond_the_limit(f):
     assert f(H=(1 << 16) + 1, Hk=1, ld_q=1 << 23) == E_SHAPE

@@ -203,6 +203,32 @@ def test_caches_beyond_32_bits(kla):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("native", [True, False])
+def test_single_tokens_far_apart(kla, monkeypatch, native, dtype):
+    """The t-th token of each sequence of a long batch: more than 2^24 elements from one to the next."""
+    if not native:
+        monkeypatch.setattr(kla, "_native", kla._StepByStep)
+    c = Case(14, dtype, 8, 2, 128, 16, [70, 0], [1, 1])
+    T = (1 << 24) // (2 * 128) + 8
+    far = []
+    for x in (c.q, c.k, c.v):
+        w = torch.empty(2, T if x is not c.q else T // 4 + 2, *x.shape[2:], dtype=dtype, device="cuda")
+        w[:, 7] = x[0]
+        assert w.stride(0) > 1 << 24
+        far.append(w[:, 7:8])
+    for q, k, v in (far, (far[0], c.k.view(2, 1, 2, 128), far[2])):
+        kc, vc = c.kc.clone(), c.vc.clone()
+        c.check(kla.kla_attn_step(q[:, 0], k[:, 0], v[:, 0], kc, vc, c.table, c.cached), None, 128 ** -0.5, 0, kc, vc)
+        kc, vc = c.kc.clone(), c.vc.clone()
+        o, lse = kla.kla_attn_extend(q, k, v, kc, vc, c.table, c.cached, want_lse=True)
+        c.check(o[:, 0], lse[:, 0], 128 ** -0.5, 0, kc, vc)
+    with pytest.raises(ValueError, match="2\\^24"):
+        kla.kla_attn_fwd(*far)
+    with pytest.raises(ValueError, match="2\\^24"):
+        kla.kla_attn(*far)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("cached,new,max_len", [(3000, 1, None), (3000, 40, 2 ** 31 - 1), (60, 1, None)])
 def test_scores_that_are_minus_infinity_or_nan(kla, dtype, cached, new, max_len):
     """Keys in several parts: a NaN among scores of -inf is a NaN in o and lse, as the formulas have it, in whichever part it stands."""
