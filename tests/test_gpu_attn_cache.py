@@ -202,6 +202,28 @@ def test_caches_beyond_32_bits(kla):
         assert torch.equal(bits(kc[far[i].item()]), bits(k2[i].nan_to_num(0))) and torch.equal(bits(vc[far[i].item()]), bits(v2[i].nan_to_num(0)))
 
 
+def test_caches_of_more_than_2_to_32_elements(kla):
+    """Pages whose elements, not only their bytes, lie beyond 2^32 of the cache, for single tokens and for chunks."""
+    P, Hk, page, D = 4200, 8, 1024, 128
+    c = Case(13, torch.bfloat16, 8, Hk, D, page, [1500, 900, 1000], [1, 1, 70], room=0)
+    kc, vc = (torch.empty(P, Hk, page, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    far = [P - 1 - i for i in range(len(c.kc))]
+    assert min(far) * Hk * page * D > 2 ** 32
+    table = torch.where(c.table >= 0, torch.tensor(far, device="cuda", dtype=torch.int32)[c.table.clamp(min=0).long()], c.table)
+
+    def calls(kc, vc, table):
+        a = kla.kla_attn_step(c.q[0, :2], c.k[0, :2], c.v[0, :2], kc, vc, table[:2], c.cached[:2])
+        b = [kla.kla_attn_extend(*(t[:, 2:].contiguous() for t in (c.q, c.k, c.v)), kc, vc, table[2:], c.cached[2:], max_len=m) for m in (None, 2 ** 31 - 1)]
+        return (a, *b)
+    for i, p in enumerate(far):
+        kc[p], vc[p] = c.kc[i], c.vc[i]
+    near_k, near_v = c.kc.clone(), c.vc.clone()
+    for x, y in zip(calls(kc, vc, table), calls(near_k, near_v, c.table)):
+        assert torch.isfinite(x).all() and torch.equal(bits(x), bits(y))
+    for i, p in enumerate(far):
+        assert torch.equal(bits(kc[p]), bits(near_k[i])) and torch.equal(bits(vc[p]), bits(near_v[i]))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("native", [True, False])
 def test_single_tokens_far_apart(kla, monkeypatch, native, dtype):
