@@ -158,7 +158,8 @@ template <typename T, int D, int RW, int KW, bool PAGED> struct Fwd {
         // (nothing seen so far: m is -inf and any score above it makes a reference)
         if (__any(top * r.c > s.m * r.c + 1.f)) {
             const float m = fmaxf(s.m, top), mc = m == -__builtin_inff() ? 0.f : m * r.c;
-            const float f = exp2_hw(s.m * r.c - mc);     // (0 from -inf)
+            // From references as they were rounded: exactly 1 for a row whose own has not moved.  (Never above 1, also where nothing was seen so far: sums of zero.)
+            const float f = exp2_hw(fminf(s.mc - mc, 0.f));
             s.m = m; s.mc = mc;
             s.l *= f;
 #pragma unroll

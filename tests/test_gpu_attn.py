@@ -126,6 +126,23 @@ def test_scores_far_apart(kla):
     check([400], q[0], k[0], v[0], o[0], lse[0], 0.125, True, 0)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H,D", [(2, 64), (2, 128), (150, 64), (130, 128)])
+def test_rows_are_not_scaled_for_others(kla, dtype, H, D):
+    """Rows whose largest score comes first keep their reference, and their bits, whatever the rows beside them do: even tokens' scores fall along the
+    keys; odd ones' rise in one call, so that their tile is scaled again and again, and fall in the other."""
+    T = 390
+    _q, _k, v, _ = _inputs(24, dtype, (1, T), H, H, D)
+    q, k = torch.zeros_like(v), torch.zeros_like(v)
+    k[..., 0] = -torch.arange(T, device="cuda").to(dtype)[:, None]
+    q[..., 0] = torch.linspace(0.5, 1.7, H, device="cuda").to(dtype)
+    rising = q.clone()
+    rising[:, 1::2] *= -1
+    (o, lse), (o2, lse2) = (kla.kla_attn_fwd(x, k, v, scale=0.3, causal=False) for x in (q, rising))
+    assert torch.equal(bits(o[:, ::2]), bits(o2[:, ::2])) and torch.equal(bits(lse[:, ::2]), bits(lse2[:, ::2]))
+    assert (lse2[:, 1::2] > lse[:, 1::2] + 40).all()
+
+
 def test_remainder(kla):
     """o and rest together are o before its rounding: what the other rounding of the way, of the weights, leaves is within its own bound."""
     q, k, v, _ = _inputs(20, torch.bfloat16, (1, 150), 4, 2, 64)
