@@ -505,7 +505,8 @@ int kla_attn_bwd(const void *q, long ld_q, const void *k, long ld_k, const void 
  *   page_table  [sequences, max_pages] int32        in   device; rows ld_table apart: entry p holds the page of positions p page ..
  *   cached      [sequences] int32                   in   device; taken as at least 0 and at most max_pages page
  *   o           [N, T, H, D] dt, lse [N, T, H] fp32 or NULL    out
- *   max_len     a bound of cached + new tokens for how the work is cut: results beyond it are right, but slower
+ *   max_len     a bound of cached + new tokens for how the work is cut (tiles of 32 or 128 query rows, parts of the keys): results beyond
+ *               it are right, but slower, and so may be those of sequences far below it
  * Entries matter for positions below `cached` in some query's window, and for new tokens.  Others in the row's first max_pages may be read
  * too, and the pages that they name, without a part in any result.  An entry that is no page (below 0 or
  * from n_pages on) reads as the nearest page that is one, and nothing is stored through it; nor are new tokens at positions from

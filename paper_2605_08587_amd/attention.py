@@ -169,7 +169,7 @@ def kla_attn_extend(q, k, v, k_cache, v_cache, page_table, cached, scale=None, w
     values of position p of sequence s stand in k_cache, v_cache [pages,Hk,page,D] at [page_table[s, p // page], :, p % page] (page_table
     int32, page a power of two from 16 to 1024); those of the new tokens are stored there.  cached is not advanced.  Returns o, with want_lse
     (o, lse).  max_len: a bound of cached + new tokens, if the caller knows a closer one than the table's width (only how the work
-    is cut depends on it)."""
+    is cut depends on it: a chunk over short caches in a wide table can be slower without)."""
     host = _host(cu_seqlens, cu_seqlens_host)
     if workspace is None:
         r = _native("attn_extend", "kla_attn_extend", q, k, v, k_cache, v_cache, page_table, cached, _scale(scale, q), window, cu_seqlens, host, max_len,

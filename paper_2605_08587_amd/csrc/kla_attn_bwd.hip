@@ -10,8 +10,9 @@
 // and rounded to the inputs' type where they enter a product; sums are fp32.
 //
 // bf16, 8 x 4096 tokens, 8 heads of 128, causal: dk, dv 618 us (0.89 PFLOP/s), dq 441 us (0.94), delta 32 us (200 MB at 6.3 TB/s);
-// bound by the vector ALU beside the matrix pipe, and by the clocks.  6 sequences of 1000 to 5000 tokens, window 1024, 16 heads over 4 of 64: dk, dv
-// 251 us, where 564 workgroups come to 512 places, dq 123 us.
+// at 1.7 GHz and with the matrix pipe busy 47 and 49 % of the cycles (counted).  No pipe is full (the vector ALU issues in 37 and 33 % of the cycles, 45 % with an
+// exponential as four): a SIMD has two waves, and they stand at waits and barriers for 34 and 41 % of their time.  6 sequences of 1000 to 5000 tokens, window
+// 1024, 16 heads over 4 of 64: dk, dv 251 us, where 572 workgroups with keys come to 512 places (1.3 waves to a SIMD on the average), dq 123 us.
 #include "kla_attn.hpp"
 
 namespace kla {
